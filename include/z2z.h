@@ -59,7 +59,8 @@ enum {
   Z2Z_ST_TABLE_FULL = 4,     /* hash probe ran through the whole table (cannot happen at load <= 1/2) */
   Z2Z_ST_WAIT_TIMEOUT = 8,   /* a bounded wait inside a kernel gave up                          */
   Z2Z_ST_OUTPUT_TRUNCATED = 16, /* z2z_lzw_decode: the base tokens did not fit in T_out_max      */
-  Z2Z_ST_HALF_RANGE = 32     /* z2z_set_encoder_half_scratch: an encoder weight lies outside fp16's range */
+  Z2Z_ST_HALF_RANGE = 32,    /* z2z_set_encoder_half_scratch: an encoder weight lies outside fp16's range */
+  Z2Z_ST_BAD_PARENT = 64     /* z2z_beam_reorder: no sequence, or one that is overwritten itself; state unchanged */
 };
 
 enum { Z2Z_DTYPE_FP32 = 0, Z2Z_DTYPE_BF16 = 1 };
@@ -247,6 +248,113 @@ int32_t z2z_embed_lookup(z2z_codebook* cb, const int32_t* d_codes, int32_t N,
 int32_t z2z_sample_filtered(const float* d_logits, int32_t N, int64_t ld, const int32_t* d_n_cols,
                             int32_t top_k, float top_p, float temperature, uint64_t seed, uint64_t step,
                             int32_t row_base, int32_t* d_choice, int32_t* d_kept, z2z_stream stream);
+
+/* The same lookup times a scale (models that multiply their input embeddings, e.g. by sqrt(d)):
+ * d_out[r] = scale * row, the product taken in fp32 and rounded once to the configured dtype; rows
+ * without a token are zero.  Arguments, codes and status as for z2z_embed_lookup; scale is finite.
+ * d_out must not overlap the tables.                                                            */
+int32_t z2z_embed_lookup_scaled(z2z_codebook* cb, const int32_t* d_codes, int32_t N,
+                                const int32_t* d_row_seq, const void* d_WE, const void* d_Eh,
+                                float scale, void* d_out, z2z_stream stream);
+
+/* Gradient of z2z_embed_lookup_scaled for its tables, by sorted tokens:
+ *   d_grad_WE[v]    (+)= scale * sum of d_grad_out[r] over the rows r whose code is v
+ *   d_grad_Eh[b][k] (+)= scale * sum over the rows of sequence b whose code is V + k
+ * (what enters the hyper-encoder's own backward pass).  The rows of a target are added in fp32 in
+ * an order fixed by N and the codes: the same call gives the same bits.
+ *   d_codes, N, d_row_seq: as in the lookup; rows with Z2Z_CODE_NONE, and codes that name nothing
+ *            (Z2Z_ST_BAD_TOKEN), add nothing.  N <= 2^24.
+ *   d_grad_out [N, d] in the configured dtype;
+ *   grad_dtype  Z2Z_DTYPE_* of both gradient tables (fp32 for sums over micro batches);
+ *   accumulate  1: added to what the tables hold, rounded once; rows that no code names are neither
+ *            read nor written.  0: every row of d_grad_WE and the n_b rows of every sequence of
+ *            d_grad_Eh are written, zero where no code names them; rows from n_b on stay as they are.
+ *   d_grad_WE [V, d], d_grad_Eh [B, cap, d]: 16-byte aligned; either may be NULL (a frozen table):
+ *            its rows are then left out.
+ *   d_scratch: 256-byte aligned, at least z2z_embed_grad_scratch_bytes for the session's
+ *            configuration and N; its contents need not be kept between calls.  Calls that share it
+ *            must be ordered by the caller.                                                      */
+int32_t z2z_embed_grad_scratch_bytes(const z2z_config* cfg, int32_t N, size_t* out_bytes);
+int32_t z2z_embed_grad(z2z_codebook* cb, const int32_t* d_codes, int32_t N, const int32_t* d_row_seq,
+                       const void* d_grad_out, float scale, int32_t grad_dtype, int32_t accumulate,
+                       void* d_grad_WE, void* d_grad_Eh, void* d_scratch, size_t scratch_bytes,
+                       z2z_stream stream);
+
+/* Distillation on joint logits: a student's row against a teacher's K best columns.
+ * With l the row's logits, C its columns, q = softmax(l / T) over them and p = softmax(t / T) over the
+ * teacher's entries that the row can see:
+ *   loss_r = T^2 * sum_j p_j (log p_j - log q_{id_j}),
+ *   d loss_r / d l_c = T (q_c - sum of p_j over id_j = c).
+ *   d_logits [N, cols] of dtype (Z2Z_DTYPE_*), rows ld elements apart (as z2z_dynamic_logits stores
+ *            them: cols = ld = V + cap, fp32); aligned to their elements;
+ *   d_n_cols [N] columns of row r that exist (V + visible hypertokens; read as 0 .. cols), or NULL = all.
+ *            What lies behind them is not read.  Columns of -inf have no probability;
+ *   d_teacher_ids, d_teacher_logits [N, K]: the teacher's columns and its logits for them, in any
+ *            order, 0 <= K <= 1024.  An id outside the row's columns (Z2Z_CODE_NONE for shorter lists) is
+ *            left out, a logit of -inf has no probability, and what the same column is given twice adds up;
+ *   temperature > 0, finite;
+ *   d_loss [N] out, d_lse [N] out: log sum_c exp(l_c / T).
+ * A row without columns, or with nothing but -inf (lse = -inf), and a row that is left no teacher entry, has
+ * loss 0 and gradient 0.  A NaN or +inf logit makes the loss, lse and gradient of its row NaN.
+ * z2z_distill_loss also writes, when d_grad is not NULL, the gradient of sum_r w_r loss_r in the same pass over
+ * the logits: d_row_weight [N] = w, or NULL = 1 (d_loss stays unweighted; without d_grad it is not read).
+ * z2z_distill_grad is the backward pass on its own: d_lse is what z2z_distill_loss left there for the same
+ * arguments, d_grad_loss [N] the derivative for d_loss.
+ *   d_grad [N, cols] of dtype, rows ld apart: every column is written, 0 from n_cols on.  A row whose
+ *            weight is 0 has gradient 0 whatever its logits are.  d_grad == d_logits is allowed (the
+ *            logits are then overwritten); they must not overlap in another way.                   */
+int32_t z2z_distill_loss(const void* d_logits, int32_t dtype, int32_t N, int32_t cols, int64_t ld,
+                         const int32_t* d_n_cols, const int32_t* d_teacher_ids,
+                         const float* d_teacher_logits, int32_t K, float temperature,
+                         const float* d_row_weight, float* d_loss, float* d_lse, void* d_grad,
+                         z2z_stream stream);
+int32_t z2z_distill_grad(const void* d_logits, int32_t dtype, int32_t N, int32_t cols, int64_t ld,
+                         const int32_t* d_n_cols, const int32_t* d_teacher_ids,
+                         const float* d_teacher_logits, int32_t K, float temperature,
+                         const float* d_lse, const float* d_grad_loss, void* d_grad, z2z_stream stream);
+
+/* Beam search over the joint vocabularies (the paper decodes greedily or by sampling).  The beams of a request
+ * are `beams` consecutive sequences of the session, each with its own codebook and caches: group g is the
+ * sequences g * beams .. (g + 1) * beams - 1; B is a multiple of beams, 1 <= beams <= 32.
+ * z2z_beam_select picks the `beams` best continuations of every group.  A live beam b offers its columns c in
+ * [0, V + n_b) with s = score_b + (l_c - lse_b), computed in fp64; a finished one offers itself, unchanged.
+ * What has s = -inf or NaN is no candidate (a dead beam has score -inf).  Order: higher s, then lower
+ * sequence, then higher logit, then lower column.
+ * The winners are dealt to the group's slots so that the best continuation of a beam stays in its slot and the
+ * others, in order, take the slots of beams that have none: what z2z_beam_reorder then has to copy is never
+ * overwritten.  With fewer candidates than beams the slots that are left are dead.
+ *   d_logits [B, V + cap] fp32 and d_lse [B]: as z2z_dynamic_logits stores them for hidden row b of
+ *            sequence b (d_logits_debug, d_lse);
+ *   d_scores [B] sums of log-probabilities so far (a request's first step: 0 for one beam, -inf for the others);
+ *   d_finished [B] or NULL = none;  eos: base token that finishes a beam, or -1;
+ *   d_parent [B] out: the sequence whose continuation slot b holds (b itself in a dead slot);
+ *   d_code [B] out: its new code, Z2Z_CODE_NONE for a finished or dead one;
+ *   d_next_scores [B] out (-inf in a dead slot); d_next_finished [B] out or NULL (1 also for a dead slot);
+ *   d_active [B] out or NULL: 1 where d_code is a code (z2z_lzw_step's d_active).
+ * d_next_scores may be d_scores and d_next_finished may be d_finished; the outputs overlap nothing else.   */
+int32_t z2z_beam_select(z2z_codebook* cb, int32_t beams, const float* d_logits, const float* d_lse,
+                        const float* d_scores, const uint8_t* d_finished, int32_t eos, int32_t* d_parent,
+                        int32_t* d_code, float* d_next_scores, uint8_t* d_next_finished, uint8_t* d_active,
+                        z2z_stream stream);
+
+/* Sequence b takes over the state of sequence d_parent[b]: codebook, hash, counters, status, the parent's n rows
+ * of the caches, and the caller's own per-sequence rows.  d_parent[b] == b leaves it as it is.
+ * A parent must keep its own state (d_parent[d_parent[b]] == d_parent[b], as z2z_beam_select deals them), so that
+ * nothing is overwritten that is still to be read; otherwise sequence b is left as it is and
+ * Z2Z_ST_BAD_PARENT is set for it.  Cache rows from the parent's n on stay as they are.
+ *   d_Eh, d_Uh [B, cap, d]: may be NULL when cap is 0, and the same for tied tables;
+ *   d_Eh_f32, d_Uh_f32 [B, cap, d] or NULL: the optional fp32 copies, treated alike;
+ *   h_states: n_states (0 .. 8) HOST records of rows of the caller's own (token histories, block tables, ...):
+ *            sequence b's row is `bytes` bytes at d_base + b * stride; bytes, stride and d_base are multiples
+ *            of 4, stride >= bytes.
+ * All buffers are distinct from one another and from the workspace.                                     */
+typedef struct {
+  void* d_base;
+  size_t stride, bytes;
+} z2z_seq_rows;
+int32_t z2z_beam_reorder(z2z_codebook* cb, const int32_t* d_parent, void* d_Eh, void* d_Uh,
+                         float* d_Eh_f32, float* d_Uh_f32, const z2z_seq_rows* h_states,
+                         int32_t n_states, z2z_stream stream);
 
 /* Host -> device transfer of a small per-step input (the hidden rows of a decode step) by a kernel
  * instead of a copy-engine transfer (no counterpart in the paper; end-to-end latency aid).  The

@@ -7,7 +7,8 @@ this module.
 
 Pins: tests/test_oracle_lzw.py::test_lookup_* (a hypertoken's row under the parameter-free
 averaging encoder equals the mean of the looked-up rows of the base tokens the LZW oracle
-decompresses it to; a stream of base tokens alone reduces to numpy's row gather).
+decompresses it to; a stream of base tokens alone reduces to numpy's row gather), and
+tests/test_oracle_operators.py (the gradient is the adjoint of the scaled lookup).
 """
 from __future__ import annotations
 
@@ -36,3 +37,26 @@ def lookup(codes: Sequence[int], row_seq: Optional[Sequence[int]], W_E: np.ndarr
         elif z != -1:
             bad.append(b)
     return out, bad
+
+
+def lookup_scaled(codes, row_seq, W_E, E_h, n, scale: float):
+    """The lookup times a scale (models that multiply their input embeddings)."""
+    out, bad = lookup(codes, row_seq, W_E, E_h, n)
+    return out * float(scale), bad
+
+
+def lookup_grad(codes, row_seq, g: np.ndarray, V: int, cap: int, B: int, n: Sequence[int], scale: float):
+    """Gradient of sum(g * lookup_scaled) for both tables: (dW_E [V, d], dE_h [B, cap, d]), and, in the same shapes
+    without d, how many rows name a target and the sums of the magnitudes of what is added (for error bounds)."""
+    d = g.shape[1]
+    dW, dE = np.zeros((V, d)), np.zeros((B, cap, d))
+    aW, aE = np.zeros((V, d)), np.zeros((B, cap, d))
+    cW, cE = np.zeros(V, dtype=np.int64), np.zeros((B, cap), dtype=np.int64)
+    for r, z in enumerate(codes):
+        z, b = int(z), int(row_seq[r]) if row_seq is not None else r
+        x = g[r] * float(scale)
+        if 0 <= z < V:
+            dW[z] += x; aW[z] += np.abs(x); cW[z] += 1
+        elif V <= z < V + int(n[b]):
+            dE[b, z - V] += x; aE[b, z - V] += np.abs(x); cE[b, z - V] += 1
+    return dW, dE, cW, cE, aW, aE

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libz2z.so")
 
 OK = 0
 ST_CAP_FROZEN, ST_BAD_TOKEN, ST_TABLE_FULL, ST_WAIT_TIMEOUT, ST_OUTPUT_TRUNCATED, ST_HALF_RANGE = 1, 2, 4, 8, 16, 32
+ST_BAD_PARENT = 64
 DTYPE_FP32, DTYPE_BF16 = 0, 1
 SELECT_ARGMAX, SELECT_GUMBEL = 0, 1
 CODE_NONE, CODE_SELECTED = -1, -2
@@ -28,7 +29,8 @@ EXPORTS = ["z2z_workspace_bytes", "z2z_codebook_init", "z2z_lzw_encode", "z2z_lz
            "z2z_codebook_read", "z2z_codebook_destroy", "z2z_last_error", "z2z_profile",
            "z2z_profile_read", "z2z_set_tensor_cores", "z2z_logits_static_scratch",
            "z2z_lzw_decode", "z2z_embed_lookup", "z2z_upload_rows", "z2z_sample_filtered",
-           "z2z_set_encoder_half_scratch"]
+           "z2z_set_encoder_half_scratch", "z2z_embed_lookup_scaled", "z2z_embed_grad_scratch_bytes", "z2z_embed_grad",
+           "z2z_distill_loss", "z2z_distill_grad", "z2z_beam_select", "z2z_beam_reorder"]
 
 
 class Config(C.Structure):
@@ -38,6 +40,22 @@ class Config(C.Structure):
 
 class EncoderWeights(C.Structure):
     _fields_ = [("tensors", C.POINTER(C.c_void_p)), ("n_tensors", C.c_int32)]
+
+
+class SeqRows(C.Structure):
+    _fields_ = [("d_base", C.c_void_p), ("stride", C.c_size_t), ("bytes", C.c_size_t)]
+
+
+_P, _I, _F, _L = C.c_void_p, C.c_int32, C.c_float, C.c_int64
+# Argument types of the calls that are made with plain Python numbers (an address of 0 is None).
+_ARGTYPES = {
+    "z2z_embed_lookup_scaled": [_P, _P, _I, _P, _P, _P, _F, _P, _P],
+    "z2z_embed_grad": [_P, _P, _I, _P, _P, _F, _I, _I, _P, _P, _P, C.c_size_t, _P],
+    "z2z_distill_loss": [_P, _I, _I, _I, _L, _P, _P, _P, _I, _F, _P, _P, _P, _P, _P],
+    "z2z_distill_grad": [_P, _I, _I, _I, _L, _P, _P, _P, _I, _F, _P, _P, _P, _P],
+    "z2z_beam_select": [_P, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P],
+    "z2z_beam_reorder": [_P, _P, _P, _P, _P, _P, C.POINTER(SeqRows), _I, _P],
+}
 
 
 class Z2ZError(RuntimeError):
@@ -59,6 +77,8 @@ def lib() -> C.CDLL:
         for name in EXPORTS:
             if name != "z2z_last_error":
                 getattr(_lib, name).restype = C.c_int32
+        for name, types in _ARGTYPES.items():
+            getattr(_lib, name).argtypes = types
     return _lib
 
 
@@ -76,6 +96,31 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise Z2ZError(what)
+
+
+def _dev(t: Optional[torch.Tensor], dtype, numel: int, name: str):
+    """Address of a contiguous device tensor of this type and size, None for None."""
+    if t is None:
+        return None
+    _need(t.dtype == dtype and t.numel() == numel and t.is_cuda and t.is_contiguous(),
+          f"{name} must be a contiguous device tensor of {numel} {dtype}")
+    return t.data_ptr()
+
+
+def _enqueue(name: str, on: torch.Tensor, *args):
+    """The call on the current stream of the device that `on` lies on."""
+    _need(on.is_cuda, f"{name} needs device tensors")
+    fn, dev = getattr(lib(), name), on.get_device()
+    if dev == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, torch.cuda.current_stream().cuda_stream))
 
 
 def make_config(V, d, M, cap, B, dtype, enc_layers, enc_heads, enc_dff, tied=0) -> Config:
@@ -197,6 +242,110 @@ def z2z_embed_lookup(cb: Codebook, codes: torch.Tensor, row_seq: Optional[torch.
     """codes [N] int32 -> out [N, d]: W_E rows for base tokens, cached E_h rows for hypertokens."""
     _check(lib().z2z_embed_lookup(cb.handle, _ptr(codes), C.c_int32(codes.numel()), _ptr(row_seq),
                                   _ptr(W_E), _ptr(E_h), _ptr(out), _stream()))
+
+
+def _table_dtype(cb: Codebook):
+    return torch.bfloat16 if cb.cfg.dtype == DTYPE_BF16 else torch.float32
+
+
+def _cache(cb: Codebook, t: Optional[torch.Tensor], dtype, name: str):
+    """Address of a [B, cap, d] tensor; sessions without hypertokens have none."""
+    return _dev(t, dtype, cb.cfg.B * cb.cfg.cap * cb.cfg.d, name) if cb.cfg.cap > 0 else None
+
+
+def z2z_embed_lookup_scaled(cb: Codebook, codes: torch.Tensor, row_seq: Optional[torch.Tensor], W_E: torch.Tensor,
+                            E_h: Optional[torch.Tensor], scale: float, out: torch.Tensor):
+    """codes [N] int32 -> out [N, d] = scale * row: W_E rows for base tokens, cached E_h rows for hypertokens."""
+    c, N, dt = cb.cfg, codes.numel(), _table_dtype(cb)
+    _enqueue("z2z_embed_lookup_scaled", out, cb.handle, _dev(codes, torch.int32, N, "codes"), N,
+             _dev(row_seq, torch.int32, N, "row_seq"), _dev(W_E, dt, c.V * c.d, "W_E"), _cache(cb, E_h, dt, "E_h"),
+             scale, _dev(out, dt, N * c.d, "out"))
+
+
+def z2z_embed_grad_scratch_bytes(cfg: Config, N: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().z2z_embed_grad_scratch_bytes(C.byref(cfg), C.c_int32(N), C.byref(out)))
+    return out.value
+
+
+def z2z_embed_grad(cb: Codebook, codes: torch.Tensor, row_seq: Optional[torch.Tensor], grad_out: torch.Tensor, scale: float,
+                   accumulate: bool, grad_WE: Optional[torch.Tensor], grad_Eh: Optional[torch.Tensor], scratch: torch.Tensor):
+    """Gradient of z2z_embed_lookup_scaled for its tables (None: a frozen one), of the type the gradients have (fp32 or
+    bf16, both the same); scratch: uint8 tensor of z2z_embed_grad_scratch_bytes."""
+    c, N = cb.cfg, codes.numel()
+    some = grad_WE if grad_WE is not None else grad_Eh
+    _need(some is not None and some.dtype in (torch.float32, torch.bfloat16), "grad_WE or grad_Eh must be given, fp32 or bf16")
+    _enqueue("z2z_embed_grad", some, cb.handle, _dev(codes, torch.int32, N, "codes"), N, _dev(row_seq, torch.int32, N, "row_seq"),
+             _dev(grad_out, _table_dtype(cb), N * c.d, "grad_out"), scale,
+             DTYPE_FP32 if some.dtype == torch.float32 else DTYPE_BF16, 1 if accumulate else 0,
+             _dev(grad_WE, some.dtype, c.V * c.d, "grad_WE"), _cache(cb, grad_Eh, some.dtype, "grad_Eh"),
+             _dev(scratch, torch.uint8, scratch.numel(), "scratch"), scratch.numel())
+
+
+def _distill_args(logits: torch.Tensor, n_cols, teacher_ids, teacher_logits, temperature: float):
+    _need(logits.dim() == 2 and logits.is_cuda and logits.dtype in (torch.float32, torch.bfloat16)
+          and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits must be a device matrix with contiguous rows, fp32 or bf16")
+    N, cols = logits.shape
+    K = teacher_ids.shape[1] if teacher_ids is not None else 0
+    return N, (logits.data_ptr(), DTYPE_FP32 if logits.dtype == torch.float32 else DTYPE_BF16, N, cols,
+               logits.stride(0) if N > 1 else cols, _dev(n_cols, torch.int32, N, "n_cols"), _dev(teacher_ids, torch.int32, N * K, "teacher_ids"),
+               _dev(teacher_logits, torch.float32, N * K, "teacher_logits"), K, temperature)
+
+
+def _like(grad: Optional[torch.Tensor], logits: torch.Tensor):
+    if grad is None:
+        return None
+    _need(grad.dtype == logits.dtype and grad.is_cuda and grad.shape == logits.shape
+          and (grad.stride() == logits.stride() or grad.shape[0] == 1 and grad.is_contiguous()),
+          "grad must have the shape, type and strides of logits")
+    return grad.data_ptr()
+
+
+def z2z_distill_loss(logits: torch.Tensor, n_cols: Optional[torch.Tensor], teacher_ids: Optional[torch.Tensor],
+                     teacher_logits: Optional[torch.Tensor], temperature: float, row_weight: Optional[torch.Tensor],
+                     loss: torch.Tensor, lse: torch.Tensor, grad: Optional[torch.Tensor] = None):
+    """logits [N, cols] (rows may be strided), teacher_ids / teacher_logits [N, K] -> loss [N], lse [N] and, when given, the
+    gradient of sum(row_weight * loss) for the logits."""
+    N, args = _distill_args(logits, n_cols, teacher_ids, teacher_logits, temperature)
+    _enqueue("z2z_distill_loss", logits, *args, _dev(row_weight, torch.float32, N, "row_weight"),
+             _dev(loss, torch.float32, N, "loss"), _dev(lse, torch.float32, N, "lse"), _like(grad, logits))
+
+
+def z2z_distill_grad(logits: torch.Tensor, n_cols: Optional[torch.Tensor], teacher_ids: Optional[torch.Tensor],
+                     teacher_logits: Optional[torch.Tensor], temperature: float, lse: torch.Tensor, grad_loss: torch.Tensor,
+                     grad: torch.Tensor):
+    """Backward pass of z2z_distill_loss: lse as it left it, grad_loss [N] -> grad [N, cols]."""
+    N, args = _distill_args(logits, n_cols, teacher_ids, teacher_logits, temperature)
+    _enqueue("z2z_distill_grad", logits, *args, _dev(lse, torch.float32, N, "lse"), _dev(grad_loss, torch.float32, N, "grad_loss"),
+             _like(grad, logits))
+
+
+def z2z_beam_select(cb: Codebook, beams: int, logits: torch.Tensor, lse: torch.Tensor, scores: torch.Tensor,
+                    finished: Optional[torch.Tensor], eos: int, parent: torch.Tensor, code: torch.Tensor,
+                    next_scores: torch.Tensor, next_finished: Optional[torch.Tensor] = None, active: Optional[torch.Tensor] = None):
+    """Best continuations of every group of `beams` consecutive sequences, dealt to the group's slots (see z2z.h).
+    logits [B, V + cap] and lse [B] as z2z_dynamic_logits stores them; finished / next_finished / active are uint8."""
+    B = cb.cfg.B
+    _enqueue("z2z_beam_select", logits, cb.handle, beams, _dev(logits, torch.float32, B * (cb.cfg.V + cb.cfg.cap), "logits"),
+             _dev(lse, torch.float32, B, "lse"), _dev(scores, torch.float32, B, "scores"), _dev(finished, torch.uint8, B, "finished"), eos,
+             _dev(parent, torch.int32, B, "parent"), _dev(code, torch.int32, B, "code"), _dev(next_scores, torch.float32, B, "next_scores"),
+             _dev(next_finished, torch.uint8, B, "next_finished"), _dev(active, torch.uint8, B, "active"))
+
+
+def z2z_beam_reorder(cb: Codebook, parent: torch.Tensor, E_h: Optional[torch.Tensor], U_h: Optional[torch.Tensor],
+                     E_h_f32: Optional[torch.Tensor] = None, U_h_f32: Optional[torch.Tensor] = None, states=()):
+    """Sequence b takes over the codebook, caches and rows of sequence parent[b]; states: tensors [B, ...] of the caller's
+    own whose row b belongs to sequence b."""
+    c, dt = cb.cfg, _table_dtype(cb)
+    rows = (SeqRows * len(states))() if states else None
+    for r, t in zip(rows or (), states):
+        _need(t.is_cuda and t.dim() > 0 and t.shape[0] == c.B and t[0].is_contiguous(), "a state must be a device tensor [B, ...] with contiguous rows")
+        e = t.element_size()
+        r.d_base, r.bytes = t.data_ptr(), t.numel() // c.B * e
+        r.stride = t.stride(0) * e if c.B > 1 else r.bytes
+    _enqueue("z2z_beam_reorder", parent, cb.handle, _dev(parent, torch.int32, c.B, "parent"), _cache(cb, E_h, dt, "E_h"),
+             _cache(cb, U_h, dt, "U_h"), _cache(cb, E_h_f32, torch.float32, "E_h_f32"), _cache(cb, U_h_f32, torch.float32, "U_h_f32"),
+             rows, len(states))
 
 
 def z2z_sample_filtered(logits: torch.Tensor, n_cols: torch.Tensor, top_k: int, top_p: float, temperature: float,

@@ -1,5 +1,6 @@
 // extern "C" entry points declared in include/z2z.h: argument checks, workspace views, and the
 // order in which the kernels of each call are enqueued.  No arithmetic of the method lives here.
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -44,6 +45,8 @@ int fail_cuda(cudaError_t e, const char* where) {
     cudaError_t e__ = (call);                                  \
     if (e__ != cudaSuccess) return fail_cuda(e__, where);      \
   } while (0)
+
+bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 int check_config(const z2z_config* c) {
   if (!c) return fail(Z2Z_ERR_INVALID_ARG, "config is NULL");
@@ -305,6 +308,105 @@ int32_t z2z_embed_lookup(z2z_codebook* cb, const int32_t* d_codes, int32_t N,
   const int eb = cb->cfg.dtype == Z2Z_DTYPE_BF16 ? 2 : 4;
   Z2Z_CUDA(z2z::launch_embed_lookup(cb->view, d_codes, N, d_row_seq, d_WE, d_Eh, d_out, cb->cfg.d, eb,
                                     reinterpret_cast<cudaStream_t>(stream)), "embed_lookup");
+  return Z2Z_OK;
+}
+
+int32_t z2z_embed_lookup_scaled(z2z_codebook* cb, const int32_t* d_codes, int32_t N,
+                                const int32_t* d_row_seq, const void* d_WE, const void* d_Eh,
+                                float scale, void* d_out, z2z_stream stream) {
+  if (!cb) return fail(Z2Z_ERR_INVALID_ARG, "cb is NULL");
+  if (N < 0) return fail(Z2Z_ERR_INVALID_ARG, "N < 0");
+  if (!std::isfinite(scale)) return fail(Z2Z_ERR_INVALID_ARG, "scale is not finite");
+  if (N == 0) return Z2Z_OK;
+  if (!d_codes || !d_WE || !d_out) return fail(Z2Z_ERR_INVALID_ARG, "d_codes / d_WE / d_out is NULL");
+  if (!d_Eh && cb->cfg.cap > 0) return fail(Z2Z_ERR_INVALID_ARG, "d_Eh is NULL");
+  if (misaligned(d_WE, 16) || misaligned(d_Eh, 16) || misaligned(d_out, 16)) return fail(Z2Z_ERR_INVALID_ARG, "tables and rows must be 16-byte aligned");
+  if (!d_row_seq && N > cb->cfg.B) return fail(Z2Z_ERR_INVALID_ARG, "d_row_seq is required when N > B");
+  Z2Z_CUDA(z2z::launch_embed_lookup_scaled(cb->view, d_codes, N, d_row_seq, d_WE, d_Eh, scale, d_out, cb->cfg.d, cb->cfg.dtype,
+                                           reinterpret_cast<cudaStream_t>(stream)), "embed_lookup_scaled");
+  return Z2Z_OK;
+}
+
+int32_t z2z_embed_grad_scratch_bytes(const z2z_config* cfg, int32_t N, size_t* out_bytes) {
+  int rc = check_config(cfg);
+  if (rc) return rc;
+  if (N < 0 || N > z2z::kEmbedGradMaxRows) return fail(Z2Z_ERR_INVALID_ARG, "need 0 <= N <= 2^24");
+  if (!out_bytes) return fail(Z2Z_ERR_INVALID_ARG, "out_bytes is NULL");
+  *out_bytes = z2z::embed_grad_scratch_bytes(N, cfg->d);
+  return Z2Z_OK;
+}
+
+int32_t z2z_embed_grad(z2z_codebook* cb, const int32_t* d_codes, int32_t N, const int32_t* d_row_seq,
+                       const void* d_grad_out, float scale, int32_t grad_dtype, int32_t accumulate,
+                       void* d_grad_WE, void* d_grad_Eh, void* d_scratch, size_t scratch_bytes,
+                       z2z_stream stream) {
+  if (!cb) return fail(Z2Z_ERR_INVALID_ARG, "cb is NULL");
+  if (N < 0 || N > z2z::kEmbedGradMaxRows) return fail(Z2Z_ERR_INVALID_ARG, "need 0 <= N <= 2^24");
+  if (!std::isfinite(scale)) return fail(Z2Z_ERR_INVALID_ARG, "scale is not finite");
+  if (grad_dtype != Z2Z_DTYPE_FP32 && grad_dtype != Z2Z_DTYPE_BF16) return fail(Z2Z_ERR_INVALID_ARG, "unknown grad_dtype");
+  if (accumulate != 0 && accumulate != 1) return fail(Z2Z_ERR_INVALID_ARG, "accumulate must be 0 or 1");
+  if (!d_grad_WE && !d_grad_Eh) return fail(Z2Z_ERR_INVALID_ARG, "d_grad_WE and d_grad_Eh are both NULL");
+  if (N > 0 && (!d_codes || !d_grad_out)) return fail(Z2Z_ERR_INVALID_ARG, "d_codes / d_grad_out is NULL");
+  if (misaligned(d_grad_WE, 16) || misaligned(d_grad_Eh, 16) || misaligned(d_grad_out, 16)) return fail(Z2Z_ERR_INVALID_ARG, "gradients must be 16-byte aligned");
+  if (!d_row_seq && N > cb->cfg.B) return fail(Z2Z_ERR_INVALID_ARG, "d_row_seq is required when N > B");
+  const size_t need = z2z::embed_grad_scratch_bytes(N, cb->cfg.d);
+  if (need > 0 && (!d_scratch || misaligned(d_scratch, 256))) return fail(Z2Z_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
+  if (scratch_bytes < need) return fail(Z2Z_ERR_WORKSPACE_TOO_SMALL, "scratch smaller than z2z_embed_grad_scratch_bytes");
+  z2z::EmbedGradArgs a{};
+  a.codes = d_codes; a.N = N; a.row_seq = d_row_seq; a.g = d_grad_out; a.g_dtype = cb->cfg.dtype; a.d = cb->cfg.d; a.scale = scale;
+  a.grad_dtype = grad_dtype; a.accumulate = accumulate != 0;
+  a.gWE = d_grad_WE; a.gEh = cb->cfg.cap > 0 ? d_grad_Eh : nullptr;
+  a.scratch = reinterpret_cast<char*>(d_scratch);
+  Z2Z_CUDA(z2z::launch_embed_grad(cb->view, a, reinterpret_cast<cudaStream_t>(stream)), "embed_grad");
+  return Z2Z_OK;
+}
+
+int32_t z2z_beam_select(z2z_codebook* cb, int32_t beams, const float* d_logits, const float* d_lse,
+                        const float* d_scores, const uint8_t* d_finished, int32_t eos, int32_t* d_parent,
+                        int32_t* d_code, float* d_next_scores, uint8_t* d_next_finished, uint8_t* d_active,
+                        z2z_stream stream) {
+  if (!cb) return fail(Z2Z_ERR_INVALID_ARG, "cb is NULL");
+  if (beams < 1 || beams > z2z::kMaxBeams) return fail(Z2Z_ERR_INVALID_ARG, "need 1 <= beams <= 32");
+  if (cb->cfg.B % beams != 0) return fail(Z2Z_ERR_INVALID_ARG, "B must be a multiple of beams");
+  if (eos < -1 || eos >= cb->cfg.V) return fail(Z2Z_ERR_INVALID_ARG, "eos must be a base token or -1");
+  if (!d_logits || !d_lse || !d_scores || !d_parent || !d_code || !d_next_scores) return fail(Z2Z_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (misaligned(d_logits, 4) || misaligned(d_lse, 4) || misaligned(d_scores, 4) || misaligned(d_next_scores, 4) || misaligned(d_parent, 4) || misaligned(d_code, 4))
+    return fail(Z2Z_ERR_INVALID_ARG, "arrays must be aligned to their elements");
+  z2z::BeamSelectArgs a{};
+  a.beams = beams; a.logits = d_logits; a.lse = d_lse; a.scores = d_scores; a.finished = d_finished; a.eos = eos;
+  a.parent = d_parent; a.code = d_code; a.next_scores = d_next_scores; a.next_finished = d_next_finished; a.active = d_active;
+  a.lists = cb->ws + cb->plan.off_lpart; a.lists_bytes = cb->plan.lpart_bytes;
+  Z2Z_CUDA(z2z::launch_beam_select(cb->view, a, reinterpret_cast<cudaStream_t>(stream)), "beam_select");
+  return Z2Z_OK;
+}
+
+int32_t z2z_beam_reorder(z2z_codebook* cb, const int32_t* d_parent, void* d_Eh, void* d_Uh,
+                         float* d_Eh_f32, float* d_Uh_f32, const z2z_seq_rows* h_states,
+                         int32_t n_states, z2z_stream stream) {
+  if (!cb) return fail(Z2Z_ERR_INVALID_ARG, "cb is NULL");
+  if (!d_parent) return fail(Z2Z_ERR_INVALID_ARG, "d_parent is NULL");
+  if (cb->cfg.cap > 0 && (!d_Eh || !d_Uh)) return fail(Z2Z_ERR_INVALID_ARG, "d_Eh / d_Uh is NULL");
+  if (n_states < 0 || n_states > z2z::kMaxSeqRows) return fail(Z2Z_ERR_INVALID_ARG, "need 0 <= n_states <= 8");
+  if (n_states > 0 && !h_states) return fail(Z2Z_ERR_INVALID_ARG, "h_states is NULL");
+  z2z::BeamReorderArgs a{};
+  a.parent = d_parent;
+  const int es = cb->cfg.dtype == Z2Z_DTYPE_BF16 ? 2 : 4;
+  void* const caches[4] = {d_Eh, d_Uh == d_Eh ? nullptr : d_Uh, d_Eh_f32, d_Uh_f32 == d_Eh_f32 ? nullptr : d_Uh_f32};
+  for (int i = 0; i < 4 && cb->cfg.cap > 0; ++i) {
+    if (!caches[i]) continue;
+    if (misaligned(caches[i], 16)) return fail(Z2Z_ERR_INVALID_ARG, "caches must be 16-byte aligned");
+    a.cache[a.n_caches] = reinterpret_cast<char*>(caches[i]);
+    a.cache_row_bytes[a.n_caches++] = cb->cfg.d * (i < 2 ? es : 4);
+  }
+  for (int i = 0; i < n_states; ++i) {
+    const z2z_seq_rows& r = h_states[i];
+    if (r.bytes == 0) continue;
+    if (!r.d_base) return fail(Z2Z_ERR_INVALID_ARG, "d_base of a state is NULL");
+    if (misaligned(r.d_base, 4) || r.bytes % 4 || r.stride % 4) return fail(Z2Z_ERR_INVALID_ARG, "d_base, stride and bytes of a state must be multiples of 4");
+    if (r.stride < r.bytes) return fail(Z2Z_ERR_INVALID_ARG, "stride of a state is smaller than its bytes");
+    a.rows[a.n_rows] = reinterpret_cast<char*>(r.d_base); a.stride[a.n_rows] = r.stride; a.bytes[a.n_rows++] = r.bytes;
+  }
+  Z2Z_CUDA(z2z::launch_beam_reorder(cb->view, a, reinterpret_cast<cudaStream_t>(stream)), "beam_reorder");
   return Z2Z_OK;
 }
 

@@ -49,6 +49,45 @@ __global__ void __launch_bounds__(kLookupThreads) k_embed_lookup(
   }
 }
 
+namespace {
+// 16 bytes of a row times a scale: the product in fp32, one rounding to the storage type.
+template <typename T> __device__ __forceinline__ uint4 scaled(uint4 v, float a);
+template <> __device__ __forceinline__ uint4 scaled<float>(uint4 v, float a) {
+  return make_uint4(__float_as_uint(__uint_as_float(v.x) * a), __float_as_uint(__uint_as_float(v.y) * a),
+                    __float_as_uint(__uint_as_float(v.z) * a), __float_as_uint(__uint_as_float(v.w) * a));
+}
+__device__ __forceinline__ uint32_t scaled_pair(uint32_t v, float a) {
+  const __nv_bfloat162 r = __floats2bfloat162_rn(__uint_as_float(v << 16) * a, __uint_as_float(v & 0xffff0000u) * a);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+template <> __device__ __forceinline__ uint4 scaled<__nv_bfloat16>(uint4 v, float a) {
+  return make_uint4(scaled_pair(v.x, a), scaled_pair(v.y, a), scaled_pair(v.z, a), scaled_pair(v.w, a));
+}
+}  // namespace
+
+// out[r] = scale * row(codes[r]).
+template <typename T>
+__global__ void __launch_bounds__(kLookupThreads) k_embed_lookup_scaled(
+    CbView cb, const int32_t* codes, int N, const int32_t* row_seq, const uint4* WE, const uint4* Eh, float scale, uint4* out,
+    int row_vecs) {
+  sm100::pdl_wait();
+  sm100::pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const int warps = (gridDim.x * blockDim.x) >> 5;
+  for (int r = (blockIdx.x * blockDim.x + threadIdx.x) >> 5; r < N; r += warps) {
+    const int z = codes[r];
+    const int b = row_seq ? row_seq[r] : r;
+    const uint4* src = nullptr;
+    if ((unsigned)b < (unsigned)cb.B) {
+      if (z >= 0 && z < cb.V) src = WE + (size_t)z * row_vecs;
+      else if (z >= cb.V && z - cb.V < cb.n[b]) src = Eh + ((size_t)b * cb.cap + (z - cb.V)) * row_vecs;
+      else if (lane == 0 && z != Z2Z_CODE_NONE) atomicOr(&cb.status[b], Z2Z_ST_BAD_TOKEN);
+    }
+    uint4* dst = out + (size_t)r * row_vecs;
+    for (int i = lane; i < row_vecs; i += 32) dst[i] = src ? scaled<T>(src[i], scale) : make_uint4(0, 0, 0, 0);
+  }
+}
+
 cudaError_t launch_embed_lookup(const CbView& cb, const int32_t* codes, int N,
                                 const int32_t* row_seq, const void* WE, const void* Eh, void* out,
                                 int d, int elem_bytes, cudaStream_t s) {
@@ -59,6 +98,18 @@ cudaError_t launch_embed_lookup(const CbView& cb, const int32_t* codes, int N,
   if (blocks > full) blocks = full;
   return launch_pdl(k_embed_lookup, dim3(blocks), dim3(kLookupThreads), 0, s, cb, codes, N, row_seq,
                     reinterpret_cast<const uint4*>(WE), reinterpret_cast<const uint4*>(Eh), reinterpret_cast<uint4*>(out), row_vecs);
+}
+
+cudaError_t launch_embed_lookup_scaled(const CbView& cb, const int32_t* codes, int N, const int32_t* row_seq, const void* WE,
+                                       const void* Eh, float scale, void* out, int d, int dtype, cudaStream_t s) {
+  const int row_vecs = d * (dtype == Z2Z_DTYPE_BF16 ? 2 : 4) / 16;
+  const int warps_per_block = kLookupThreads / 32;
+  int blocks = (N + warps_per_block - 1) / warps_per_block;
+  const int full = 148 * 8;
+  if (blocks > full) blocks = full;
+  auto kern = dtype == Z2Z_DTYPE_BF16 ? k_embed_lookup_scaled<__nv_bfloat16> : k_embed_lookup_scaled<float>;
+  return launch_pdl(kern, dim3(blocks), dim3(kLookupThreads), 0, s, cb, codes, N, row_seq,
+                    reinterpret_cast<const uint4*>(WE), reinterpret_cast<const uint4*>(Eh), scale, reinterpret_cast<uint4*>(out), row_vecs);
 }
 
 }  // namespace z2z

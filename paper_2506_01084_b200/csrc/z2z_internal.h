@@ -45,6 +45,44 @@ cudaError_t launch_embed_lookup(const CbView& cb, const int32_t* codes, int N,
 cudaError_t launch_lzw_step(const CbView& cb, const int32_t* new_codes, const uint8_t* active,
                             int none_sits_out, int32_t* new_entry, cudaStream_t s);
 
+cudaError_t launch_embed_lookup_scaled(const CbView& cb, const int32_t* codes, int N, const int32_t* row_seq, const void* WE,
+                                       const void* Eh, float scale, void* out, int d, int dtype, cudaStream_t s);
+
+// ---- z2z_embed_grad.cu -----------------------------------------------------------------------
+constexpr int kEmbedGradMaxRows = 1 << 24;
+struct EmbedGradArgs {
+  const int32_t* codes; int N;
+  const int32_t* row_seq;       // [N] or NULL
+  const void* g;                // [N, d] of g_dtype
+  int g_dtype, d;
+  float scale;
+  int grad_dtype; bool accumulate;
+  void *gWE, *gEh;              // [V, d], [B, cap, d]; NULL: left out
+  char* scratch;
+};
+size_t embed_grad_scratch_bytes(int N, int d);
+cudaError_t launch_embed_grad(const CbView& cb, const EmbedGradArgs& a, cudaStream_t s);
+
+// ---- z2z_beam.cu -----------------------------------------------------------------------------
+constexpr int kMaxBeams = 32;
+struct BeamSelectArgs {
+  int beams;
+  const float* logits;          // [B, V + cap]
+  const float* lse; const float* scores; const uint8_t* finished;
+  int eos;
+  int32_t* parent; int32_t* code; float* next_scores; uint8_t* next_finished; uint8_t* active;
+  char* lists;                  // scratch: each beam's best columns
+  size_t lists_bytes;
+};
+cudaError_t launch_beam_select(const CbView& cb, const BeamSelectArgs& a, cudaStream_t s);
+constexpr int kMaxSeqRows = 8;
+struct BeamReorderArgs {
+  const int32_t* parent;
+  char* cache[4]; int cache_row_bytes[4]; int n_caches;        // [B, cap] rows
+  char* rows[kMaxSeqRows]; size_t stride[kMaxSeqRows], bytes[kMaxSeqRows]; int n_rows;
+};
+cudaError_t launch_beam_reorder(const CbView& cb, const BeamReorderArgs& a, cudaStream_t s);
+
 // ---- z2z_encoder.cu --------------------------------------------------------------------------
 // Work list of one encoder pass: up to `list` entries of together at most chunk * M rows, entry e ->
 // (sequence, entry number).
