@@ -107,20 +107,23 @@ def _dev(t: Optional[torch.Tensor], dtype, numel: int, name: str):
     """Address of a contiguous device tensor of this type and size, None for None."""
     if t is None:
         return None
-    _need(t.dtype == dtype and t.numel() == numel and t.is_cuda and t.is_contiguous(),
-          f"{name} must be a contiguous device tensor of {numel} {dtype}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.numel() == numel and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise Z2ZError(f"{name} must be a contiguous device tensor of {numel} {dtype}")
 
 
-def _enqueue(name: str, on: torch.Tensor, *args):
+def _enqueue(fn, on: torch.Tensor, *args):
     """The call on the current stream of the device that `on` lies on."""
-    _need(on.is_cuda, f"{name} needs device tensors")
-    fn, dev = getattr(lib(), name), on.get_device()
+    dev = on.get_device()
     if dev == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+        rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    elif dev < 0:
+        raise Z2ZError("device tensors are needed")
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+            rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if rc:
+        _check(rc)
 
 
 def make_config(V, d, M, cap, B, dtype, enc_layers, enc_heads, enc_dff, tied=0) -> Config:
@@ -257,7 +260,7 @@ def z2z_embed_lookup_scaled(cb: Codebook, codes: torch.Tensor, row_seq: Optional
                             E_h: Optional[torch.Tensor], scale: float, out: torch.Tensor):
     """codes [N] int32 -> out [N, d] = scale * row: W_E rows for base tokens, cached E_h rows for hypertokens."""
     c, N, dt = cb.cfg, codes.numel(), _table_dtype(cb)
-    _enqueue("z2z_embed_lookup_scaled", out, cb.handle, _dev(codes, torch.int32, N, "codes"), N,
+    _enqueue(lib().z2z_embed_lookup_scaled, out, cb.handle, _dev(codes, torch.int32, N, "codes"), N,
              _dev(row_seq, torch.int32, N, "row_seq"), _dev(W_E, dt, c.V * c.d, "W_E"), _cache(cb, E_h, dt, "E_h"),
              scale, _dev(out, dt, N * c.d, "out"))
 
@@ -275,7 +278,7 @@ def z2z_embed_grad(cb: Codebook, codes: torch.Tensor, row_seq: Optional[torch.Te
     c, N = cb.cfg, codes.numel()
     some = grad_WE if grad_WE is not None else grad_Eh
     _need(some is not None and some.dtype in (torch.float32, torch.bfloat16), "grad_WE or grad_Eh must be given, fp32 or bf16")
-    _enqueue("z2z_embed_grad", some, cb.handle, _dev(codes, torch.int32, N, "codes"), N, _dev(row_seq, torch.int32, N, "row_seq"),
+    _enqueue(lib().z2z_embed_grad, some, cb.handle, _dev(codes, torch.int32, N, "codes"), N, _dev(row_seq, torch.int32, N, "row_seq"),
              _dev(grad_out, _table_dtype(cb), N * c.d, "grad_out"), scale,
              DTYPE_FP32 if some.dtype == torch.float32 else DTYPE_BF16, 1 if accumulate else 0,
              _dev(grad_WE, some.dtype, c.V * c.d, "grad_WE"), _cache(cb, grad_Eh, some.dtype, "grad_Eh"),
@@ -307,7 +310,7 @@ def z2z_distill_loss(logits: torch.Tensor, n_cols: Optional[torch.Tensor], teach
     """logits [N, cols] (rows may be strided), teacher_ids / teacher_logits [N, K] -> loss [N], lse [N] and, when given, the
     gradient of sum(row_weight * loss) for the logits."""
     N, args = _distill_args(logits, n_cols, teacher_ids, teacher_logits, temperature)
-    _enqueue("z2z_distill_loss", logits, *args, _dev(row_weight, torch.float32, N, "row_weight"),
+    _enqueue(lib().z2z_distill_loss, logits, *args, _dev(row_weight, torch.float32, N, "row_weight"),
              _dev(loss, torch.float32, N, "loss"), _dev(lse, torch.float32, N, "lse"), _like(grad, logits))
 
 
@@ -316,7 +319,7 @@ def z2z_distill_grad(logits: torch.Tensor, n_cols: Optional[torch.Tensor], teach
                      grad: torch.Tensor):
     """Backward pass of z2z_distill_loss: lse as it left it, grad_loss [N] -> grad [N, cols]."""
     N, args = _distill_args(logits, n_cols, teacher_ids, teacher_logits, temperature)
-    _enqueue("z2z_distill_grad", logits, *args, _dev(lse, torch.float32, N, "lse"), _dev(grad_loss, torch.float32, N, "grad_loss"),
+    _enqueue(lib().z2z_distill_grad, logits, *args, _dev(lse, torch.float32, N, "lse"), _dev(grad_loss, torch.float32, N, "grad_loss"),
              _like(grad, logits))
 
 
@@ -326,7 +329,7 @@ def z2z_beam_select(cb: Codebook, beams: int, logits: torch.Tensor, lse: torch.T
     """Best continuations of every group of `beams` consecutive sequences, dealt to the group's slots (see z2z.h).
     logits [B, V + cap] and lse [B] as z2z_dynamic_logits stores them; finished / next_finished / active are uint8."""
     B = cb.cfg.B
-    _enqueue("z2z_beam_select", logits, cb.handle, beams, _dev(logits, torch.float32, B * (cb.cfg.V + cb.cfg.cap), "logits"),
+    _enqueue(lib().z2z_beam_select, logits, cb.handle, beams, _dev(logits, torch.float32, B * (cb.cfg.V + cb.cfg.cap), "logits"),
              _dev(lse, torch.float32, B, "lse"), _dev(scores, torch.float32, B, "scores"), _dev(finished, torch.uint8, B, "finished"), eos,
              _dev(parent, torch.int32, B, "parent"), _dev(code, torch.int32, B, "code"), _dev(next_scores, torch.float32, B, "next_scores"),
              _dev(next_finished, torch.uint8, B, "next_finished"), _dev(active, torch.uint8, B, "active"))
@@ -343,7 +346,7 @@ def z2z_beam_reorder(cb: Codebook, parent: torch.Tensor, E_h: Optional[torch.Ten
         e = t.element_size()
         r.d_base, r.bytes = t.data_ptr(), t.numel() // c.B * e
         r.stride = t.stride(0) * e if c.B > 1 else r.bytes
-    _enqueue("z2z_beam_reorder", parent, cb.handle, _dev(parent, torch.int32, c.B, "parent"), _cache(cb, E_h, dt, "E_h"),
+    _enqueue(lib().z2z_beam_reorder, parent, cb.handle, _dev(parent, torch.int32, c.B, "parent"), _cache(cb, E_h, dt, "E_h"),
              _cache(cb, U_h, dt, "U_h"), _cache(cb, E_h_f32, torch.float32, "E_h_f32"), _cache(cb, U_h_f32, torch.float32, "U_h_f32"),
              rows, len(states))
 

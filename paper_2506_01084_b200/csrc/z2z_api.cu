@@ -332,7 +332,7 @@ int32_t z2z_embed_grad_scratch_bytes(const z2z_config* cfg, int32_t N, size_t* o
   if (rc) return rc;
   if (N < 0 || N > z2z::kEmbedGradMaxRows) return fail(Z2Z_ERR_INVALID_ARG, "need 0 <= N <= 2^24");
   if (!out_bytes) return fail(Z2Z_ERR_INVALID_ARG, "out_bytes is NULL");
-  *out_bytes = z2z::embed_grad_scratch_bytes(N, cfg->d);
+  *out_bytes = z2z::embed_grad_scratch_bytes(*cfg, N);
   return Z2Z_OK;
 }
 
@@ -349,7 +349,7 @@ int32_t z2z_embed_grad(z2z_codebook* cb, const int32_t* d_codes, int32_t N, cons
   if (N > 0 && (!d_codes || !d_grad_out)) return fail(Z2Z_ERR_INVALID_ARG, "d_codes / d_grad_out is NULL");
   if (misaligned(d_grad_WE, 16) || misaligned(d_grad_Eh, 16) || misaligned(d_grad_out, 16)) return fail(Z2Z_ERR_INVALID_ARG, "gradients must be 16-byte aligned");
   if (!d_row_seq && N > cb->cfg.B) return fail(Z2Z_ERR_INVALID_ARG, "d_row_seq is required when N > B");
-  const size_t need = z2z::embed_grad_scratch_bytes(N, cb->cfg.d);
+  const size_t need = z2z::embed_grad_scratch_bytes(cb->cfg, N);
   if (need > 0 && (!d_scratch || misaligned(d_scratch, 256))) return fail(Z2Z_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
   if (scratch_bytes < need) return fail(Z2Z_ERR_WORKSPACE_TOO_SMALL, "scratch smaller than z2z_embed_grad_scratch_bytes");
   z2z::EmbedGradArgs a{};

@@ -60,7 +60,7 @@ struct EmbedGradArgs {
   void *gWE, *gEh;              // [V, d], [B, cap, d]; NULL: left out
   char* scratch;
 };
-size_t embed_grad_scratch_bytes(int N, int d);
+size_t embed_grad_scratch_bytes(const z2z_config& c, int N);
 cudaError_t launch_embed_grad(const CbView& cb, const EmbedGradArgs& a, cudaStream_t s);
 
 // ---- z2z_beam.cu -----------------------------------------------------------------------------
