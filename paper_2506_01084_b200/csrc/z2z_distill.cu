@@ -1,7 +1,24 @@
 // Distillation of joint logits from a teacher's top logits.  With l the row's logits over its C columns,
 // q = softmax(l / T), and p = softmax(t / T) over the teacher's entries that the row can see:
 //   loss = T^2 sum_j p_j (log p_j - log q_{id_j}),     d loss / d l_c = T (q_c - sum_{id_j = c} p_j).
+//
+// One kernel, a cluster of 1 to 8 blocks per row.  Every block reads its share of the columns once and folds it into a
+// running maximum and sum of exponentials; every warp sends its pair to the shared memory of all blocks; one cluster
+// barrier.  When the gradient is asked for, the share stays in shared memory until then (a thread only ever reads back
+// what it has brought itself, so that its own copies' completion is all it waits for): the logits are read once and the
+// gradient written once.  Rows longer than eight blocks hold (some 440000 fp32 columns) are read again.  The backward
+// pass on its own is the same with the normaliser found anew: that is no byte more, and does not depend on what a stored
+// lse has lost (2^-24 of |lse|, in every probability).
+// Bound by HBM, for bf16 rows with little left: 2 exponentials a column, at 16 per clock and SM, take 0.7 of the bytes'
+// time.  Hence the packed maxima, one update of the maximum per kFold vectors, and the factor of a bf16 gradient in
+// the exponent.
+// Exponents are kept base 2: z = c x - r with c = log2(e) / T, one fused operation, and r the rounded product of c with
+// the maximum.  What r's rounding does to the terms it does to their sum, so that it drops out of q; it stays in lse, at
+// one rounding of m / T.
+#include <cooperative_groups.h>
+
 #include <cmath>
+#include <type_traits>
 
 #include "z2z_common.cuh"
 #include "z2z_internal.h"
@@ -12,131 +29,369 @@ namespace z2z {
 namespace {
 
 constexpr int kDistillMaxK = 1024;
-constexpr int kDistillThreads = 512;
+constexpr int kDistillThreads = 256;     // of a block, at most
+constexpr int kFold = 4;                 // vectors of 16 bytes that a thread folds at once, and waits for at once
+constexpr size_t kShareBytes = 72 << 10;              // of a row per block, for three blocks per SM
+constexpr size_t kShareMax = 208 << 10;               // ... and at most, for one
 
 struct DistillArgs {
   const void* logits; int cols; long long ld;
   const int32_t* n_cols; const int32_t* ids; const float* t; int K;
-  float inv_t, temperature;
+  float inv_t, temperature, c;  // c = log2(e) / T
   const float* weight;          // row weights (gradient), or NULL = 1
-  float* loss; float* lse;      // out; the backward pass reads lse
+  float* loss; float* lse;      // out, or NULL
   void* grad;                   // or NULL
+  int grad_skew;                // the gradient's rows are not aligned to 16 bytes where the logits' are
 };
 
-struct Teacher { int id[kDistillMaxK]; float p[kDistillMaxK]; float red[32]; };
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float kLn2 = 0.693147180559945f, kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ float block_max(float v, float* red) {
+template <typename T> constexpr int kPer = 16 / (int)sizeof(T);          // columns of 16 bytes
+template <typename T> __device__ __forceinline__ void unpack(const uint4& v, float (&x)[kPer<T>]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = threadIdx.x % 32 < blockDim.x / 32 ? red[threadIdx.x & 31] : -INFINITY;
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 4) x[i % kPer<T>] = __uint_as_float(w[i]);
+    else { x[(2 * i) % kPer<T>] = __uint_as_float(w[i] << 16); x[(2 * i + 1) % kPer<T>] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+}
+template <typename T> __device__ __forceinline__ uint4 packed(const float (&x)[kPer<T>]) {
+  uint32_t w[4];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 4) w[i] = __float_as_uint(x[i % kPer<T>]);
+    else {
+      const __nv_bfloat162 r = __floats2bfloat162_rn(x[(2 * i) % kPer<T>], x[(2 * i + 1) % kPer<T>]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&r);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A row's columns as 16-byte vectors: `head` columns in front of the first 16-byte boundary, `vecs` vectors, `tail` columns.
+struct RowSplit { int head, vecs, tail; };
+template <typename T> __device__ __forceinline__ RowSplit split_row(const T* row, int cols) {
+  const int off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+  RowSplit s;
+  s.head = off ? min(cols, kPer<T> - off) : 0;
+  s.vecs = (cols - s.head) / kPer<T>;
+  s.tail = cols - s.head - s.vecs * kPer<T>;
+  return s;
+}
+
+// Maximum of the columns of some vectors (NaN does not count).
+template <typename T, int n> __device__ __forceinline__ float max_of(const uint4 (&v)[n]);
+template <> __device__ __forceinline__ float max_of<float, kFold>(const uint4 (&v)[kFold]) {
+  float t = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < kFold; ++u)
+    t = fmaxf(t, fmaxf(fmaxf(__uint_as_float(v[u].x), __uint_as_float(v[u].y)), fmaxf(__uint_as_float(v[u].z), __uint_as_float(v[u].w))));
+  return t;
+}
+template <> __device__ __forceinline__ float max_of<__nv_bfloat16, kFold>(const uint4 (&v)[kFold]) {
+  auto two = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+  __nv_bfloat162 t = two(v[0].x);
+#pragma unroll
+  for (int u = 0; u < kFold; ++u)
+    t = __hmax2(t, __hmax2(__hmax2(two(v[u].x), two(v[u].y)), __hmax2(two(v[u].z), two(v[u].w))));
+  return fmaxf(__low2float(t), __high2float(t));
+}
+
+// Running maximum m and s = sum of 2^(c x - c m).  What is at or below kMasked (the lowest value of either type, -inf),
+// or has a product with c beyond the type's range, adds nothing; NaN and +inf make s NaN.  As long as there is nothing
+// visible m is kMasked and s 0, or NaN.
+constexpr float kMasked = -8.507059173023462e37f;          // -2^126
+__device__ __forceinline__ float ref_of(float m, float c) { return m > kMasked ? c * m : -INFINITY; }
+struct Fold {
+  float m = kMasked, r = -INFINITY, s = 0.f;               // r = ref_of(m, c)
+  __device__ __forceinline__ void raise(float top, float c) {
+    if (top > m && c * top > -INFINITY) {
+      const float r2 = c * top;
+      if (r > -INFINITY) s *= ex2(r - r2);
+      m = top; r = r2;
+    }
+  }
+  // (behind raise: no x is above m)
+  template <int n> __device__ __forceinline__ void add(const float (&x)[n], float c) {
+    if (r == -INFINITY) {
+#pragma unroll
+      for (int i = 0; i < n; ++i) s += x[i] == x[i] ? 0.f : x[i];
+      return;
+    }
+    float a = 0.f, b = 0.f;
+#pragma unroll
+    for (int i = 0; i < n; i += 2) { a += ex2(fmaf(x[i], c, -r)); b += ex2(fmaf(x[i + 1], c, -r)); }
+    s += a + b;
+  }
+};
+__device__ __forceinline__ float warp_max(float v) {
+  float t;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(t) : "f"(v));
+  return t;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ float block_sum(float v, float* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = threadIdx.x % 32 < blockDim.x / 32 ? red[threadIdx.x & 31] : 0.f;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+// The warp's pair, in every lane.
+__device__ __forceinline__ Fold warp_fold(Fold f, float c) {
+  Fold t;
+  t.m = warp_max(f.m);
+  t.r = ref_of(t.m, c);
+  t.s = warp_sum(f.r > -INFINITY ? f.s * ex2(f.r - t.r) : f.s);
+  return t;
+}
+
+// The teacher's entries in shared memory: id (-1: left out), p, and the row's logit there.
+struct TeacherView { int* id; float* p; float* x; };
+__device__ __forceinline__ TeacherView teacher_at(char* smem, int K) {
+  const int K4 = (K + 3) & ~3;
+  TeacherView v;
+  v.id = reinterpret_cast<int*>(smem); v.p = reinterpret_cast<float*>(smem) + K4; v.x = reinterpret_cast<float*>(smem) + 2 * K4;
   return v;
+}
+__host__ __device__ inline size_t teacher_bytes(int K) { return (size_t)((K + 3) & ~3) * 12; }
+
+// One warp: reads the K entries, normalises p over those that the row can see.  Returns whether there is one, and log2 of the
+// normaliser and the reference of the exponents (the base-2 logarithm of p_j is c t_j - ref - lg).
+__device__ __forceinline__ bool load_teacher(const DistillArgs& a, int r, int C, const TeacherView& v, float& ref, float& lg) {
+  const int lane = threadIdx.x & 31;
+  float tm = -INFINITY;
+  for (int j = lane; j < ((a.K + 3) & ~3); j += 32) {
+    int id = -1;
+    float t = -INFINITY;
+    if (j < a.K) {
+      id = a.ids[(size_t)r * a.K + j];
+      t = a.t[(size_t)r * a.K + j];
+    }
+    if ((unsigned)id >= (unsigned)C || t == -INFINITY) { id = -1; t = -INFINITY; }
+    v.id[j] = id; v.p[j] = t;
+    tm = fmaxf(tm, t != t ? INFINITY : t);
+  }
+  tm = warp_max(tm);
+  ref = a.c * tm; lg = 0.f;
+  if (tm == -INFINITY) return false;
+  float s = 0.f;
+  for (int j = lane; j < a.K; j += 32) if (v.id[j] >= 0) s += ex2(fmaf(v.p[j], a.c, -ref));
+  s = warp_sum(s);
+  lg = log2f(s);
+  const float inv = 1.f / s;
+  for (int j = lane; j < a.K; j += 32) if (v.id[j] >= 0) v.p[j] = ex2(fmaf(v.p[j], a.c, -ref)) * inv;
+  __syncwarp();
+  return true;
+}
+
+// The gradient in the teacher's columns [c0, c1), behind a barrier after the columns' own: k (q - sum of p), the sums by
+// whoever holds a column's first entry.  q_of(x): the probability of a column with logit x.
+template <typename T, typename Q>
+__device__ __forceinline__ void put_teacher(const DistillArgs& a, const TeacherView& v, T* out, int c0, int c1, float k, Q q_of) {
+  for (int j = threadIdx.x; j < a.K; j += blockDim.x) {
+    const int id = v.id[j];
+    if (id < c0 || id >= c1) continue;
+    float p = 0.f;
+    bool first = true;
+    for (int i = 0; i < a.K; i += 4) {
+      const int4 o = *reinterpret_cast<const int4*>(v.id + i);
+      if (o.x == id) { first &= i >= j; p += v.p[i]; }
+      if (o.y == id) { first &= i + 1 >= j; p += v.p[i + 1]; }
+      if (o.z == id) { first &= i + 2 >= j; p += v.p[i + 2]; }
+      if (o.w == id) { first &= i + 3 >= j; p += v.p[i + 3]; }
+    }
+    if (first) out[id] = from_f32<T>(k * (q_of(v.x[j]) - p));
+  }
+}
+
+__device__ __forceinline__ void copy_async(void* smem, const void* g) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(smem)), "l"(g) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Until at most `left` groups of this thread's copies are under way.
+__device__ __forceinline__ void copy_wait(int left) {
+  switch (left) {
+    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+    case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+  }
 }
 
 }  // namespace
 
-// One block per row.  BACKWARD: lse is given and only the gradient is written.
-template <typename T, bool BACKWARD>
-__global__ void __launch_bounds__(kDistillThreads) k_distill_row(DistillArgs a) {
-  __shared__ Teacher tc;
+// Grid: rows x blocks of a cluster.  HOLD: the share stays in shared memory (behind the teacher's entries).
+template <typename T, bool GRAD, bool HOLD>
+__global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
+  extern __shared__ __align__(16) char smem[];
+  constexpr int kN = kPer<T>, kMaxWarps = kDistillThreads / 32;
+  __shared__ float2 s_all[8 * kMaxWarps];                  // (m, s) of every warp of the row
+  __shared__ float s_t[3];                                 // the teacher's reference, log2 of its normaliser, 1 if it has an entry
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
   sm100::pdl_wait();
   sm100::pdl_trigger();
-  const int r = blockIdx.x, tid = threadIdx.x;
+  const int G = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), r = blockIdx.x / G;
+  if (G > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");       // (waited for before the first remote store)
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   const T* l = reinterpret_cast<const T*>(a.logits) + (size_t)r * a.ld;
   int C = a.n_cols ? a.n_cols[r] : a.cols;
   C = C < 0 ? 0 : (C > a.cols ? a.cols : C);
-  const float w = a.weight ? a.weight[r] : 1.f;
-  // teacher
-  float tm = -INFINITY;
-  for (int j = tid; j < a.K; j += kDistillThreads) {
-    const int id = a.ids[(size_t)r * a.K + j];
-    const float x = (unsigned)id < (unsigned)C ? a.t[(size_t)r * a.K + j] : -INFINITY;
-    tc.id[j] = x == -INFINITY ? -1 : id;
-    tc.p[j] = x;
-    tm = fmaxf(tm, x == x ? x : INFINITY);
+  const RowSplit sp = split_row(l, a.cols);
+  const int share = (sp.vecs + G - 1) / G, v0 = min(sp.vecs, rank * share), v1 = min(sp.vecs, v0 + share);
+  const uint4* lv = reinterpret_cast<const uint4*>(l + sp.head);
+  const int full = min(v1, max(v0, (C - sp.head) / kN));   // vectors [v0, full) are columns of the row; at most one behind is in part
+  const int U = (full - v0 + threads - 1) / threads, groups = (U + kFold - 1) / kFold;
+  uint4* hold = reinterpret_cast<uint4*>(smem + teacher_bytes(a.K));
+  // ---- the share's columns
+  if (HOLD) {
+    for (int g = 0; g < groups; ++g) {
+#pragma unroll
+      for (int u = 0; u < kFold; ++u) {
+        const int i = (g * kFold + u) * threads + tid;
+        if (v0 + i < full) copy_async(hold + i, lv + v0 + i);
+      }
+      copy_commit();
+    }
   }
-  tm = block_max(tm, tc.red);
-  const bool some = tm > -INFINITY;
-  float ts = 0.f;
-  for (int j = tid; j < a.K; j += kDistillThreads) if (tc.id[j] >= 0) ts += expf((tc.p[j] - tm) * a.inv_t);
-  ts = block_sum(ts, tc.red);
-  // student
-  float m = -INFINITY, s = 0.f, lse = 0.f;
-  if (!BACKWARD) {
-    for (int c = tid; c < C; c += kDistillThreads) m = fmaxf(m, to_f32<T>(l[c]));
-    m = block_max(m, tc.red);
-    for (int c = tid; c < C; c += kDistillThreads) { const float x = to_f32<T>(l[c]); s += x == -INFINITY ? 0.f : expf((x - m) * a.inv_t); }
-    s = block_sum(s, tc.red);
-    lse = s == 0.f ? -INFINITY : m * a.inv_t + logf(s);
+  // columns outside the vectors, and those of the vector that the row ends in: one a thread
+  int my_col = -1;
+  if (rank == 0 && tid < sp.head) my_col = tid;
+  else if (rank == G - 1 && tid >= 32 && tid < 32 + sp.tail) my_col = a.cols - sp.tail + tid - 32;
+  const float my_x = my_col >= 0 && my_col < C ? to_f32<T>(l[my_col]) : -INFINITY;
+  const int part = sp.head + full * kN, part_n = full < v1 ? max(0, min(kN, C - part)) : 0;
+  const float part_x = tid < part_n ? to_f32<T>(l[part + tid]) : -INFINITY;
+  // ---- the teacher, by one warp while the columns are under way.  The first block takes the loss and with it the row's
+  // logits there; the others find those of their own columns [c0, c1) in what they hold, or here.
+  const int c0 = rank == 0 ? 0 : sp.head + v0 * kN, c1 = rank == G - 1 ? a.cols : sp.head + v1 * kN;
+  auto held = [&](int id) { return HOLD && id >= sp.head + v0 * kN && id < part; };
+  const TeacherView tv = teacher_at(smem, a.K);
+  if (warp == warps - 1) {
+    float ref, lg;
+    const bool some = load_teacher(a, r, C, tv, ref, lg);
+    for (int j = lane; j < a.K; j += 32) {
+      const int id = tv.id[j];
+      if (id >= 0 && (rank == 0 || (id >= c0 && id < c1 && !held(id)))) tv.x[j] = to_f32<T>(l[id]);
+    }
+    if (lane == 0) { s_t[0] = ref; s_t[1] = lg; s_t[2] = some ? 1.f : 0.f; }
+  }
+  // ---- maximum and sum
+  Fold f;
+  const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;                     // -inf
+  {
+    const float two[2] = {my_x, part_x};
+    f.raise(fmaxf(my_x, part_x), a.c);
+    f.add(two, a.c);
+  }
+  for (int g = 0; g < groups; ++g) {
+    uint4 v[kFold];
+    if (HOLD) copy_wait(groups - 1 - g);
+#pragma unroll
+    for (int u = 0; u < kFold; ++u) {
+      const int i = (g * kFold + u) * threads + tid;
+      v[u] = v0 + i < full ? (HOLD ? hold[i] : lv[v0 + i]) : make_uint4(none, none, none, none);
+    }
+    f.raise(max_of<T, kFold>(v), a.c);
+#pragma unroll
+    for (int u = 0; u < kFold; ++u) {
+      if (v0 + (g * kFold + u) * threads + tid < full) { float x[kN]; unpack<T>(v[u], x); f.add(x, a.c); }
+    }
+  }
+  f = warp_fold(f, a.c);
+  if (G > 1) {
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (lane < G) *cluster.map_shared_rank(&s_all[rank * warps + warp], lane) = make_float2(f.m, f.s);
+    cluster.sync();                                        // (also: every logit has been read that a gradient may overwrite)
   } else {
-    lse = a.lse[r];
+    if (lane == 0) s_all[warp] = make_float2(f.m, f.s);
+    __syncthreads();
   }
-  const bool live = some && lse != -INFINITY;
-  float loss = 0.f;
-  for (int j = tid; j < a.K; j += kDistillThreads) {
-    const float x = (tc.p[j] - tm) * a.inv_t;
-    const float p = tc.id[j] >= 0 ? expf(x) / ts : 0.f;
-    if (!BACKWARD && p != 0.f) loss += p * (x - logf(ts) - ((to_f32<T>(l[tc.id[j]]) - m) * a.inv_t - logf(s)));
-    tc.p[j] = p;
+  f = Fold();
+  for (int i = lane; i < G * warps; i += 32) {
+    const float2 o = s_all[i];
+    const float orr = ref_of(o.x, a.c);
+    if (o.x > f.m) { f.s = o.y + (f.r > -INFINITY ? f.s * ex2(f.r - orr) : f.s); f.m = o.x; f.r = orr; }
+    else f.s += orr > -INFINITY ? o.y * ex2(orr - f.r) : o.y;
   }
-  if (!BACKWARD) {
-    loss = block_sum(loss, tc.red);
-    if (tid == 0) { a.loss[r] = live ? loss * a.temperature * a.temperature : 0.f; a.lse[r] = lse; }
+  f = warp_fold(f, a.c);
+  const bool some = s_t[2] != 0.f, live = some && f.s != 0.f;
+  const float ls = log2f(f.s);
+  if (rank == 0 && warp == 0 && a.loss) {
+    float loss = 0.f;
+    if (live) {
+      const float tl = s_t[0], lg = s_t[1];
+      for (int j = lane; j < a.K; j += 32) {
+        const float p = tv.p[j];
+        if (tv.id[j] >= 0 && p != 0.f) {
+          // log2 p_j again from the teacher's logit, which is exact where p_j is not
+          const float lp = fmaf(a.t[(size_t)r * a.K + j], a.c, -tl) - lg, lq = fmaf(tv.x[j], a.c, -f.r) - ls;
+          loss += p * (lp - lq);
+        }
+      }
+      loss = warp_sum(loss) * kLn2 * a.temperature * a.temperature;
+    }
+    if (lane == 0) { a.loss[r] = loss; a.lse[r] = f.s == 0.f ? -INFINITY : fmaf(f.m, a.inv_t, ls * kLn2); }
   }
-  if (!a.grad) return;
-  T* out = reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld;
+  if (!GRAD) return;
+  // ---- the gradient of the share
+  const float w = a.weight ? a.weight[r] : 1.f, k = w * a.temperature;
   const bool zero = !live || w == 0.f;
-  const float k = w * a.temperature;
+  T* out = reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld;
+  // k q: in bf16 with the factor in the exponent (an error of some 2^-19, to a step of 2^-8), otherwise as a product
+  const bool in_exponent = sizeof(T) == 2 && k > 0.f;
+  const float kq = in_exponent ? 1.f : k / f.s, off = in_exponent ? f.r + (ls - log2f(k)) : f.r;
+  auto value = [&](float x) { return ex2(fmaf(x, a.c, -off)) * kq; };
+  if (my_col >= 0) out[my_col] = from_f32<T>(zero || my_col >= C ? 0.f : value(my_x));
+  if (full < v1 && tid < kN) out[part + tid] = from_f32<T>(zero || tid >= part_n ? 0.f : value(part_x));
+  uint4* ov = reinterpret_cast<uint4*>(out + sp.head) + v0;
+  const int n_full = zero ? 0 : full - v0;
+  auto put = [&](int i, const float (&x)[kN]) {
+    if (!a.grad_skew) __stcs(ov + i, packed<T>(x));
+    else {
+#pragma unroll
+      for (int u = 0; u < kN; ++u) out[sp.head + (v0 + i) * kN + u] = from_f32<T>(x[u]);
+    }
+  };
+  auto columns = [&](auto scaled) {
+#pragma unroll 4
+    for (int i = tid; i < n_full; i += threads) {
+      float x[kN];
+      unpack<T>(HOLD ? hold[i] : lv[v0 + i], x);
+#pragma unroll
+      for (int u = 0; u < kN; ++u) x[u] = decltype(scaled)::value ? value(x[u]) : ex2(fmaf(x[u], a.c, -off));
+      put(i, x);
+    }
+  };
+  if (in_exponent) columns(std::false_type()); else columns(std::true_type());
+  const float nothing[kN] = {};
+  for (int i = n_full + tid; i < v1 - v0; i += threads) if (zero || v0 + i != full) put(i, nothing);
+  if (zero) return;
   __syncthreads();
-  // the teacher's columns: taken before the row is overwritten, written behind it
-  float at[kDistillMaxK / kDistillThreads];
-  int n_at = 0;
-  for (int j = tid; j < a.K; j += kDistillThreads, ++n_at) {
-    const int id = tc.id[j];
+  // the teacher's columns, over the columns' own: k (q - sum of p), the sum by whoever holds a column's first entry
+  for (int j = tid; j < a.K; j += threads) {
+    const int id = tv.id[j];
+    if (id < c0 || id >= c1) continue;
     float p = 0.f;
-    bool first = id >= 0;
-    for (int i = 0; i < a.K && first; ++i)
-      if (tc.id[i] == id) { if (i < j) first = false; else p += tc.p[i]; }
-    const float x = first ? to_f32<T>(l[id]) : 0.f;
-    const float q = BACKWARD ? expf(fmaf(x, a.inv_t, -lse)) : expf((x - m) * a.inv_t) / s;
-    at[n_at & 1] = first ? k * (q - p) : 0.f;
-  }
-  __syncthreads();
-  for (int c = tid; c < a.cols; c += kDistillThreads) {
-    float d = 0.f;
-    if (!zero && c < C) {
-      const float x = to_f32<T>(l[c]);
-      d = k * (BACKWARD ? expf(fmaf(x, a.inv_t, -lse)) : (x == -INFINITY ? 0.f : expf((x - m) * a.inv_t)) / s);
+    bool first = true;
+    for (int i = 0; i < a.K; i += 4) {
+      const int4 o = *reinterpret_cast<const int4*>(tv.id + i);
+      if (o.x == id) { first &= i >= j; p += tv.p[i]; }
+      if (o.y == id) { first &= i + 1 >= j; p += tv.p[i + 1]; }
+      if (o.z == id) { first &= i + 2 >= j; p += tv.p[i + 2]; }
+      if (o.w == id) { first &= i + 3 >= j; p += tv.p[i + 3]; }
     }
-    out[c] = from_f32<T>(d);
+    if (!first) continue;
+    const float x = rank != 0 && held(id) ? to_f32<T>(reinterpret_cast<const T*>(hold)[id - sp.head - v0 * kN]) : tv.x[j];
+    out[id] = from_f32<T>(k * (ex2(fmaf(x, a.c, -f.r)) / f.s - p));
   }
-  __syncthreads();
-  n_at = 0;
-  if (!zero)
-    for (int j = tid; j < a.K; j += kDistillThreads, ++n_at) {
-      const int id = tc.id[j];
-      bool first = id >= 0;
-      for (int i = 0; i < j && first; ++i) if (tc.id[i] == id) first = false;
-      if (first) out[id] = from_f32<T>(at[n_at & 1]);
-    }
 }
 
 namespace {
+
 int fail_arg(const char* msg) { set_last_error(msg); return Z2Z_ERR_INVALID_ARG; }
 
 int check_distill(const void* logits, int dtype, int N, int cols, int64_t ld, const int32_t* ids, const float* t, int K, float temperature,
@@ -155,12 +410,54 @@ int check_distill(const void* logits, int dtype, int N, int cols, int64_t ld, co
   return Z2Z_OK;
 }
 
-template <bool BACKWARD>
-int launch_distill(const DistillArgs& a, int dtype, int N, cudaStream_t s) {
-  cudaError_t e = dtype == Z2Z_DTYPE_BF16 ? launch_pdl(k_distill_row<__nv_bfloat16, BACKWARD>, dim3(N), dim3(kDistillThreads), 0, s, a)
-                                          : launch_pdl(k_distill_row<float, BACKWARD>, dim3(N), dim3(kDistillThreads), 0, s, a);
-  if (e != cudaSuccess) { set_last_error(cudaGetErrorString(e)); return Z2Z_ERR_CUDA; }
-  return Z2Z_OK;
+int done(cudaError_t e) {
+  if (e == cudaSuccess) return Z2Z_OK;
+  set_last_error(cudaGetErrorString(e));
+  return Z2Z_ERR_CUDA;
+}
+
+template <typename T, bool GRAD, bool HOLD>
+cudaError_t launch_loss_typed(const DistillArgs& a, int N, int G, int threads, size_t smem, cudaStream_t s) {
+  auto kern = k_distill<T, GRAD, HOLD>;
+  if (smem > 48 << 10) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)N * (unsigned)G);
+  lc.blockDim = dim3(threads);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)G; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = at; lc.numAttrs = 2;
+  return cudaLaunchKernelEx(&lc, kern, a);
+}
+
+template <typename T>
+cudaError_t launch_loss(const DistillArgs& a, int N, cudaStream_t s) {
+  const size_t row = (size_t)a.cols * sizeof(T);
+  // Blocks per row: so many that a block's share leaves room for three on an SM, and more while all rows together do not
+  // occupy the machine's SMs
+  int G = 1;
+  while (G < 8 && (row / G > kShareBytes || ((long long)N * 2 * G <= 148 && row / G > 4096))) G *= 2;
+  const int vecs = (int)((row / 16 + G - 1) / G);
+  int threads = (vecs / 2 + 63) / 64 * 64;                 // two vectors a thread at least
+  threads = threads < 64 ? 64 : (threads > kDistillThreads ? kDistillThreads : threads);
+  const size_t teacher = teacher_bytes(a.K), share = (size_t)vecs * 16;
+  if (!a.grad) return launch_loss_typed<T, false, false>(a, N, G, threads, teacher, s);
+  if (share <= kShareMax) return launch_loss_typed<T, true, true>(a, N, G, threads, teacher + share, s);
+  return launch_loss_typed<T, true, false>(a, N, G, threads, teacher, s);
+}
+
+DistillArgs distill_args(const void* logits, int cols, int64_t ld, const int32_t* n_cols, const int32_t* ids, const float* t, int K, float temperature,
+                         const float* weight, float* loss, float* lse, void* grad) {
+  const int skew = grad && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(logits)) & 15) ? 1 : 0;
+  return DistillArgs{logits, cols, ld, n_cols, ids, t, K, 1.f / temperature, temperature, (float)(1.4426950408889634 / (double)temperature),
+                     weight, loss, lse, grad, skew};
 }
 }  // namespace
 
@@ -176,9 +473,10 @@ int32_t z2z_distill_loss(const void* d_logits, int32_t dtype, int32_t N, int32_t
   const int rc = z2z::check_distill(d_logits, dtype, N, cols, ld, d_teacher_ids, d_teacher_logits, K, temperature, d_grad);
   if (rc || N == 0) return rc;
   if (!d_loss || !d_lse) return z2z::fail_arg("d_loss / d_lse is NULL");
-  z2z::DistillArgs a{d_logits, cols, ld, d_n_cols, d_teacher_ids, d_teacher_logits, K, 1.f / temperature, temperature,
-                     d_row_weight, d_loss, d_lse, d_grad};
-  return z2z::launch_distill<false>(a, dtype, N, reinterpret_cast<cudaStream_t>(stream));
+  const z2z::DistillArgs a = z2z::distill_args(d_logits, cols, ld, d_n_cols, d_teacher_ids, d_teacher_logits, K, temperature, d_row_weight, d_loss,
+                                               d_lse, d_grad);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return z2z::done(dtype == Z2Z_DTYPE_BF16 ? z2z::launch_loss<__nv_bfloat16>(a, N, s) : z2z::launch_loss<float>(a, N, s));
 }
 
 int32_t z2z_distill_grad(const void* d_logits, int32_t dtype, int32_t N, int32_t cols, int64_t ld,
@@ -188,9 +486,10 @@ int32_t z2z_distill_grad(const void* d_logits, int32_t dtype, int32_t N, int32_t
   const int rc = z2z::check_distill(d_logits, dtype, N, cols, ld, d_teacher_ids, d_teacher_logits, K, temperature, d_grad);
   if (rc || N == 0) return rc;
   if (!d_lse || !d_grad_loss || !d_grad) return z2z::fail_arg("d_lse / d_grad_loss / d_grad is NULL");
-  z2z::DistillArgs a{d_logits, cols, ld, d_n_cols, d_teacher_ids, d_teacher_logits, K, 1.f / temperature, temperature,
-                     d_grad_loss, nullptr, const_cast<float*>(d_lse), d_grad};
-  return z2z::launch_distill<true>(a, dtype, N, reinterpret_cast<cudaStream_t>(stream));
+  const z2z::DistillArgs a = z2z::distill_args(d_logits, cols, ld, d_n_cols, d_teacher_ids, d_teacher_logits, K, temperature, d_grad_loss, nullptr,
+                                               nullptr, d_grad);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return z2z::done(dtype == Z2Z_DTYPE_BF16 ? z2z::launch_loss<__nv_bfloat16>(a, N, s) : z2z::launch_loss<float>(a, N, s));
 }
 
 }  // extern "C"
