@@ -294,12 +294,14 @@ int32_t z2z_embed_grad(z2z_codebook* cb, const int32_t* d_codes, int32_t N, cons
  *            left out, a logit of -inf has no probability, and what the same column is given twice adds up;
  *   temperature > 0, finite;
  *   d_loss [N] out, d_lse [N] out: log sum_c exp(l_c / T).
- * A row without columns, or with nothing but -inf (lse = -inf), and a row that is left no teacher entry, has
- * loss 0 and gradient 0.  A NaN or +inf logit makes the loss, lse and gradient of its row NaN.
+ * A row without columns, or masked throughout (nothing but -inf or values at or below -2^126, such as the
+ * lowest of the type: lse = -inf), and a row that is left no teacher entry, has loss 0 and gradient 0.
+ * A NaN or +inf logit makes the loss, lse and gradient of its row NaN (without a teacher entry: the lse).
  * z2z_distill_loss also writes, when d_grad is not NULL, the gradient of sum_r w_r loss_r in the same pass over
  * the logits: d_row_weight [N] = w, or NULL = 1 (d_loss stays unweighted; without d_grad it is not read).
- * z2z_distill_grad is the backward pass on its own: d_lse is what z2z_distill_loss left there for the same
- * arguments, d_grad_loss [N] the derivative for d_loss.
+ * z2z_distill_grad is the backward pass on its own: d_grad_loss [N] is the derivative for d_loss, d_lse what
+ * z2z_distill_loss left there for the same arguments (rows of -inf are not read again; the normaliser of the
+ * others is found anew, since lse has lost 2^-24 of its size, and every probability with it).
  *   d_grad [N, cols] of dtype, rows ld apart: every column is written, 0 from n_cols on.  A row whose
  *            weight is 0 has gradient 0 whatever its logits are.  d_grad == d_logits is allowed (the
  *            logits are then overwritten); they must not overlap in another way.                   */

@@ -237,7 +237,7 @@ int32_t z2z_codebook_init(z2z_codebook** cb, const z2z_config* cfg, void* d_ws, 
   v.status = reinterpret_cast<int32_t*>(h->ws + plan.off_status);
   v.n_emb = reinterpret_cast<int32_t*>(h->ws + plan.off_n_emb);
   *cb = h;
-  Z2Z_CUDA(cudaMemsetAsync(h->ws + plan.off_words, 0, 256, reinterpret_cast<cudaStream_t>(stream)), "codebook_init");
+  Z2Z_CUDA(cudaMemsetAsync(h->ws + plan.off_words, 0, 256 + plan.tickets_bytes, reinterpret_cast<cudaStream_t>(stream)), "codebook_init");
   // The stream GEMM's result matrix is all zero between GEMMs.  What a decode step uses of it (1-10 MB) is
   // cleared here together with the codebooks, so that a graph captured from the session's first steps holds
   // no clear; a pass that needs more clears the rest itself.  (The whole matrix is 280-440 MB at d = 3072 /
@@ -376,6 +376,7 @@ int32_t z2z_beam_select(z2z_codebook* cb, int32_t beams, const float* d_logits, 
   a.beams = beams; a.logits = d_logits; a.lse = d_lse; a.scores = d_scores; a.finished = d_finished; a.eos = eos;
   a.parent = d_parent; a.code = d_code; a.next_scores = d_next_scores; a.next_finished = d_next_finished; a.active = d_active;
   a.lists = cb->ws + cb->plan.off_lpart; a.lists_bytes = cb->plan.lpart_bytes;
+  a.tickets = reinterpret_cast<unsigned*>(cb->ws + cb->plan.off_tickets);
   Z2Z_CUDA(z2z::launch_beam_select(cb->view, a, reinterpret_cast<cudaStream_t>(stream)), "beam_select");
   return Z2Z_OK;
 }

@@ -70,6 +70,7 @@ struct WsPlan {
   size_t off_Ahl, off_Hhl;                        // bf16 hi/lo activations (tensor-core path)
   size_t off_g1_X, off_g1_QKV, off_g1_Ahl, off_g1_Hhl;   // second encoder of the decode step
   size_t off_words;                               // device words: [0] kernel error, [2], [3] decode logits, [4] decode update
+  size_t off_tickets, tickets_bytes;              // blocks of a beam selection that are done, a word per group; behind the words
   size_t off_part, part_bytes;                    // fp32 GEMM results of the hyper-encoder passes
   size_t off_lpart, lpart_bytes;                  // logits partial reductions
   size_t off_plan, plan_bytes;                    // per-row-tile plan of the prompt-scoring logits kernel
@@ -140,6 +141,8 @@ inline WsPlan plan_workspace(const z2z_config& c) {
   p.part_bytes = ((Rp / 128) * 2 * ((wide + 127) / 128) + 256) * (size_t)65536;
   p.off_part = take(p.part_bytes);
   p.off_words = take(256);
+  p.tickets_bytes = (size_t)c.B * 4;
+  p.off_tickets = take(p.tickets_bytes);
   p.lpart_bytes = (size_t)kLogitPartRows * 32;
   p.off_lpart = take(p.lpart_bytes);
   p.plan_bytes = (size_t)kPrefillPlanTiles * 3 * 4;

@@ -73,13 +73,14 @@ struct BeamSelectArgs {
   int32_t* parent; int32_t* code; float* next_scores; uint8_t* next_finished; uint8_t* active;
   char* lists;                  // scratch: each beam's best columns
   size_t lists_bytes;
+  unsigned* tickets;            // a word per group, zero before and after
 };
 cudaError_t launch_beam_select(const CbView& cb, const BeamSelectArgs& a, cudaStream_t s);
 constexpr int kMaxSeqRows = 8;
 struct BeamReorderArgs {
   const int32_t* parent;
   char* cache[4]; int cache_row_bytes[4]; int n_caches;        // [B, cap] rows
-  char* rows[kMaxSeqRows]; size_t stride[kMaxSeqRows], bytes[kMaxSeqRows]; int n_rows;
+  char* rows[kMaxSeqRows + 1]; size_t stride[kMaxSeqRows + 1], bytes[kMaxSeqRows + 1]; int n_rows;      // (one more for the hash)
 };
 cudaError_t launch_beam_reorder(const CbView& cb, const BeamReorderArgs& a, cudaStream_t s);
 
