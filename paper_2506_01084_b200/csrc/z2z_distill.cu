@@ -32,6 +32,8 @@ constexpr int kDistillMaxK = 1024;
 constexpr int kDistillThreads = 256;     // of a block, at most
 constexpr int kFold = 4;                 // vectors of 16 bytes that a thread folds at once, and waits for at once
 constexpr size_t kShareBytes = 72 << 10;              // of a row per block, for three blocks per SM
+constexpr size_t kStreamRow = 32 << 10;               // rows from here on for the persistent form
+constexpr int kStreamSlots = 148;                     // its blocks
 constexpr size_t kShareMax = 208 << 10;               // ... and at most, for one
 
 struct DistillArgs {
@@ -85,20 +87,18 @@ template <typename T> __device__ __forceinline__ RowSplit split_row(const T* row
 }
 
 // Maximum of the columns of some vectors (NaN does not count).
-template <typename T, int n> __device__ __forceinline__ float max_of(const uint4 (&v)[n]);
-template <> __device__ __forceinline__ float max_of<float, kFold>(const uint4 (&v)[kFold]) {
-  float t = -INFINITY;
+template <typename T, int n> __device__ __forceinline__ float max_of(const uint4 (&v)[n]) {
+  if (sizeof(T) == 4) {
+    float t = -INFINITY;
 #pragma unroll
-  for (int u = 0; u < kFold; ++u)
-    t = fmaxf(t, fmaxf(fmaxf(__uint_as_float(v[u].x), __uint_as_float(v[u].y)), fmaxf(__uint_as_float(v[u].z), __uint_as_float(v[u].w))));
-  return t;
-}
-template <> __device__ __forceinline__ float max_of<__nv_bfloat16, kFold>(const uint4 (&v)[kFold]) {
+    for (int u = 0; u < n; ++u)
+      t = fmaxf(t, fmaxf(fmaxf(__uint_as_float(v[u].x), __uint_as_float(v[u].y)), fmaxf(__uint_as_float(v[u].z), __uint_as_float(v[u].w))));
+    return t;
+  }
   auto two = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
   __nv_bfloat162 t = two(v[0].x);
 #pragma unroll
-  for (int u = 0; u < kFold; ++u)
-    t = __hmax2(t, __hmax2(__hmax2(two(v[u].x), two(v[u].y)), __hmax2(two(v[u].z), two(v[u].w))));
+  for (int u = 0; u < n; ++u) t = __hmax2(t, __hmax2(__hmax2(two(v[u].x), two(v[u].y)), __hmax2(two(v[u].z), two(v[u].w))));
   return fmaxf(__low2float(t), __high2float(t));
 }
 
@@ -123,10 +123,14 @@ struct Fold {
       for (int i = 0; i < n; ++i) s += x[i] == x[i] ? 0.f : x[i];
       return;
     }
-    float a = 0.f, b = 0.f;
+    float e[n];
 #pragma unroll
-    for (int i = 0; i < n; i += 2) { a += ex2(fmaf(x[i], c, -r)); b += ex2(fmaf(x[i + 1], c, -r)); }
-    s += a + b;
+    for (int i = 0; i < n; ++i) e[i] = ex2(fmaf(x[i], c, -r));
+#pragma unroll
+    for (int w = n / 2; w > 0; w /= 2)
+#pragma unroll
+      for (int i = 0; i < w; ++i) e[i] += e[i + w];
+    s += e[0];
   }
 };
 __device__ __forceinline__ float warp_max(float v) {
@@ -224,6 +228,301 @@ __device__ __forceinline__ void copy_wait(int left) {
 
 }  // namespace
 
+// Many long rows: one persistent block per SM, each with a row, or clusters of a few blocks with one.  A block goes over its
+// share twice, the second time for the gradient.  The rows in work at one time are held to kLiveBytes, which L2 keeps until
+// they are read again, so that HBM sees the logits once.  (Two blocks per SM with a row each, 78 MB: half of the second
+// read missed L2.  Holding the rows in the shared memory of clusters of four: a fourth of every row's time went into its
+// barrier, and clusters of four leave a seventh of the SMs without work: 291 us for 2048 bf16 rows of 132352 columns.)
+// One thread fills a ring of kStages chunks by bulk copies and runs on from the first pass into the second and from there into
+// the next row.  Thirty warps have the columns; one more has, a row ahead, the teacher, the columns outside the
+// vectors and the loss, and, behind the barrier of the following row, the teacher's columns of the gradient.
+constexpr int kStreamWarps = 30, kStreamThreads = 32 * kStreamWarps, kStreamK = 256, kStages = 3;
+constexpr int kPairs = kStreamWarps + 1;                   // warps that meet in a row's exchange
+constexpr int kChunk = kFold * kStreamThreads;             // vectors of a chunk, at most
+constexpr size_t kLiveBytes = (size_t)40 << 20;
+
+struct alignas(16) StreamTeacher { int id[kStreamK]; float p[kStreamK], x[kStreamK]; float ref, lg; int some, c0, c1; };
+
+// One warp: x becomes the gradient in this block's teacher columns, k (q - sum of p), with the sum in a column's first entry;
+// id becomes -1 where nothing is to be written.
+__device__ __forceinline__ void finish_teacher(const DistillArgs& a, StreamTeacher& t, bool zero, float k, const Fold& f) {
+  const int lane = threadIdx.x & 31;
+  unsigned write = 0u;                                     // bit per entry of this lane
+  for (int j = lane, b = 0; j < a.K; j += 32, ++b) {
+    const int id = t.id[j];
+    if (zero || id < t.c0 || id >= t.c1) continue;
+    float p = 0.f;
+    bool first = true;
+    for (int i = 0; i < a.K; i += 4) {
+      const int4 o = *reinterpret_cast<const int4*>(t.id + i);
+      if (o.x == id || o.y == id || o.z == id || o.w == id) {
+        if (o.x == id) { first &= i >= j; p += t.p[i]; }
+        if (o.y == id) { first &= i + 1 >= j; p += t.p[i + 1]; }
+        if (o.z == id) { first &= i + 2 >= j; p += t.p[i + 2]; }
+        if (o.w == id) { first &= i + 3 >= j; p += t.p[i + 3]; }
+      }
+    }
+    if (!first) continue;
+    t.x[j] = k * (ex2(fmaf(t.x[j], a.c, -f.r)) / f.s - p);
+    write |= 1u << b;
+  }
+  __syncwarp();
+  for (int j = lane, b = 0; j < a.K; j += 32, ++b) if (!((write >> b) & 1u)) t.id[j] = -1;
+  __syncwarp();
+}
+template <typename T> __device__ __forceinline__ void put_teacher(const DistillArgs& a, const StreamTeacher& t, T* out) {
+  for (int j = threadIdx.x & 31; j < a.K; j += 32) if (t.id[j] >= 0) out[t.id[j]] = from_f32<T>(t.x[j]);
+}
+
+// A block's part of a row: vectors [v0, v1), up to `full` columns of the row; columns [c0, c1) in all.
+template <typename T> struct RowPart { const T* l; int head, v0, v1, full, c0, c1; };
+
+// Chunks of a part of n vectors: as many as it takes, all of about the same size, at least one.
+__device__ __forceinline__ int chunks_of(int n) { return n <= kChunk ? 1 : (n + kChunk - 1) / kChunk; }
+
+template <typename T, bool GRAD>
+__global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(DistillArgs a, int N, int log_g) {
+  extern __shared__ __align__(128) char smem[];
+  constexpr int kN = kPer<T>;
+  __shared__ float2 s_all[2][8 * kPairs];
+  __shared__ StreamTeacher s_teacher[2];
+  __shared__ __align__(8) unsigned long long s_full[kStages], s_empty[kStages], s_pairs[2];
+  __shared__ int s_abort;                                  // a wait has given up: no one waits any more, the losses are NaN
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  sm100::pdl_wait();
+  sm100::pdl_trigger();
+  const int G = 1 << log_g, rank = (int)cluster.block_rank();
+  const int clusters = gridDim.x >> log_g, r0 = blockIdx.x >> log_g;
+  const int rows = r0 < N ? (N - r0 + clusters - 1) / clusters : 0;
+  const int tid = threadIdx.x, lane = tid & 31, warp = sm100::uniform_warp();
+  auto row_at = [&](int i) { return r0 + i * clusters; };
+  auto cols_of = [&](int i) {
+    if (i >= rows) return 0;
+    const int c = a.n_cols ? a.n_cols[row_at(i)] : a.cols;
+    return c < 0 ? 0 : (c > a.cols ? a.cols : c);
+  };
+  auto part_of = [&](int i, int C) {
+    RowPart<T> q;
+    q.l = reinterpret_cast<const T*>(a.logits) + (size_t)row_at(i) * a.ld;
+    const RowSplit sp = split_row(q.l, a.cols);
+    const int share = (sp.vecs + G - 1) >> log_g;
+    q.head = sp.head;
+    q.v0 = min(sp.vecs, rank * share); q.v1 = min(sp.vecs, q.v0 + share);
+    q.full = min(q.v1, max(q.v0, (C - sp.head) / kN));
+    q.c0 = rank == 0 ? 0 : q.head + q.v0 * kN; q.c1 = rank == G - 1 ? a.cols : q.head + q.v1 * kN;
+    return q;
+  };
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) { sm100::mbar_init(sm100::smem_u32(&s_full[i]), 1); sm100::mbar_init(sm100::smem_u32(&s_empty[i]), kStreamWarps); }
+    for (int i = 0; i < 2; ++i) sm100::mbar_init(sm100::smem_u32(&s_pairs[i]), 1);
+    s_abort = 0;
+    sm100::mbar_init_fence();
+  }
+  if (G > 1) cluster.sync();                               // all blocks are there before anything is sent to them
+  else __syncthreads();
+  if (rows == 0) return;
+  auto wait = [&](unsigned long long* bar, int parity) {   // by a whole warp
+    if (!*reinterpret_cast<volatile int*>(&s_abort)) sm100::mbar_wait(sm100::smem_u32(bar), (uint32_t)parity, &s_abort);
+    __syncwarp();
+  };
+  // one exchange per row: every warp's pair to all blocks of the cluster.  Behind it all that the block's warps did ahead of
+  // it is done.
+  auto exchange = [&](int i, Fold f) {
+    f = warp_fold(f, a.c);
+    if (G == 1) {
+      if (lane == 0) s_all[i & 1][warp] = make_float2(f.m, f.s);
+    } else {
+      if (warp == kStreamWarps && lane == 0) sm100::mbar_expect_tx(sm100::smem_u32(&s_pairs[i & 1]), (uint32_t)(G * kPairs * 8));
+      if (lane < G)
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                     ::"r"(sm100::map_to_cta(sm100::smem_u32(&s_all[i & 1][rank * kPairs + warp]), lane)), "f"(f.m), "f"(f.s),
+                       "r"(sm100::map_to_cta(sm100::smem_u32(&s_pairs[i & 1]), lane)) : "memory");
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kPairs) : "memory");
+    if (G > 1) wait(&s_pairs[i & 1], (i >> 1) & 1);
+    f = Fold();
+    for (int j = lane; j < G * kPairs; j += 32) {
+      const float2 o = s_all[i & 1][j];
+      const float orr = ref_of(o.x, a.c);
+      if (o.x > f.m) { f.s = o.y + (f.r > -INFINITY ? f.s * ex2(f.r - orr) : f.s); f.m = o.x; f.r = orr; }
+      else f.s += orr > -INFINITY ? o.y * ex2(orr - f.r) : o.y;
+    }
+    return warp_fold(f, a.c);
+  };
+  if (warp < kStreamWarps) {
+    // ---- the columns
+    const uint4* const ring = reinterpret_cast<const uint4*>(smem) + tid;
+    const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;                   // -inf
+    int stage = 0, phase = 0;
+    // this thread's vectors of the next chunk, of which the block has n; what lies behind them is -inf
+    auto take = [&](uint4 (&v)[kFold], int n) {
+      wait(&s_full[stage], phase);
+      const uint4* from = ring + stage * kChunk;
+#pragma unroll
+      for (int u = 0; u < kFold; ++u) v[u] = u * kStreamThreads + tid < n ? from[u * kStreamThreads] : make_uint4(none, none, none, none);
+      __syncwarp();
+      if (lane == 0) sm100::mbar_arrive(sm100::smem_u32(&s_empty[stage]));
+      if (++stage == kStages) { stage = 0; phase ^= 1; }
+    };
+    int C1 = cols_of(1);
+    RowPart<T> q = part_of(0, cols_of(0));
+    for (int i = 0; i < rows; ++i) {
+      const int r = row_at(i), n = q.full - q.v0, chunks = chunks_of(n), per = (n + chunks - 1) / chunks;
+      const float w = GRAD && a.weight ? a.weight[r] : 1.f;
+      Fold f;
+      for (int v0 = 0, c = 0; c < chunks; ++c, v0 += per) {
+        uint4 v[kFold];
+        const int m = min(per, n - v0);
+        take(v, m);
+        f.raise(max_of<T>(v), a.c);
+#pragma unroll
+        for (int u = 0; u < kFold; ++u)
+          if (u * kStreamThreads + warp * 32 < m) { float x[kN]; unpack<T>(v[u], x); f.add(x, a.c); }
+      }
+      f = exchange(i, f);
+      if (GRAD) {
+        const bool zero = !s_teacher[i & 1].some || f.s == 0.f || w == 0.f;
+        const float k = w * a.temperature;
+        // k q: in bf16 with the factor in the exponent (an error of some 2^-19, to a step of 2^-8), otherwise as a product
+        const bool in_exponent = sizeof(T) == 2 && k > 0.f;
+        const float kq = zero ? 0.f : in_exponent ? 1.f : k / f.s;
+        const float off = in_exponent ? f.r + (log2f(f.s) - log2f(k)) : f.r;
+        T* out = reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld + q.head;
+        uint4* ov = reinterpret_cast<uint4*>(out) + q.v0;
+        auto put = [&](int v, const uint4& x) {
+          if (!a.grad_skew) { __stcs(ov + v, x); return; }
+          const T* e = reinterpret_cast<const T*>(&x);
+#pragma unroll
+          for (int u = 0; u < kN; ++u) out[(q.v0 + v) * kN + u] = e[u];
+        };
+        for (int v0 = 0, c = 0; c < chunks; ++c, v0 += per) {
+          uint4 v[kFold];
+          const int m = min(per, n - v0);
+          take(v, m);
+#pragma unroll
+          for (int u = 0; u < kFold; ++u) {
+            if (u * kStreamThreads + warp * 32 >= m) break;
+            float x[kN];
+            unpack<T>(v[u], x);
+            if (zero) {
+#pragma unroll
+              for (int e = 0; e < kN; ++e) x[e] = 0.f;
+            } else {
+#pragma unroll
+              for (int e = 0; e < kN; ++e) x[e] = ex2(fmaf(x[e], a.c, -off));
+              if (!in_exponent) {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) x[e] *= kq;
+              }
+            }
+            if (u * kStreamThreads + tid < m) put(v0 + u * kStreamThreads + tid, packed<T>(x));
+          }
+        }
+        for (int v = max(n, 0) + tid; v < q.v1 - q.v0; v += kStreamThreads) if (q.v0 + v != q.full) put(v, make_uint4(0u, 0u, 0u, 0u));
+      }
+      if (i + 1 < rows) { q = part_of(i + 1, C1); C1 = cols_of(i + 2); }
+    }
+    if (GRAD) asm volatile("bar.sync 1, %0;" ::"n"(32 * kPairs) : "memory");
+  } else if (warp == kStreamWarps) {
+    // ---- everything else
+    // columns outside the vectors, one a lane: in front of them, of the one that the row ends in, behind them
+    auto edge_of = [&](const RowPart<T>& q) {
+      if (lane < 8) return rank == 0 && lane < q.head ? lane : -1;
+      if (lane < 16) return q.full < q.v1 && lane - 8 < kN ? q.head + q.full * kN + lane - 8 : -1;
+      const int tail = a.cols - q.head - (a.cols - q.head) / kN * kN;
+      return lane < 24 && rank == G - 1 && lane - 16 < tail ? a.cols - tail + lane - 16 : -1;
+    };
+    float edge_x = 0.f;
+    // the first block takes the loss and with it the row's logits at all entries, the others those of their own columns
+    auto prepare = [&](int i, int C, const RowPart<T>& q) {
+      StreamTeacher& t = s_teacher[i & 1];
+      const int e = edge_of(q);
+      edge_x = e >= 0 && e < C ? to_f32<T>(q.l[e]) : -INFINITY;
+      const TeacherView tv{t.id, t.p, t.x};
+      float ref, lg;
+      const bool some = load_teacher(a, row_at(i), C, tv, ref, lg);
+      for (int j = lane; j < a.K; j += 32) {
+        const int id = t.id[j];
+        if (id >= 0 && (rank == 0 || (id >= q.c0 && id < q.c1))) t.x[j] = to_f32<T>(q.l[id]);
+      }
+      if (lane == 0) { t.ref = ref; t.lg = lg; t.some = some; t.c0 = q.c0; t.c1 = q.c1; }
+      __syncwarp();
+    };
+    int C = cols_of(0), C1 = cols_of(1);
+    RowPart<T> q = part_of(0, C);
+    prepare(0, C, q);
+    for (int i = 0; i < rows; ++i) {
+      const int r = row_at(i);
+      const float w = GRAD && a.weight ? a.weight[r] : 1.f;
+      Fold f;
+      const float two[2] = {edge_x, -INFINITY};
+      f.raise(edge_x, a.c);
+      f.add(two, a.c);
+      f = exchange(i, f);
+      // (all warps of the block have written the row before's gradient)
+      if (GRAD && i > 0) put_teacher<T>(a, s_teacher[(i - 1) & 1], reinterpret_cast<T*>(a.grad) + (size_t)row_at(i - 1) * a.ld);
+      StreamTeacher& t = s_teacher[i & 1];
+      const bool live = t.some && f.s != 0.f;
+      const float ls = log2f(f.s);
+      if (rank == 0 && a.loss) {
+        float loss = 0.f;
+        if (live)
+          for (int j = lane; j < a.K; j += 32) {
+            const float p = t.p[j];
+            if (t.id[j] >= 0 && p != 0.f) loss += p * (fmaf(a.t[(size_t)r * a.K + j], a.c, -t.ref) - t.lg - (fmaf(t.x[j], a.c, -f.r) - ls));
+          }
+        loss = warp_sum(loss) * kLn2 * a.temperature * a.temperature;
+        const bool lost = *reinterpret_cast<volatile int*>(&s_abort) != 0;
+        if (lane == 0) { a.loss[r] = lost ? NAN : loss; a.lse[r] = lost ? NAN : f.s == 0.f ? -INFINITY : fmaf(f.m, a.inv_t, ls * kLn2); }
+      }
+      if (GRAD) {
+        const bool zero = !live || w == 0.f;
+        const float k = w * a.temperature;
+        const int e = edge_of(q);
+        if (e >= 0) (reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld)[e] = from_f32<T>(zero || e >= C ? 0.f : k * (ex2(fmaf(edge_x, a.c, -f.r)) / f.s));
+        finish_teacher(a, t, zero, k, f);
+      }
+      if (i + 1 < rows) {
+        C = C1; C1 = cols_of(i + 2);
+        q = part_of(i + 1, C);
+        prepare(i + 1, C, q);
+      }
+    }
+    if (GRAD) {
+      asm volatile("bar.sync 1, %0;" ::"n"(32 * kPairs) : "memory");
+      put_teacher<T>(a, s_teacher[(rows - 1) & 1], reinterpret_cast<T*>(a.grad) + (size_t)row_at(rows - 1) * a.ld);
+    }
+  } else {
+    // ---- the copies
+    int stage = 0, phase = 1;                              // (a stage that was never filled is empty)
+    int C1 = cols_of(0);
+    for (int i = 0; i < rows; ++i) {
+      const RowPart<T> q = part_of(i, C1);
+      C1 = cols_of(i + 1);
+      const uint4* lv = reinterpret_cast<const uint4*>(q.l + q.head) + q.v0;
+      const int n = q.full - q.v0, chunks = chunks_of(n), per = (n + chunks - 1) / chunks;
+      for (int pass = 0; pass < (GRAD ? 2 : 1); ++pass)
+        for (int v0 = 0, c = 0; c < chunks; ++c, v0 += per) {
+          wait(&s_empty[stage], phase);
+          const int m = min(per, n - v0);
+          if (lane == 0) {
+            const uint32_t bar = sm100::smem_u32(&s_full[stage]);
+            if (m <= 0) sm100::mbar_arrive(bar);           // (a part without columns)
+            else if (!*reinterpret_cast<volatile int*>(&s_abort)) {
+              sm100::mbar_expect_tx(bar, (uint32_t)m * 16u);
+              asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                           ::"r"(sm100::smem_u32(smem) + (uint32_t)(stage * kChunk) * 16u), "l"(lv + v0), "r"((uint32_t)m * 16u), "r"(bar) : "memory");
+            }
+          }
+          __syncwarp();
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+    }
+    // (the block's shared memory outlives the copies: the columns' warps wait for each of them)
+  }
+}
+
 // Grid: rows x blocks of a cluster.  HOLD: the share stays in shared memory (behind the teacher's entries).
 template <typename T, bool GRAD, bool HOLD>
 __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
@@ -295,7 +594,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
       const int i = (g * kFold + u) * threads + tid;
       v[u] = v0 + i < full ? (HOLD ? hold[i] : lv[v0 + i]) : make_uint4(none, none, none, none);
     }
-    f.raise(max_of<T, kFold>(v), a.c);
+    f.raise(max_of<T>(v), a.c);
 #pragma unroll
     for (int u = 0; u < kFold; ++u) {
       if (v0 + (g * kFold + u) * threads + tid < full) { float x[kN]; unpack<T>(v[u], x); f.add(x, a.c); }
@@ -437,9 +736,38 @@ cudaError_t launch_loss_typed(const DistillArgs& a, int N, int G, int threads, s
   return cudaLaunchKernelEx(&lc, kern, a);
 }
 
+template <typename T, bool GRAD>
+cudaError_t launch_stream(const DistillArgs& a, int N, int log_g, cudaStream_t s) {
+  auto kern = k_distill_stream<T, GRAD>;
+  constexpr int smem = kStages * kChunk * 16;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  const long long most = kStreamSlots >> log_g;            // clusters
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)((N < most ? N : most) << log_g));
+  lc.blockDim = dim3(kStreamThreads + 64);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 1u << log_g; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = at; lc.numAttrs = 2;
+  return cudaLaunchKernelEx(&lc, kern, a, N, log_g);
+}
+
 template <typename T>
 cudaError_t launch_loss(const DistillArgs& a, int N, cudaStream_t s) {
   const size_t row = (size_t)a.cols * sizeof(T);
+  if (a.K <= kStreamK && row >= kStreamRow && N >= kStreamSlots) {
+    // blocks per row: so many that the rows in work stay in L2, and more where the last round would leave much of the machine idle
+    int log_g = 0;
+    if (a.grad) while (log_g < 3 && row * (kStreamSlots >> log_g) > kLiveBytes) ++log_g;
+    auto rounds = [&](int l) { const long long m = kStreamSlots >> l; return (double)((N + m - 1) / m) / (1 << l); };
+    for (int l = log_g + 1; l <= 3; ++l) if (rounds(l) < 0.9 * rounds(log_g)) log_g = l;
+    return a.grad ? launch_stream<T, true>(a, N, log_g, s) : launch_stream<T, false>(a, N, log_g, s);
+  }
   // Blocks per row: so many that a block's share leaves room for three on an SM, and more while all rows together do not
   // occupy the machine's SMs
   int G = 1;

@@ -59,8 +59,9 @@ def bounds(l, ids, t, T, w, dt, want_grad):
     return b_loss, b_lse, k * (b_q + b_p) * 1.01 + 3 * u * np.abs(want_grad) + HALF[dt] * np.abs(want_grad) + k * 2.0 ** -126
 
 
-def check(logits, n_cols, ids, t, T, w, cols=None, ld=None, in_place=False):
-    """All forms of the call on one batch.  logits: fp32 / bf16 host tensor [N, cols]."""
+def check(logits, n_cols, ids, t, T, w, ld=None, in_place=False, rows=None):
+    """All forms of the call on one batch, held against the oracle row by row (`rows`: in these).  logits: fp32 / bf16 host
+    tensor [N, cols]."""
     N, cols = logits.shape
     dt = logits.dtype
     ld = ld or cols
@@ -83,7 +84,7 @@ def check(logits, n_cols, ids, t, T, w, cols=None, ld=None, in_place=False):
         assert (g[:, cols:] == 9.0).all()                    # what lies between the rows is not touched
     assert (buf[:, cols:] == 777.0).all()
     L = f64(logits)
-    for r in range(N):
+    for r in range(N) if rows is None else rows:
         C = cols if n_cols is None else min(max(int(n_cols[r]), 0), cols)
         l = L[r, :C]
         ii = np.zeros(0, np.int64) if ids is None else ids[r].astype(np.int64)
@@ -208,6 +209,28 @@ def test_distill_edges(dt, cols):
     w[8] = -0.5
     check(l, n, ids, t, 1.0, w, in_place=True)
     check(l, n, ids, t, 2.5, w, ld=cols + 1)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,cols,K", [(300, 9001, 5), (301, 20483, 127), (350, 33000, 128), (297, 40001, 0), (160, 65537, 33), (80, 140000, 64), (75, 262147, 3)])
+def test_distill_of_many_rows(dt, N, cols, K):
+    # more rows than the blocks take at once: rows of every length, among them such without columns, without a
+    # teacher, with a weight of zero and with NaN, next to ordinary ones
+    rng = np.random.default_rng(N + cols)
+    l = (torch.from_numpy(rng.standard_normal((N, cols)).astype(np.float32)) * 2).to(dt)
+    ids = rng.integers(0, cols, (N, K)) if K else None
+    t = (rng.standard_normal((N, K)) * 2 + 5).astype(np.float32) if K else None
+    n = [cols - int(x) for x in rng.integers(0, cols // 2, N)]
+    n[3], n[4], n[9], n[N - 1] = 0, cols, 1, 7
+    w = rng.random(N).astype(np.float32) + 0.1
+    w[5], w[20] = 0.0, -1.0
+    l[6, 1] = np.nan
+    l[7] = -np.inf
+    if K:
+        ids[8] = -1
+        ids[10, :] = ids[10, 0]
+    rows = [0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 20, 36, 37, 73, 74, N // 2, N - 2, N - 1]
+    check(l, n, ids, t, 1.3, w, ld=cols + (cols % 3), in_place=True, rows=rows)
 
 
 def test_distill_without_a_teacher_list():
