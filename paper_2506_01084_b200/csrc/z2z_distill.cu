@@ -234,11 +234,11 @@ __device__ __forceinline__ void copy_wait(int left) {
 // read missed L2.  Holding the rows in the shared memory of clusters of four: a fourth of every row's time went into its
 // barrier, and clusters of four leave a seventh of the SMs without work: 291 us for 2048 bf16 rows of 132352 columns.)
 // One thread fills a ring of kStages chunks by bulk copies and runs on from the first pass into the second and from there into
-// the next row.  Thirty warps have the columns; one more has, a row ahead, the teacher, the columns outside the
+// the next row.  Fifteen warps have the columns, eight vectors of a chunk each; one more has, a row ahead, the teacher, the columns outside the
 // vectors and the loss, and, behind the barrier of the following row, the teacher's columns of the gradient.
-constexpr int kStreamWarps = 30, kStreamThreads = 32 * kStreamWarps, kStreamK = 256, kStages = 3;
+constexpr int kStreamWarps = 15, kStreamThreads = 32 * kStreamWarps, kStreamFold = 8, kStreamK = 256, kStages = 3;
 constexpr int kPairs = kStreamWarps + 1;                   // warps that meet in a row's exchange
-constexpr int kChunk = kFold * kStreamThreads;             // vectors of a chunk, at most
+constexpr int kChunk = kStreamFold * kStreamThreads;       // vectors of a chunk, at most
 constexpr size_t kLiveBytes = (size_t)40 << 20;
 
 struct alignas(16) StreamTeacher { int id[kStreamK]; float p[kStreamK], x[kStreamK]; float ref, lg; int some, c0, c1; };
@@ -276,9 +276,6 @@ template <typename T> __device__ __forceinline__ void put_teacher(const DistillA
 
 // A block's part of a row: vectors [v0, v1), up to `full` columns of the row; columns [c0, c1) in all.
 template <typename T> struct RowPart { const T* l; int head, v0, v1, full, c0, c1; };
-
-// Chunks of a part of n vectors: as many as it takes, all of about the same size, at least one.
-__device__ __forceinline__ int chunks_of(int n) { return n <= kChunk ? 1 : (n + kChunk - 1) / kChunk; }
 
 template <typename T, bool GRAD>
 __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(DistillArgs a, int N, int log_g) {
@@ -355,31 +352,37 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
     const uint4* const ring = reinterpret_cast<const uint4*>(smem) + tid;
     const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;                   // -inf
     int stage = 0, phase = 0;
-    // this thread's vectors of the next chunk, of which the block has n; what lies behind them is -inf
-    auto take = [&](uint4 (&v)[kFold], int n) {
+    // This thread's vectors of the next chunk, of which the block has m.  A whole chunk is worked on without a condition;
+    // what lies behind a part of one is -inf.
+    using Vecs = uint4[kStreamFold];
+    auto take = [&](auto whole, Vecs& v, int m) {
       wait(&s_full[stage], phase);
       const uint4* from = ring + stage * kChunk;
 #pragma unroll
-      for (int u = 0; u < kFold; ++u) v[u] = u * kStreamThreads + tid < n ? from[u * kStreamThreads] : make_uint4(none, none, none, none);
+      for (int u = 0; u < kStreamFold; ++u)
+        v[u] = decltype(whole)::value || u * kStreamThreads + tid < m ? from[u * kStreamThreads] : make_uint4(none, none, none, none);
       __syncwarp();
       if (lane == 0) sm100::mbar_arrive(sm100::smem_u32(&s_empty[stage]));
       if (++stage == kStages) { stage = 0; phase ^= 1; }
     };
+    auto has = [&](auto whole, int u, int m) { return decltype(whole)::value || u * kStreamThreads + warp * 32 < m; };       // any of the warp
     int C1 = cols_of(1);
     RowPart<T> q = part_of(0, cols_of(0));
     for (int i = 0; i < rows; ++i) {
-      const int r = row_at(i), n = q.full - q.v0, chunks = chunks_of(n), per = (n + chunks - 1) / chunks;
+      const int r = row_at(i), n = q.full - q.v0;
       const float w = GRAD && a.weight ? a.weight[r] : 1.f;
       Fold f;
-      for (int v0 = 0, c = 0; c < chunks; ++c, v0 += per) {
-        uint4 v[kFold];
-        const int m = min(per, n - v0);
-        take(v, m);
+      auto fold = [&](auto whole, int m) {
+        Vecs v;
+        take(whole, v, m);
         f.raise(max_of<T>(v), a.c);
 #pragma unroll
-        for (int u = 0; u < kFold; ++u)
-          if (u * kStreamThreads + warp * 32 < m) { float x[kN]; unpack<T>(v[u], x); f.add(x, a.c); }
-      }
+        for (int u = 0; u < kStreamFold; ++u)
+          if (has(whole, u, m)) { float x[kN]; unpack<T>(v[u], x); f.add(x, a.c); }
+      };
+      int v0 = 0;
+      for (; v0 + kChunk <= n; v0 += kChunk) fold(std::true_type(), kChunk);
+      if (v0 < n || n == 0) fold(std::false_type(), n - v0);                   // (a part without columns has a chunk, too)
       f = exchange(i, f);
       if (GRAD) {
         const bool zero = !s_teacher[i & 1].some || f.s == 0.f || w == 0.f;
@@ -396,29 +399,34 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
 #pragma unroll
           for (int u = 0; u < kN; ++u) out[(q.v0 + v) * kN + u] = e[u];
         };
-        for (int v0 = 0, c = 0; c < chunks; ++c, v0 += per) {
-          uint4 v[kFold];
-          const int m = min(per, n - v0);
-          take(v, m);
+        auto columns = [&](auto whole, auto scaled, int m) {
+          Vecs v;
+          take(whole, v, m);
 #pragma unroll
-          for (int u = 0; u < kFold; ++u) {
-            if (u * kStreamThreads + warp * 32 >= m) break;
+          for (int u = 0; u < kStreamFold; ++u) {
+            if (!has(whole, u, m)) break;
             float x[kN];
             unpack<T>(v[u], x);
-            if (zero) {
 #pragma unroll
-              for (int e = 0; e < kN; ++e) x[e] = 0.f;
-            } else {
+            for (int e = 0; e < kN; ++e) { x[e] = ex2(fmaf(x[e], a.c, -off)); if (decltype(scaled)::value) x[e] *= kq; }
+            if (!decltype(whole)::value) {
+              if (zero) {
 #pragma unroll
-              for (int e = 0; e < kN; ++e) x[e] = ex2(fmaf(x[e], a.c, -off));
-              if (!in_exponent) {
-#pragma unroll
-                for (int e = 0; e < kN; ++e) x[e] *= kq;
+                for (int e = 0; e < kN; ++e) x[e] = 0.f;
               }
+              if (u * kStreamThreads + tid < m) put(v0 + u * kStreamThreads + tid, packed<T>(x));
+            } else {
+              __stcs(ov + v0 + u * kStreamThreads + tid, packed<T>(x));
             }
-            if (u * kStreamThreads + tid < m) put(v0 + u * kStreamThreads + tid, packed<T>(x));
           }
+        };
+        v0 = 0;
+        const bool plain = !zero && !a.grad_skew;          // (rows of zeros, and gradients aligned otherwise, take the chunks in part)
+        for (; plain && v0 + kChunk <= n; v0 += kChunk) {
+          if (in_exponent) columns(std::true_type(), std::integral_constant<bool, sizeof(T) == 4>(), kChunk);
+          else columns(std::true_type(), std::true_type(), kChunk);
         }
+        for (; v0 < n || (n == 0 && v0 == 0); v0 += kChunk) columns(std::false_type(), std::true_type(), min(kChunk, n - v0));
         for (int v = max(n, 0) + tid; v < q.v1 - q.v0; v += kStreamThreads) if (q.v0 + v != q.full) put(v, make_uint4(0u, 0u, 0u, 0u));
       }
       if (i + 1 < rows) { q = part_of(i + 1, C1); C1 = cols_of(i + 2); }
@@ -501,11 +509,11 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
       const RowPart<T> q = part_of(i, C1);
       C1 = cols_of(i + 1);
       const uint4* lv = reinterpret_cast<const uint4*>(q.l + q.head) + q.v0;
-      const int n = q.full - q.v0, chunks = chunks_of(n), per = (n + chunks - 1) / chunks;
+      const int n = q.full - q.v0;
       for (int pass = 0; pass < (GRAD ? 2 : 1); ++pass)
-        for (int v0 = 0, c = 0; c < chunks; ++c, v0 += per) {
+        for (int v0 = 0; v0 < n || (n == 0 && v0 == 0); v0 += kChunk) {
           wait(&s_empty[stage], phase);
-          const int m = min(per, n - v0);
+          const int m = min(kChunk, n - v0);
           if (lane == 0) {
             const uint32_t bar = sm100::smem_u32(&s_full[stage]);
             if (m <= 0) sm100::mbar_arrive(bar);           // (a part without columns)
