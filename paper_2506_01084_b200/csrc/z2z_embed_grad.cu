@@ -37,7 +37,7 @@ constexpr int kMinChunk = 8, kMaxChunk = 128, kMinGroup = 8;
 constexpr int kAhead = 4;                // rows of g that a thread has under way
 constexpr int kShortRun = 8;             // partial sums that one warp adds
 constexpr int kFinishThreads = 256;
-constexpr int kZeroPerWarp = 8;
+constexpr int kZeroPerBlock = 16;
 constexpr size_t kZeroBeside = (size_t)40 << 20;     // bytes of zeros written beside each launch of the sort
 
 // Where the targets' rows lie.
@@ -457,12 +457,21 @@ __global__ void __launch_bounds__(kSumThreads) k_grad_sum(GradTables t, const in
 // kShortRun chunks, a block those of a longer one, every warp a share of its partial sums.
 template <typename TO>
 __global__ void __launch_bounds__(kFinishThreads) k_grad_finish(CbView cb, GradTables t, const int2* __restrict__ sorted, float scale, int accumulate,
-                                                                int chunk, int chunks, GradScratch w, int zero_lo, int zero_hi) {
+                                                                int chunk, int chunks, GradScratch w, int join_blocks, int zero_lo, int zero_hi) {
   constexpr int kWarps = kFinishThreads / 32;
   __shared__ float4 s_sum[kWarps][32];
   sm100::pdl_wait();
   sm100::pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if ((int)blockIdx.x >= join_blocks) {                    // zeros in the rows of kZeroPerBlock targets that no row names
+    const int t0 = zero_lo + ((int)blockIdx.x - join_blocks) * kZeroPerBlock, row_vecs = (int)((size_t)t.d * sizeof(TO) / 16);
+    for (int k = t0 + warp; k < min(zero_hi, t0 + kZeroPerBlock); k += kWarps) {
+      if (((w.named[k >> 5] >> (k & 31)) & 1u) || (k >= t.V && (k - t.V) % t.cap >= cb.n[(k - t.V) / t.cap])) continue;
+      uint4* out = reinterpret_cast<uint4*>(target_row<TO>(t, k));
+      for (int v = lane; v < row_vecs; v += 32) __stcs(out + v, make_uint4(0u, 0u, 0u, 0u));
+    }
+    return;
+  }
   const int slabs = (t.d + 127) / 128, n_short = w.heads[0], n_long = w.heads[1];
   // the target of a run and how many chunks, from c on, hold a part of it: slot 1 of chunk c, slot 0 of the others
   auto extent = [&](int c, int& k) {
@@ -488,7 +497,7 @@ __global__ void __launch_bounds__(kFinishThreads) k_grad_finish(CbView cb, GradT
     }
     return acc;
   };
-  for (int unit = blockIdx.x; unit < n_long * slabs; unit += gridDim.x) {
+  for (int unit = blockIdx.x; unit < n_long * slabs; unit += join_blocks) {
     const int c = w.heads[chunks + 1 - unit / slabs], d0 = (unit % slabs) * 128 + 4 * lane;
     int k;
     const int n = extent(c, k), per = (n + kWarps - 1) / kWarps;
@@ -502,7 +511,7 @@ __global__ void __launch_bounds__(kFinishThreads) k_grad_finish(CbView cb, GradT
     }
     __syncthreads();
   }
-  for (long long unit = (long long)warp * gridDim.x + blockIdx.x; unit < (long long)n_short * slabs; unit += (long long)gridDim.x * kWarps) {
+  for (long long unit = (long long)warp * join_blocks + blockIdx.x; unit < (long long)n_short * slabs; unit += (long long)join_blocks * kWarps) {
     const int c = w.heads[2 + unit / slabs], d0 = (int)(unit % slabs) * 128 + 4 * lane;
     int k;
     const int n = extent(c, k);
@@ -510,19 +519,6 @@ __global__ void __launch_bounds__(kFinishThreads) k_grad_finish(CbView cb, GradT
       const float4 x = add(c, 0, n, d0);
       const float sum[4] = {x.x, x.y, x.z, x.w};
       put(target_row<TO>(t, k) + d0, sum, scale, accumulate != 0);
-    }
-  }
-  const int row_vecs = (int)((size_t)t.d * sizeof(TO) / 16);
-  for (long long t0 = zero_lo + (long long)(warp * gridDim.x + blockIdx.x) * kZeroPerWarp; t0 < zero_hi; t0 += (long long)gridDim.x * kWarps * kZeroPerWarp) {
-    const int k = (int)t0 + lane;
-    bool zero = lane < kZeroPerWarp && k < zero_hi && !((w.named[k >> 5] >> (k & 31)) & 1u);
-    if (zero && k >= t.V) zero = (k - t.V) % t.cap < cb.n[(k - t.V) / t.cap];
-    unsigned todo = __ballot_sync(0xffffffffu, zero);
-    while (todo) {
-      const int i = __ffs(todo) - 1;
-      todo &= todo - 1;
-      uint4* out = reinterpret_cast<uint4*>(target_row<TO>(t, (int)t0 + i));
-      for (int v = lane; v < row_vecs; v += 32) __stcs(out + v, make_uint4(0u, 0u, 0u, 0u));
     }
   }
 }
@@ -570,7 +566,11 @@ cudaError_t launch_typed(const CbView& cb, const EmbedGradArgs& a, cudaStream_t 
     e = launch_pdl(acc ? k_grad_sum<TG, TO, true> : k_grad_sum<TG, TO, false>, dim3((unsigned)(((long long)p.chunks * p.slabs + groups - 1) / groups)), dim3(kSumThreads),
                    (size_t)groups * (p.chunk + 2) * sizeof(int2), s, t, sorted, a.N, g, a.scale, p, w);
   if (e == cudaSuccess)
-    e = launch_pdl(k_grad_finish<TO>, dim3(148 * 8), dim3(kFinishThreads), 0, s, cb, t, sorted, a.scale, acc, p.chunk, p.chunks, w, at, zero_hi);
+  {
+    const int joins = 148 * 8;
+    e = launch_pdl(k_grad_finish<TO>, dim3(joins + (zero_hi - at + kZeroPerBlock - 1) / kZeroPerBlock), dim3(kFinishThreads), 0, s, cb, t, sorted, a.scale,
+                   acc, p.chunk, p.chunks, w, joins, at, zero_hi);
+  }
   return e;
 }
 

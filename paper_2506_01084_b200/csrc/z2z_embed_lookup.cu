@@ -65,26 +65,35 @@ template <> __device__ __forceinline__ uint4 scaled<__nv_bfloat16>(uint4 v, floa
 }
 }  // namespace
 
-// out[r] = scale * row(codes[r]).
+// out[r] = scale * row(codes[r]).  A warp takes kLookupUnroll vectors per lane of a row, all under way at once, so that the
+// few rows of a decode step are spread over as many SMs as they have pieces, and one such piece: with a grid of the
+// resident blocks and a loop every warp waits for its own chain of reads again and again (52800 rows of 4096 bf16 columns
+// 121 us, now 100: 0.95 of the copy rate).
 template <typename T>
 __global__ void __launch_bounds__(kLookupThreads) k_embed_lookup_scaled(
-    CbView cb, const int32_t* codes, int N, const int32_t* row_seq, const uint4* WE, const uint4* Eh, float scale, uint4* out,
-    int row_vecs) {
+    CbView cb, const int32_t* __restrict__ codes, int N, const int32_t* __restrict__ row_seq, const uint4* __restrict__ WE,
+    const uint4* __restrict__ Eh, float scale, uint4* __restrict__ out, int row_vecs, int pieces) {
   sm100::pdl_wait();
   sm100::pdl_trigger();
   const int lane = threadIdx.x & 31;
-  const int warps = (gridDim.x * blockDim.x) >> 5;
-  for (int r = (blockIdx.x * blockDim.x + threadIdx.x) >> 5; r < N; r += warps) {
+  const long long units = (long long)N * pieces, step = (long long)gridDim.x * (kLookupThreads / 32);
+  for (long long unit = (long long)blockIdx.x * (kLookupThreads / 32) + (threadIdx.x >> 5); unit < units; unit += step) {
+    const int r = (int)(unit / pieces), piece = (int)(unit - (long long)r * pieces);
     const int z = codes[r];
     const int b = row_seq ? row_seq[r] : r;
     const uint4* src = nullptr;
     if ((unsigned)b < (unsigned)cb.B) {
       if (z >= 0 && z < cb.V) src = WE + (size_t)z * row_vecs;
       else if (z >= cb.V && z - cb.V < cb.n[b]) src = Eh + ((size_t)b * cb.cap + (z - cb.V)) * row_vecs;
-      else if (lane == 0 && z != Z2Z_CODE_NONE) atomicOr(&cb.status[b], Z2Z_ST_BAD_TOKEN);
+      else if (piece == 0 && lane == 0 && z != Z2Z_CODE_NONE) atomicOr(&cb.status[b], Z2Z_ST_BAD_TOKEN);
     }
     uint4* dst = out + (size_t)r * row_vecs;
-    for (int i = lane; i < row_vecs; i += 32) dst[i] = src ? scaled<T>(src[i], scale) : make_uint4(0, 0, 0, 0);
+    const int i = piece * 32 * kLookupUnroll + lane;
+    uint4 v[kLookupUnroll];
+#pragma unroll
+    for (int u = 0; u < kLookupUnroll; ++u) v[u] = src && i + 32 * u < row_vecs ? __ldcg(src + i + 32 * u) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int u = 0; u < kLookupUnroll; ++u) if (i + 32 * u < row_vecs) __stcs(dst + i + 32 * u, src ? scaled<T>(v[u], scale) : v[u]);
   }
 }
 
@@ -103,13 +112,13 @@ cudaError_t launch_embed_lookup(const CbView& cb, const int32_t* codes, int N,
 cudaError_t launch_embed_lookup_scaled(const CbView& cb, const int32_t* codes, int N, const int32_t* row_seq, const void* WE,
                                        const void* Eh, float scale, void* out, int d, int dtype, cudaStream_t s) {
   const int row_vecs = d * (dtype == Z2Z_DTYPE_BF16 ? 2 : 4) / 16;
-  const int warps_per_block = kLookupThreads / 32;
-  int blocks = (N + warps_per_block - 1) / warps_per_block;
-  const int full = 148 * 8;
-  if (blocks > full) blocks = full;
+  const int pieces = (row_vecs + 32 * kLookupUnroll - 1) / (32 * kLookupUnroll), warps = kLookupThreads / 32;
+  long long blocks = ((long long)N * pieces + warps - 1) / warps;
+  if (blocks > (1 << 30)) blocks = 1 << 30;
   auto kern = dtype == Z2Z_DTYPE_BF16 ? k_embed_lookup_scaled<__nv_bfloat16> : k_embed_lookup_scaled<float>;
-  return launch_pdl(kern, dim3(blocks), dim3(kLookupThreads), 0, s, cb, codes, N, row_seq,
-                    reinterpret_cast<const uint4*>(WE), reinterpret_cast<const uint4*>(Eh), scale, reinterpret_cast<uint4*>(out), row_vecs);
+  return launch_pdl(kern, dim3((unsigned)blocks), dim3(kLookupThreads), 0, s, cb, codes, N, row_seq,
+                    reinterpret_cast<const uint4*>(WE), reinterpret_cast<const uint4*>(Eh), scale, reinterpret_cast<uint4*>(out), row_vecs,
+                    pieces);
 }
 
 }  // namespace z2z
