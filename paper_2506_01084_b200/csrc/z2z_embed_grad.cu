@@ -7,7 +7,9 @@
 // their rows, so that the result does not depend on which block ran first.  No atomics touch a gradient.
 //
 //   k_grad_small   up to kSmallRows rows: one launch, no sort.  Every block holds all targets in shared memory; the block of
-//                  a target's first row finds the others and adds them up.
+//                  a target's first row finds the others and adds them up.  (1000 rows of 512 bf16 columns 11 us, through
+//                  the launches below 16; at 1500 rows either takes 17.  A single target for all rows is the worst case, 1024
+//                  rows one after the other.)
 //   k_grad_keys, k_grad_scatter (x passes), k_grad_sum, k_grad_finish otherwise:
 //     * the sort has digits of 9 bits (two passes up to 2^18 targets) over at most kTiles tiles.  A pass is one
 //       launch: every block sums the tiles' digit counts itself (a table of 2 KB per tile, from L2) instead of waiting
@@ -27,7 +29,7 @@ namespace z2z {
 
 namespace {
 
-constexpr int kSmallRows = 512;
+constexpr int kSmallRows = 1024;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits, kMaxPasses = 3;
 constexpr int kTiles = 148;              // at most one block per SM and pass
 constexpr int kTileRows = 1024;          // and at least so many rows for each
@@ -55,6 +57,17 @@ __device__ __forceinline__ int target_of(const CbView& cb, const GradTables& t, 
   if (z >= cb.V && z - cb.V < cb.n[b]) return t.gEh ? cb.V + b * cb.cap + (z - cb.V) : t.total;
   *bad = z != Z2Z_CODE_NONE;
   return t.total;
+}
+
+// Lanes with the same digit as this one's (among those that have one): a vote per bit.
+__device__ __forceinline__ unsigned same_digit(int dgt) {
+  unsigned peers = __ballot_sync(0xffffffffu, dgt >= 0);
+#pragma unroll
+  for (int b = 0; b < kDigitBits; ++b) {
+    const unsigned m = __ballot_sync(0xffffffffu, (dgt >> b) & 1);
+    peers &= (dgt >> b) & 1 ? m : ~m;
+  }
+  return peers;
 }
 
 // 16 bytes of a row of g as fp32, and that many columns of a table's row.
@@ -357,7 +370,7 @@ __global__ void __launch_bounds__(kSortThreads) k_grad_scatter(CbView cb, GradTa
   // the warps' digits are counted, then placed, in order
   auto count = [&](int2 e) {
     const int dgt = e.x >= 0 ? (e.x >> shift) & (kDigits - 1) : -1;
-    const unsigned peers = __match_any_sync(0xffffffffu, dgt);
+    const unsigned peers = same_digit(dgt);
     if (dgt >= 0 && (__ffs(peers) - 1) == lane) s_base[warp][dgt] += __popc(peers);
     __syncwarp();
   };
@@ -370,7 +383,7 @@ __global__ void __launch_bounds__(kSortThreads) k_grad_scatter(CbView cb, GradTa
   __syncthreads();
   auto place = [&](int2 e) {
     const int dgt = e.x >= 0 ? (e.x >> shift) & (kDigits - 1) : -1;
-    const unsigned peers = __match_any_sync(0xffffffffu, dgt);
+    const unsigned peers = same_digit(dgt);
     int at = 0;
     if (dgt >= 0) at = s_base[warp][dgt] + __popc(peers & ((1u << lane) - 1u));
     __syncwarp();
