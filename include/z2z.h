@@ -292,7 +292,7 @@ int32_t z2z_embed_grad(z2z_codebook* cb, const int32_t* d_codes, int32_t N, cons
  *   d_teacher_ids, d_teacher_logits [N, K]: the teacher's columns and its logits for them, in any
  *            order, 0 <= K <= 1024.  An id outside the row's columns (Z2Z_CODE_NONE for shorter lists) is
  *            left out, a logit of -inf has no probability, and what the same column is given twice adds up;
- *   temperature > 0, finite;
+ *   temperature > 0, finite; logits / temperature stay within fp32's range;
  *   d_loss [N] out, d_lse [N] out: log sum_c exp(l_c / T).
  * A row without columns, or masked throughout (nothing but -inf or values at or below -2^126, such as the
  * lowest of the type: lse = -inf), and a row that is left no teacher entry, has loss 0 and gradient 0.
@@ -302,6 +302,7 @@ int32_t z2z_embed_grad(z2z_codebook* cb, const int32_t* d_codes, int32_t N, cons
  * z2z_distill_grad is the backward pass on its own: d_grad_loss [N] is the derivative for d_loss, d_lse what
  * z2z_distill_loss left there for the same arguments (rows of -inf are not read again; the normaliser of the
  * others is found anew, since lse has lost 2^-24 of its size, and every probability with it).
+ * (A wait inside the kernels that gives up leaves NaN in the row's d_loss and d_lse.)
  *   d_grad [N, cols] of dtype, rows ld apart: every column is written, 0 from n_cols on.  A row whose
  *            weight is 0 has gradient 0 whatever its logits are.  d_grad == d_logits is allowed (the
  *            logits are then overwritten); they must not overlap in another way.                   */
@@ -333,7 +334,9 @@ int32_t z2z_distill_grad(const void* d_logits, int32_t dtype, int32_t N, int32_t
  *   d_code [B] out: its new code, Z2Z_CODE_NONE for a finished or dead one;
  *   d_next_scores [B] out (-inf in a dead slot); d_next_finished [B] out or NULL (1 also for a dead slot);
  *   d_active [B] out or NULL: 1 where d_code is a code (z2z_lzw_step's d_active).
- * d_next_scores may be d_scores and d_next_finished may be d_finished; the outputs overlap nothing else.   */
+ * d_next_scores may be d_scores and d_next_finished may be d_finished; the outputs overlap nothing else.
+ * The call keeps its lists in the session's workspace: like all calls of a session it is ordered behind the
+ * others by the caller.                                                                               */
 int32_t z2z_beam_select(z2z_codebook* cb, int32_t beams, const float* d_logits, const float* d_lse,
                         const float* d_scores, const uint8_t* d_finished, int32_t eos, int32_t* d_parent,
                         int32_t* d_code, float* d_next_scores, uint8_t* d_next_finished, uint8_t* d_active,

@@ -42,9 +42,16 @@ struct DistillArgs {
   float inv_t, temperature, c;  // c = log2(e) / T
   const float* weight;          // row weights (gradient), or NULL = 1
   float* loss; float* lse;      // out, or NULL
+  const float* old_lse;         // or NULL: rows of -inf here have nothing visible
   void* grad;                   // or NULL
   int grad_skew;                // the gradient's rows are not aligned to 16 bytes where the logits' are
 };
+
+__device__ __forceinline__ int visible_cols(const DistillArgs& a, int r) {
+  const int c = a.n_cols ? a.n_cols[r] : a.cols;
+  if (a.old_lse && a.old_lse[r] == -INFINITY) return 0;
+  return c < 0 ? 0 : (c > a.cols ? a.cols : c);
+}
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -294,11 +301,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
   const int rows = r0 < N ? (N - r0 + clusters - 1) / clusters : 0;
   const int tid = threadIdx.x, lane = tid & 31, warp = sm100::uniform_warp();
   auto row_at = [&](int i) { return r0 + i * clusters; };
-  auto cols_of = [&](int i) {
-    if (i >= rows) return 0;
-    const int c = a.n_cols ? a.n_cols[row_at(i)] : a.cols;
-    return c < 0 ? 0 : (c > a.cols ? a.cols : c);
-  };
+  auto cols_of = [&](int i) { return i < rows ? visible_cols(a, row_at(i)) : 0; };
   auto part_of = [&](int i, int C) {
     RowPart<T> q;
     q.l = reinterpret_cast<const T*>(a.logits) + (size_t)row_at(i) * a.ld;
@@ -546,8 +549,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   if (G > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");       // (waited for before the first remote store)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   const T* l = reinterpret_cast<const T*>(a.logits) + (size_t)r * a.ld;
-  int C = a.n_cols ? a.n_cols[r] : a.cols;
-  C = C < 0 ? 0 : (C > a.cols ? a.cols : C);
+  const int C = visible_cols(a, r);
   const RowSplit sp = split_row(l, a.cols);
   const int share = (sp.vecs + G - 1) / G, v0 = min(sp.vecs, rank * share), v1 = min(sp.vecs, v0 + share);
   const uint4* lv = reinterpret_cast<const uint4*>(l + sp.head);
@@ -750,9 +752,8 @@ cudaError_t launch_stream(const DistillArgs& a, int N, int log_g, cudaStream_t s
   constexpr int smem = kStages * kChunk * 16;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  const long long most = kStreamSlots >> log_g;            // clusters
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3((unsigned)((N < most ? N : most) << log_g));
+  lc.gridDim = dim3(1u << log_g);
   lc.blockDim = dim3(kStreamThreads + 64);
   lc.dynamicSmemBytes = smem;
   lc.stream = s;
@@ -761,7 +762,16 @@ cudaError_t launch_stream(const DistillArgs& a, int N, int log_g, cudaStream_t s
   at[0].val.clusterDim.x = 1u << log_g; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
   at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[1].val.programmaticStreamSerializationAllowed = 1;
-  lc.attrs = at; lc.numAttrs = 2;
+  lc.attrs = at; lc.numAttrs = 1;
+  // clusters that are resident at one time (those of four and eight leave the rest of a GPC without one)
+  static int fit[4] = {0, 0, 0, 0};
+  int most = kStreamSlots >> log_g;
+  if (log_g > 1) {
+    if (!fit[log_g] && (e = cudaOccupancyMaxActiveClusters(&fit[log_g], kern, &lc)) != cudaSuccess) return e;
+    if (fit[log_g] >= 1 && fit[log_g] < most) most = fit[log_g];
+  }
+  lc.gridDim = dim3((unsigned)((N < most ? N : most) << log_g));
+  lc.numAttrs = 2;
   return cudaLaunchKernelEx(&lc, kern, a, N, log_g);
 }
 
@@ -790,10 +800,10 @@ cudaError_t launch_loss(const DistillArgs& a, int N, cudaStream_t s) {
 }
 
 DistillArgs distill_args(const void* logits, int cols, int64_t ld, const int32_t* n_cols, const int32_t* ids, const float* t, int K, float temperature,
-                         const float* weight, float* loss, float* lse, void* grad) {
+                         const float* weight, float* loss, float* lse, const float* old_lse, void* grad) {
   const int skew = grad && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(logits)) & 15) ? 1 : 0;
   return DistillArgs{logits, cols, ld, n_cols, ids, t, K, 1.f / temperature, temperature, (float)(1.4426950408889634 / (double)temperature),
-                     weight, loss, lse, grad, skew};
+                     weight, loss, lse, old_lse, grad, skew};
 }
 }  // namespace
 
@@ -810,7 +820,7 @@ int32_t z2z_distill_loss(const void* d_logits, int32_t dtype, int32_t N, int32_t
   if (rc || N == 0) return rc;
   if (!d_loss || !d_lse) return z2z::fail_arg("d_loss / d_lse is NULL");
   const z2z::DistillArgs a = z2z::distill_args(d_logits, cols, ld, d_n_cols, d_teacher_ids, d_teacher_logits, K, temperature, d_row_weight, d_loss,
-                                               d_lse, d_grad);
+                                               d_lse, nullptr, d_grad);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   return z2z::done(dtype == Z2Z_DTYPE_BF16 ? z2z::launch_loss<__nv_bfloat16>(a, N, s) : z2z::launch_loss<float>(a, N, s));
 }
@@ -823,7 +833,7 @@ int32_t z2z_distill_grad(const void* d_logits, int32_t dtype, int32_t N, int32_t
   if (rc || N == 0) return rc;
   if (!d_lse || !d_grad_loss || !d_grad) return z2z::fail_arg("d_lse / d_grad_loss / d_grad is NULL");
   const z2z::DistillArgs a = z2z::distill_args(d_logits, cols, ld, d_n_cols, d_teacher_ids, d_teacher_logits, K, temperature, d_grad_loss, nullptr,
-                                               nullptr, d_grad);
+                                               nullptr, d_lse, d_grad);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   return z2z::done(dtype == Z2Z_DTYPE_BF16 ? z2z::launch_loss<__nv_bfloat16>(a, N, s) : z2z::launch_loss<float>(a, N, s));
 }

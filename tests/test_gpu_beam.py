@@ -104,6 +104,51 @@ def test_beam_select_of_masked_infinite_and_missing_values():
     run_select(cb, beams, l, n, lse, scores, fin, 4)
 
 
+@pytest.mark.parametrize("V", [1, 2, 3, 7])
+@pytest.mark.parametrize("beams", [1, 5, 32])
+def test_beam_select_with_fewer_columns_than_beams(V, beams):
+    rng = np.random.default_rng(V)
+    B = 4 * beams
+    cb = session(V, 8, 0, B, "fp32", [0] * B)
+    for k in range(4):
+        l, lse, scores = inputs(rng, B, V, 0, [0] * B)
+        scores[rng.random(B) < 0.7] = -np.inf                # a few candidates at most: dead slots
+        run_select(cb, beams, l, [0] * B, lse, scores, (rng.random(B) < 0.3).astype(np.uint8) if k else None, 0 if k == 2 else -1)
+
+
+@pytest.mark.parametrize("beams", [3, 32])
+def test_beam_select_when_one_thread_has_the_best_columns(beams):
+    # the best columns 1024 apart: those of one vector of one thread in every tile, far more than the list takes
+    V, cap = 70001, 3
+    rng = np.random.default_rng(beams)
+    cb = session(V, 8, cap, beams, "fp32", [2] * beams)
+    l, lse, scores = inputs(rng, beams, V, cap, [2] * beams)
+    for b in range(beams):
+        for k in range(4):
+            at = np.arange((5 * b) % 1000 + k, V, 1024)
+            l[b, at] = 30 + rng.integers(0, 3, at.size)      # ties among them
+    run_select(cb, beams, l, [2] * beams, lse, scores, None, -1)
+
+
+def test_beam_select_of_many_beams():
+    rng = np.random.default_rng(77)
+    V, cap, beams = 3001, 9, 4
+    B = 1024
+    n = [b % 10 for b in range(B)]
+    cb = session(V, 8, cap, B, "fp32", n)
+    l, lse, scores = inputs(rng, B, V, cap, n)
+    run_select(cb, beams, l, n, lse, scores, (rng.random(B) < 0.2).astype(np.uint8), 3)
+    parent = torch.arange(B, dtype=torch.int32)
+    parent[1::2] = parent[0::2]
+    hist = torch.arange(B, dtype=torch.int32, device=DEV).view(B, 1).clone()
+    E = torch.arange(B, device=DEV).view(B, 1, 1).expand(B, cap, 8).float().contiguous()
+    zb.z2z_beam_reorder(cb, parent.to(DEV), E, E, states=(hist,))
+    nn = zb.z2z_status(cb)[1].tolist()
+    assert nn == [n[p] for p in parent.tolist()] and hist.view(-1).tolist() == parent.tolist()
+    for b in (0, 1, 2, 511, 512, 1023):
+        assert (E[b, :nn[b]] == int(parent[b])).all() and (E[b, nn[b]:] == b).all()
+
+
 def test_beam_select_scores_in_64_bits():
     # sums that fp32 would round to the same value, or in another order
     V, cap, beams = 64, 0, 4

@@ -238,3 +238,49 @@ def test_grad_of_a_large_batch(N):
     g = torch.from_numpy(rng.standard_normal((N, d)).astype(np.float32)).bfloat16().to(DEV)
     check_grad(cb, codes, seq, g, n, V, cap, B, 2.0, torch.float32, False)
     check_grad(cb, codes, seq, g, n, V, cap, B, 2.0, torch.float32, True)
+
+
+@pytest.mark.parametrize("N,V,cap,d", [(3000, 300000, 10, 8), (160001, 1000, 65535, 8), (310001, 200000, 700, 24)])
+def test_grad_of_many_targets_and_rows(N, V, cap, d):
+    # targets beyond 18 bits (three passes of the sort), more rows than a block's registers hold, long chunks
+    rng = np.random.default_rng(N)
+    B = 5
+    n = [min(cap, V - 2), 0, min(cap, 700) // 2, 1, min(cap, 500)]
+    cb = session(V, d, cap, B, "bf16", [min(x, V - 2) for x in n])
+    seq = np.sort(rng.integers(0, B, N)).astype(np.int32)
+    nn = np.array(n)[seq]
+    codes = np.minimum(np.exp(rng.random(N) * np.log(V)), V - 1).astype(np.int64)
+    codes = np.where((rng.random(N) < 0.5) & (nn > 0), V + (rng.random(N) * nn).astype(np.int64), codes)
+    codes[rng.random(N) < 0.02] = -1
+    codes = codes.astype(np.int32)
+    g = torch.from_numpy(rng.standard_normal((N, d)).astype(np.float32)).bfloat16().to(DEV)
+    check_grad(cb, codes, seq, g, n, V, cap, B, 2.0, torch.float32, False)
+    check_grad(cb, codes, seq, g, n, V, cap, B, 0.5, torch.bfloat16, True)
+
+
+def test_grad_on_two_streams_with_scratch_of_their_own():
+    rng = np.random.default_rng(31)
+    V, cap, B, d = 500, 20, 3, 256
+    n = [20, 7, 0]
+    jobs = []
+    for N in (700, 20000):
+        cb = session(V, d, cap, B, "bf16", n)
+        codes, seq = stream(rng, N, V, B, n)
+        g = torch.from_numpy(rng.standard_normal((N, d)).astype(np.float32)).bfloat16().to(DEV)
+        gW, gE = torch.zeros(V, d, device=DEV), torch.zeros(B, cap, d, device=DEV)
+        scratch = torch.empty(zb.z2z_embed_grad_scratch_bytes(cb.cfg, N), dtype=torch.uint8, device=DEV)
+        jobs.append((cb, gpu(codes), gpu(seq), g, 1.0, False, gW, gE, scratch))
+    want = []
+    for j in jobs:
+        zb.z2z_embed_grad(*j)
+        want.append((j[6].clone(), j[7].clone()))
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, j in zip(streams, jobs):
+            with torch.cuda.stream(s):
+                j[6].fill_(3.0)
+                zb.z2z_embed_grad(*j)
+        torch.cuda.synchronize()
+        for j, (a, b) in zip(jobs, want):
+            assert torch.equal(j[6], a) and torch.equal(j[7], b)
