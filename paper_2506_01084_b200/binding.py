@@ -112,16 +112,20 @@ def _dev(t: Optional[torch.Tensor], dtype, numel: int, name: str):
     raise Z2ZError(f"{name} must be a contiguous device tensor of {numel} {dtype}")
 
 
+# Handle of a device's current stream, without the Stream object that the public call makes around it (1 us of a small call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _enqueue(fn, on: torch.Tensor, *args):
     """The call on the current stream of the device that `on` lies on."""
     dev = on.get_device()
     if dev == torch.cuda.current_device():
-        rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+        rc = fn(*args, _raw_stream(dev))
     elif dev < 0:
         raise Z2ZError("device tensors are needed")
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+            rc = fn(*args, _raw_stream(dev))
     if rc:
         _check(rc)
 
