@@ -238,16 +238,17 @@ __device__ __forceinline__ void copy_wait(int left) {
 // Many long rows: one persistent block per SM, each with a row, or clusters of a few blocks with one.  A block goes over its
 // share twice, the second time for the gradient.  The rows in work at one time are held to kLiveBytes, which L2 keeps until
 // they are read again, so that HBM sees the logits once.  One thread fills a ring of kStages chunks by bulk copies and runs on
-// from the first pass into the second and from there into the next row.  Sixteen warps have the columns, eight vectors of
+// from the first pass into the second and from there into the next row.  Fifteen warps have the columns, eight vectors of
 // a chunk each; one more has, a row ahead, the teacher, the columns outside the vectors and the loss, and, behind the
 // barrier of the following row, the teacher's columns of the gradient.
-// 2048 bf16 rows of 132352 columns 213 us, of which the bytes need 163; measured on the way there: rows held in the shared
-// memory of clusters of four 291 (a fourth of a row's time in its barrier, a seventh of the SMs without work); two blocks
-// per SM with a row each, 78 MB of live rows, half of whose second read misses L2, 250; the first pass of the next row
-// chunk by chunk in turn with the second one of this, no barrier to wait for but the gradient's lines between a row's
-// two reads, 247; fifteen warps instead of four for each scheduler 222; thirty with four vectors 226; packed fp32 pairs 225.
-// Loss alone 100: half of it is the exponentials.
-constexpr int kStreamWarps = 16, kStreamThreads = 32 * kStreamWarps, kStreamFold = 8, kStreamK = 256, kStages = 3;
+// 2048 bf16 rows of 132352 columns 214 to 221 us, of which the bytes need 163; 700 fp32 rows of 132347, loss and backward
+// pass, 225 (168).  Measured on the way there, us: rows held in the shared memory of clusters of four 291 (a fourth of a row's time
+// in its barrier, a seventh of the SMs without work); two blocks per SM with a row each, 78 MB of live rows, half of whose
+// second read misses L2, 250; the first pass of the next row chunk by chunk in turn with the second one of this, no barrier
+// to wait for but the gradient's lines between a row's two reads, 247; sixteen warps 215 and 237, with chunks of even size 217
+// and 231; thirty warps with four vectors 226; packed pairs of fp32 225.  The loss alone of bf16 rows takes 105, half of
+// which the exponentials need.
+constexpr int kStreamWarps = 15, kStreamThreads = 32 * kStreamWarps, kStreamFold = 8, kStreamK = 256, kStages = 3;
 constexpr int kPairs = kStreamWarps + 1;                   // warps that meet in a row's exchange
 constexpr int kChunk = kStreamFold * kStreamThreads;       // vectors of a chunk, at most
 constexpr size_t kLiveBytes = (size_t)40 << 20;
