@@ -2,8 +2,9 @@
 // q = softmax(l / T), and p = softmax(t / T) over the teacher's entries that the row can see:
 //   loss = T^2 sum_j p_j (log p_j - log q_{id_j}),     d loss / d l_c = T (q_c - sum_{id_j = c} p_j).
 //
-// One kernel, a cluster of 1 to 8 blocks per row.  Every block reads its share of the columns once and folds it into a
-// running maximum and sum of exponentials; every warp sends its pair to the shared memory of all blocks; one cluster
+// Two forms of one pass.  k_distill_stream takes many long rows (at least one for every two SMs, of 128 KB or
+// more, with up to 256 entries): see there.  k_distill takes the others, a cluster of 1 to 8 blocks per row.  Every block reads its share of the columns once
+// and folds it into a running maximum and sum of exponentials; every warp sends its pair to the shared memory of all blocks; one cluster
 // barrier.  When the gradient is asked for, the share stays in shared memory until then (a thread only ever reads back
 // what it has brought itself, so that its own copies' completion is all it waits for): the logits are read once and the
 // gradient written once.  Rows longer than eight blocks hold (some 440000 fp32 columns) are read again.  The backward
@@ -32,9 +33,9 @@ constexpr int kDistillMaxK = 1024;
 constexpr int kDistillThreads = 256;     // of a block, at most
 constexpr int kFold = 4;                 // vectors of 16 bytes that a thread folds at once, and waits for at once
 constexpr size_t kShareBytes = 72 << 10;              // of a row per block, for three blocks per SM
-constexpr size_t kStreamRow = 32 << 10;               // rows from here on for the persistent form
-constexpr int kStreamSlots = 148;                     // its blocks
 constexpr size_t kShareMax = 208 << 10;               // ... and at most, for one
+constexpr size_t kStreamRow = 128 << 10;              // rows from here on for the persistent form
+constexpr int kStreamSlots = 148;                     // its blocks
 
 struct DistillArgs {
   const void* logits; int cols; long long ld;
@@ -198,26 +199,6 @@ __device__ __forceinline__ bool load_teacher(const DistillArgs& a, int r, int C,
   return true;
 }
 
-// The gradient in the teacher's columns [c0, c1), behind a barrier after the columns' own: k (q - sum of p), the sums by
-// whoever holds a column's first entry.  q_of(x): the probability of a column with logit x.
-template <typename T, typename Q>
-__device__ __forceinline__ void put_teacher(const DistillArgs& a, const TeacherView& v, T* out, int c0, int c1, float k, Q q_of) {
-  for (int j = threadIdx.x; j < a.K; j += blockDim.x) {
-    const int id = v.id[j];
-    if (id < c0 || id >= c1) continue;
-    float p = 0.f;
-    bool first = true;
-    for (int i = 0; i < a.K; i += 4) {
-      const int4 o = *reinterpret_cast<const int4*>(v.id + i);
-      if (o.x == id) { first &= i >= j; p += v.p[i]; }
-      if (o.y == id) { first &= i + 1 >= j; p += v.p[i + 1]; }
-      if (o.z == id) { first &= i + 2 >= j; p += v.p[i + 2]; }
-      if (o.w == id) { first &= i + 3 >= j; p += v.p[i + 3]; }
-    }
-    if (first) out[id] = from_f32<T>(k * (q_of(v.x[j]) - p));
-  }
-}
-
 __device__ __forceinline__ void copy_async(void* smem, const void* g) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(smem)), "l"(g) : "memory");
 }
@@ -242,7 +223,7 @@ __device__ __forceinline__ void copy_wait(int left) {
 // a chunk each; one more has, a row ahead, the teacher, the columns outside the vectors and the loss, and, behind the
 // barrier of the following row, the teacher's columns of the gradient.
 // 2048 bf16 rows of 132352 columns 214 to 221 us, of which the bytes need 163; 700 fp32 rows of 132347, loss and backward
-// pass, 225 (168).  Measured on the way there, us: rows held in the shared memory of clusters of four 291 (a fourth of a row's time
+// pass, 222 (168).  Measured on the way there, us: rows held in the shared memory of clusters of four 291 (a fourth of a row's time
 // in its barrier, a seventh of the SMs without work); two blocks per SM with a row each, 78 MB of live rows, half of whose
 // second read misses L2, 250; the first pass of the next row chunk by chunk in turn with the second one of this, no barrier
 // to wait for but the gradient's lines between a row's two reads, 247; sixteen warps 215 and 237, with chunks of even size 217
@@ -783,7 +764,12 @@ cudaError_t launch_stream(const DistillArgs& a, int N, int log_g, cudaStream_t s
 template <typename T>
 cudaError_t launch_loss(const DistillArgs& a, int N, cudaStream_t s) {
   const size_t row = (size_t)a.cols * sizeof(T);
-  if (a.K <= kStreamK && row >= kStreamRow && N >= kStreamSlots) {
+  // The persistent form from rows on whose exchange is short beside their bytes, and from a row for every two SMs on.  Clusters
+  // against it, us, bf16, loss alone / with the gradient: 1024 rows of 32 KB 15 / 24 against 26 / 53, of 64 KB 22 / 44 against
+  // 32 / 61, of 128 KB 38 / 76 against 38 / 70, of 258 KB 73 / 149 against 56 / 114; 148 rows of 258 KB 14 / 32 against 13 / 23, 74
+  // rows 11 / 17 against 10 / 15, 37 rows 10 / 14 against 10 / 18.  (A longer teacher's list than kStreamK has no room beside
+  // the ring.)
+  if (a.K <= kStreamK && row >= kStreamRow && N >= kStreamSlots / 2) {
     // blocks per row: so many that the rows in work stay in L2, and more where the last round would leave much of the machine idle
     int log_g = 0;
     if (a.grad) while (log_g < 3 && row * (kStreamSlots >> log_g) > kLiveBytes) ++log_g;

@@ -231,7 +231,13 @@ def test_distill_of_many_rows(dt, N, cols, K):
         ids[8] = -1
         ids[10, :] = ids[10, 0]
     rows = [0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 20, 36, 37, 73, 74, N // 2, N - 2, N - 1] if cols < 200000 else [0, 3, 4, 5, 6, 7, 8, 9, N - 1]
-    check(l, n, ids, t, 1.3, w, ld=cols + (cols % 3), in_place=True, rows=rows)
+    check(l, n, ids, t, 1.3, w, ld=cols + (cols % 3), in_place=True, rows=[r for r in rows if r < N])
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,cols,K", [(74, 65537, 5), (300, 70003, 127), (155, 80001, 0), (90, 66001, 256), (223, 32768, 9), (223, 32767, 257)])
+def test_distill_of_many_rows_around_the_forms_limits(dt, N, cols, K):
+    test_distill_of_many_rows(dt, N, cols, K)
 
 
 def test_distill_without_a_teacher_list():
