@@ -240,6 +240,14 @@ def test_distill_of_many_rows_around_the_forms_limits(dt, N, cols, K):
     test_distill_of_many_rows(dt, N, cols, K)
 
 
+@pytest.mark.parametrize("cols", [12000, 12160, 12200, 12240, 12280, 12320])
+@pytest.mark.parametrize("K", [0, 3])
+def test_distill_of_rows_around_48_kb_of_shared_memory(K, cols):
+    rng = np.random.default_rng(cols + K)
+    l, n, ids, t = batch(rng, 100, cols, max(K, 1), torch.float32)
+    check(l, n, ids if K else None, t if K else None, 1.0, None, rows=[0, 1, 50, 99])
+
+
 def test_distill_without_a_teacher_list():
     l = torch.randn(4, 300)
     check(l, [300, 5, 0, 299], None, None, 1.0, None)
