@@ -3,7 +3,7 @@
 //   loss = T^2 sum_j p_j (log p_j - log q_{id_j}),     d loss / d l_c = T (q_c - sum_{id_j = c} p_j).
 //
 // Two forms of one pass.  k_distill_stream takes many long rows (at least one for every two SMs, of 128 KB or
-// more, with up to 256 entries): see there.  k_distill takes the others, a cluster of 1 to 8 blocks per row.  Every block reads its share of the columns once
+// more, with up to 512 entries): see there.  k_distill takes the others, a cluster of 1 to 8 blocks per row.  Every block reads its share of the columns once
 // and folds it into a running maximum and sum of exponentials; every warp sends its pair to the shared memory of all blocks; one cluster
 // barrier.  When the gradient is asked for, the share stays in shared memory until then (a thread only ever reads back
 // what it has brought itself, so that its own copies' completion is all it waits for): the logits are read once and the
@@ -33,7 +33,7 @@ constexpr int kDistillMaxK = 1024;
 constexpr int kDistillThreads = 256;     // of a block, at most
 constexpr int kFold = 4;                 // vectors of 16 bytes that a thread folds at once, and waits for at once
 constexpr size_t kShareBytes = 72 << 10;              // of a row per block, for three blocks per SM
-constexpr size_t kShareMax = 208 << 10;               // ... and at most, for one
+constexpr size_t kShareMax = 224 << 10;               // ... and at most, for one
 constexpr size_t kStreamRow = 128 << 10;              // rows from here on for the persistent form
 constexpr int kStreamSlots = 148;                     // its blocks
 
@@ -46,6 +46,7 @@ struct DistillArgs {
   const float* old_lse;         // or NULL: rows of -inf here have nothing visible
   void* grad;                   // or NULL
   int grad_skew;                // the gradient's rows are not aligned to 16 bytes where the logits' are
+  int teacher_bytes;            // of shared memory in front of the columns held there
 };
 
 __device__ __forceinline__ int visible_cols(const DistillArgs& a, int r) {
@@ -160,43 +161,147 @@ __device__ __forceinline__ Fold warp_fold(Fold f, float c) {
   return t;
 }
 
-// The teacher's entries in shared memory: id (-1: left out), p, and the row's logit there.
-struct TeacherView { int* id; float* p; float* x; };
+// The teacher's entries in shared memory: id (-1: left out), p, its base-2 logarithm, and the row's logit there; for a gradient
+// also what mark_repeats needs: a table of eight slots or more per entry, and an entry's representative.
+constexpr int kLater = 1 << 30;          // in id: an entry before this one has the same column; the other bits are the first one's number
+constexpr int kRepeated = 1 << 29;       // in id: one behind it has; the p of all of them is in v.sum()
+constexpr int kIdMask = kRepeated - 1;
+struct TeacherView {
+  int* id; float *p, *lp, *x; int* rep; unsigned short* table;
+  // p of the column that entry j, with this id, is the first one of
+  __device__ __forceinline__ float* sum() const { return reinterpret_cast<float*>(table); }
+  __device__ __forceinline__ float p_of(int j, int e) const { return e & kRepeated ? sum()[j] : p[j]; }
+};
+__host__ __device__ __forceinline__ int table_bits(int K) {
+  int b = 6;
+  while ((1 << b) < 8 * K) ++b;
+  return b;
+}
 __device__ __forceinline__ TeacherView teacher_at(char* smem, int K) {
   const int K4 = (K + 3) & ~3;
   TeacherView v;
-  v.id = reinterpret_cast<int*>(smem); v.p = reinterpret_cast<float*>(smem) + K4; v.x = reinterpret_cast<float*>(smem) + 2 * K4;
+  v.id = reinterpret_cast<int*>(smem); v.p = reinterpret_cast<float*>(smem) + K4; v.lp = v.p + K4; v.x = v.lp + K4;
+  v.rep = v.id + 4 * K4; v.table = reinterpret_cast<unsigned short*>(v.rep + K4);
   return v;
 }
-__host__ __device__ inline size_t teacher_bytes(int K) { return (size_t)((K + 3) & ~3) * 12; }
+__host__ inline size_t teacher_bytes(int K, bool grad) { return (size_t)((K + 3) & ~3) * (grad ? 20 : 16) + (grad ? (size_t)2 << table_bits(K) : 0); }
 
-// One warp: reads the K entries, normalises p over those that the row can see.  Returns whether there is one, and log2 of the
-// normaliser and the reference of the exponents (the base-2 logarithm of p_j is c t_j - ref - lg).
-__device__ __forceinline__ bool load_teacher(const DistillArgs& a, int r, int C, const TeacherView& v, float& ref, float& lg) {
+constexpr int kTeacherAhead = 8;         // entries that a lane has under way
+// One warp: reads the K entries, normalises p over those that the row can see.  Returns whether there is one.
+__device__ __forceinline__ bool load_teacher(const DistillArgs& a, int r, int C, const TeacherView& v) {
   const int lane = threadIdx.x & 31;
   float tm = -INFINITY;
-  for (int j = lane; j < ((a.K + 3) & ~3); j += 32) {
-    int id = -1;
-    float t = -INFINITY;
-    if (j < a.K) {
-      id = a.ids[(size_t)r * a.K + j];
-      t = a.t[(size_t)r * a.K + j];
+  for (int j0 = lane; j0 < a.K; j0 += 32 * kTeacherAhead) {
+    int id[kTeacherAhead];
+    float t[kTeacherAhead];
+#pragma unroll
+    for (int u = 0; u < kTeacherAhead; ++u) {
+      const size_t at = (size_t)r * a.K + min(j0 + 32 * u, a.K - 1);
+      id[u] = __ldg(a.ids + at);
+      t[u] = __ldg(a.t + at);
     }
-    if ((unsigned)id >= (unsigned)C || t == -INFINITY) { id = -1; t = -INFINITY; }
-    v.id[j] = id; v.p[j] = t;
-    tm = fmaxf(tm, t != t ? INFINITY : t);
+#pragma unroll
+    for (int u = 0; u < kTeacherAhead; ++u) {
+      const int j = j0 + 32 * u;
+      if ((unsigned)id[u] >= (unsigned)C || t[u] == -INFINITY) { id[u] = -1; t[u] = -INFINITY; }
+      if (j < a.K) { v.id[j] = id[u]; v.p[j] = t[u]; }
+      tm = fmaxf(tm, t[u] != t[u] ? INFINITY : t[u]);      // (the last entry, once more, behind the end)
+    }
   }
   tm = warp_max(tm);
-  ref = a.c * tm; lg = 0.f;
-  if (tm == -INFINITY) return false;
+  if (tm == -INFINITY) { __syncwarp(); return false; }
+  const float ref = a.c * tm;
   float s = 0.f;
   for (int j = lane; j < a.K; j += 32) if (v.id[j] >= 0) s += ex2(fmaf(v.p[j], a.c, -ref));
   s = warp_sum(s);
-  lg = log2f(s);
-  const float inv = 1.f / s;
-  for (int j = lane; j < a.K; j += 32) if (v.id[j] >= 0) v.p[j] = ex2(fmaf(v.p[j], a.c, -ref)) * inv;
+  const float lg = log2f(s), inv = 1.f / s;
+  for (int j = lane; j < a.K; j += 32)
+    if (v.id[j] >= 0) {
+      // (log2 p_j from the teacher's logit, which is exact where p_j is not)
+      const float z = fmaf(v.p[j], a.c, -ref);
+      v.p[j] = ex2(z) * inv; v.lp[j] = z - lg;
+    }
   __syncwarp();
   return true;
+}
+// The same warp: the row's logits at the entries that `wants` names.
+template <typename T, typename W>
+__device__ __forceinline__ void load_logits(const T* l, const TeacherView& v, int K, W wants) {
+  for (int j0 = threadIdx.x & 31; j0 < K; j0 += 32 * kTeacherAhead) {
+    float x[kTeacherAhead];
+#pragma unroll
+    for (int u = 0; u < kTeacherAhead; ++u) {
+      const int id = v.id[min(j0 + 32 * u, K - 1)];
+      x[u] = to_f32<T>(l[id >= 0 && wants(id) ? id : 0]);
+    }
+#pragma unroll
+    for (int u = 0; u < kTeacherAhead; ++u) if (j0 + 32 * u < K) v.x[j0 + 32 * u] = x[u];
+  }
+}
+// The same warp, when it has no more use for the ids of repeated entries: marks entries that share a column, for the gradient,
+// which has one value there, and adds their p up, in order.  Every entry writes its number to a slot that its id gives, and
+// looks who stands there afterwards: an entry of the same column represents it, and with one of another column both
+// of that column's entries go to the next round, with other slots.  A round ends it for a column in every slot that was written.
+// (1024 bf16 rows of 132352 columns with 256 / 512 entries take 121 / 144 us this way, 115 / 120 without looking; 130 / 183 with a
+// table filled by compare-and-swap, 241 / 538 where every entry looked at all others.)
+__device__ __forceinline__ void mark_repeats(const TeacherView& v, int K) {
+  const int lane = threadIdx.x & 31, shift = 32 - table_bits(K), steps = (K + 31) / 32;
+  constexpr unsigned kMul = 2654435769u;                   // (odd, as all the later rounds' are)
+  constexpr int kAhead = 4;
+  for (int j = lane; j < K; j += 32) if (v.id[j] >= 0) v.table[(unsigned)v.id[j] * kMul >> shift] = (unsigned short)j;
+  __syncwarp();
+  unsigned open = 0u;                                      // bit per entry of this lane
+  bool twice = false;
+  for (int b0 = 0; b0 < steps; b0 += kAhead) {
+    int id[kAhead], w[kAhead], other[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) { const int j = lane + 32 * (b0 + u); id[u] = j < K ? v.id[j] : -1; }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) w[u] = id[u] >= 0 ? v.table[(unsigned)id[u] * kMul >> shift] : 0;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) other[u] = v.id[w[u]];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = lane + 32 * (b0 + u);
+      if (id[u] < 0) continue;
+      if (other[u] == id[u]) { v.rep[j] = w[u]; twice |= w[u] != j; }
+      else open |= 1u << (b0 + u);
+    }
+  }
+  for (unsigned mul = kMul; __any_sync(0xffffffffu, open != 0u);) {
+    mul += 0x9e3779b8u;
+    for (unsigned m = open; m; m &= m - 1u) { const int j = lane + 32 * (__ffs(m) - 1); v.table[(unsigned)v.id[j] * mul >> shift] = (unsigned short)j; }
+    __syncwarp();
+    for (unsigned m = open; m; m &= m - 1u) {
+      const int j = lane + 32 * (__ffs(m) - 1), id = v.id[j], w = v.table[(unsigned)id * mul >> shift];
+      if (v.id[w] == id) { v.rep[j] = w; twice |= w != j; open &= ~(m & (0u - m)); }
+    }
+    __syncwarp();
+  }
+  if (!__any_sync(0xffffffffu, twice)) return;
+  // a column's first entry, at its representative; then the sums, at the first ones (both in the table's place)
+  int* const first = reinterpret_cast<int*>(v.table) + K;
+  for (int j = lane; j < K; j += 32) { first[j] = j; v.sum()[j] = v.p[j]; }
+  __syncwarp();
+  for (int j = lane; j < K; j += 32) if (v.id[j] >= 0 && v.rep[j] != j) atomicMin(&first[v.rep[j]], j);
+  __syncwarp();
+  for (int j0 = 0; j0 < K; j0 += 32) {
+    const int j = j0 + lane;
+    int f = -1;
+    if (j < K && v.id[j] >= 0) {
+      f = first[v.rep[j]];
+      if (f == j) f = -1;
+      else v.id[j] = kLater | f;
+    }
+    const unsigned peers = __match_any_sync(0xffffffffu, f);
+    if (f >= 0 && __ffs(peers) - 1 == lane) {
+      float p = v.sum()[f];
+      for (unsigned m = peers; m; m &= m - 1u) p += v.p[j0 + __ffs(m) - 1];
+      v.sum()[f] = p;
+      v.id[f] |= kRepeated;
+    }
+    __syncwarp();
+  }
 }
 
 __device__ __forceinline__ void copy_async(void* smem, const void* g) {
@@ -222,45 +327,33 @@ __device__ __forceinline__ void copy_wait(int left) {
 // from the first pass into the second and from there into the next row.  Fifteen warps have the columns, eight vectors of
 // a chunk each; one more has, a row ahead, the teacher, the columns outside the vectors and the loss, and, behind the
 // barrier of the following row, the teacher's columns of the gradient.
-// 2048 bf16 rows of 132352 columns 214 to 221 us, of which the bytes need 163; 700 fp32 rows of 132347, loss and backward
-// pass, 222 (168).  Measured on the way there, us: rows held in the shared memory of clusters of four 291 (a fourth of a row's time
+// 2048 bf16 rows of 132352 columns 214 to 226 us by the board, of which the bytes need 163; 700 fp32 rows of 132347, loss and backward
+// pass, 225 (168).  Measured on the way there, us: rows held in the shared memory of clusters of four 291 (a fourth of a row's time
 // in its barrier, a seventh of the SMs without work); two blocks per SM with a row each, 78 MB of live rows, half of whose
 // second read misses L2, 250; the first pass of the next row chunk by chunk in turn with the second one of this, no barrier
 // to wait for but the gradient's lines between a row's two reads, 247; sixteen warps 215 and 237, with chunks of even size 217
 // and 231; thirty warps with four vectors 226; packed pairs of fp32 225.  The loss alone of bf16 rows takes 105, half of
 // which the exponentials need.
-constexpr int kStreamWarps = 15, kStreamThreads = 32 * kStreamWarps, kStreamFold = 8, kStreamK = 256, kStages = 3;
+constexpr int kStreamWarps = 15, kStreamThreads = 32 * kStreamWarps, kStreamFold = 8, kStreamK = 512, kStages = 3;
 constexpr int kPairs = kStreamWarps + 1;                   // warps that meet in a row's exchange
 constexpr int kChunk = kStreamFold * kStreamThreads;       // vectors of a chunk, at most
 constexpr size_t kLiveBytes = (size_t)40 << 20;
 
-struct alignas(16) StreamTeacher { int id[kStreamK]; float p[kStreamK], x[kStreamK]; float ref, lg; int some, c0, c1; };
+struct StreamTeacher { int id[kStreamK]; float p[kStreamK], lp[kStreamK], x[kStreamK]; int some, c0, c1; };
 
 // One warp: x becomes the gradient in this block's teacher columns, k (q - sum of p), with the sum in a column's first entry;
 // id becomes -1 where nothing is to be written.
-__device__ __forceinline__ void finish_teacher(const DistillArgs& a, StreamTeacher& t, bool zero, float k, const Fold& f) {
+__device__ __forceinline__ void finish_teacher(const DistillArgs& a, StreamTeacher& t, const TeacherView& v, bool zero, float k, const Fold& f) {
   const int lane = threadIdx.x & 31;
   unsigned write = 0u;                                     // bit per entry of this lane
   for (int j = lane, b = 0; j < a.K; j += 32, ++b) {
-    const int id = t.id[j];
-    if (zero || id < t.c0 || id >= t.c1) continue;
-    float p = 0.f;
-    bool first = true;
-    for (int i = 0; i < a.K; i += 4) {
-      const int4 o = *reinterpret_cast<const int4*>(t.id + i);
-      if (o.x == id || o.y == id || o.z == id || o.w == id) {
-        if (o.x == id) { first &= i >= j; p += t.p[i]; }
-        if (o.y == id) { first &= i + 1 >= j; p += t.p[i + 1]; }
-        if (o.z == id) { first &= i + 2 >= j; p += t.p[i + 2]; }
-        if (o.w == id) { first &= i + 3 >= j; p += t.p[i + 3]; }
-      }
-    }
-    if (!first) continue;
-    t.x[j] = k * (ex2(fmaf(t.x[j], a.c, -f.r)) / f.s - p);
+    const int id = t.id[j] & kIdMask;
+    if (zero || t.id[j] < 0 || (t.id[j] & kLater) || id < t.c0 || id >= t.c1) continue;
+    t.x[j] = k * (ex2(fmaf(t.x[j], a.c, -f.r)) / f.s - v.p_of(j, t.id[j]));
     write |= 1u << b;
   }
   __syncwarp();
-  for (int j = lane, b = 0; j < a.K; j += 32, ++b) if (!((write >> b) & 1u)) t.id[j] = -1;
+  for (int j = lane, b = 0; j < a.K; j += 32, ++b) t.id[j] = (write >> b) & 1u ? t.id[j] & kIdMask : -1;
   __syncwarp();
 }
 template <typename T> __device__ __forceinline__ void put_teacher(const DistillArgs& a, const StreamTeacher& t, T* out) {
@@ -276,6 +369,8 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
   constexpr int kN = kPer<T>;
   __shared__ float2 s_all[2][8 * kPairs];
   __shared__ StreamTeacher s_teacher[2];
+  __shared__ int s_rep[GRAD ? kStreamK : 1];
+  __shared__ __align__(16) unsigned short s_table[GRAD ? 8 * kStreamK : 8];
   __shared__ __align__(8) unsigned long long s_full[kStages], s_empty[kStages], s_pairs[2];
   __shared__ int s_abort;                                  // a wait has given up: no one waits any more, the losses are NaN
   namespace cg = cooperative_groups;
@@ -432,18 +527,16 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
     };
     float edge_x = 0.f;
     // the first block takes the loss and with it the row's logits at all entries, the others those of their own columns
+    auto view_of = [&](StreamTeacher& t) { return TeacherView{t.id, t.p, t.lp, t.x, s_rep, s_table}; };
     auto prepare = [&](int i, int C, const RowPart<T>& q) {
       StreamTeacher& t = s_teacher[i & 1];
       const int e = edge_of(q);
       edge_x = e >= 0 && e < C ? to_f32<T>(q.l[e]) : -INFINITY;
-      const TeacherView tv{t.id, t.p, t.x};
-      float ref, lg;
-      const bool some = load_teacher(a, row_at(i), C, tv, ref, lg);
-      for (int j = lane; j < a.K; j += 32) {
-        const int id = t.id[j];
-        if (id >= 0 && (rank == 0 || (id >= q.c0 && id < q.c1))) t.x[j] = to_f32<T>(q.l[id]);
-      }
-      if (lane == 0) { t.ref = ref; t.lg = lg; t.some = some; t.c0 = q.c0; t.c1 = q.c1; }
+      const TeacherView tv = view_of(t);
+      const bool some = load_teacher(a, row_at(i), C, tv);
+      load_logits<T>(q.l, tv, a.K, [&](int id) { return rank == 0 || (id >= q.c0 && id < q.c1); });
+      if (GRAD && some) mark_repeats(tv, a.K);
+      if (lane == 0) { t.some = some; t.c0 = q.c0; t.c1 = q.c1; }
       __syncwarp();
     };
     int C = cols_of(0), C1 = cols_of(1);
@@ -467,7 +560,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
         if (live)
           for (int j = lane; j < a.K; j += 32) {
             const float p = t.p[j];
-            if (t.id[j] >= 0 && p != 0.f) loss += p * (fmaf(a.t[(size_t)r * a.K + j], a.c, -t.ref) - t.lg - (fmaf(t.x[j], a.c, -f.r) - ls));
+            if (t.id[j] >= 0 && p != 0.f) loss += p * (t.lp[j] - (fmaf(t.x[j], a.c, -f.r) - ls));
           }
         loss = warp_sum(loss) * kLn2 * a.temperature * a.temperature;
         const bool lost = *reinterpret_cast<volatile int*>(&s_abort) != 0;
@@ -478,7 +571,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
         const float k = w * a.temperature;
         const int e = edge_of(q);
         if (e >= 0) (reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld)[e] = from_f32<T>(zero || e >= C ? 0.f : k * (ex2(fmaf(edge_x, a.c, -f.r)) / f.s));
-        finish_teacher(a, t, zero, k, f);
+        finish_teacher(a, t, view_of(t), zero, k, f);
       }
       if (i + 1 < rows) {
         C = C1; C1 = cols_of(i + 2);
@@ -526,7 +619,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   extern __shared__ __align__(16) char smem[];
   constexpr int kN = kPer<T>, kMaxWarps = kDistillThreads / 32;
   __shared__ float2 s_all[8 * kMaxWarps];                  // (m, s) of every warp of the row
-  __shared__ float s_t[3];                                 // the teacher's reference, log2 of its normaliser, 1 if it has an entry
+  __shared__ int s_some;                                   // the teacher has an entry
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   sm100::pdl_wait();
@@ -541,7 +634,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   const uint4* lv = reinterpret_cast<const uint4*>(l + sp.head);
   const int full = min(v1, max(v0, (C - sp.head) / kN));   // vectors [v0, full) are columns of the row; at most one behind is in part
   const int U = (full - v0 + threads - 1) / threads, groups = (U + kFold - 1) / kFold;
-  uint4* hold = reinterpret_cast<uint4*>(smem + teacher_bytes(a.K));
+  uint4* hold = reinterpret_cast<uint4*>(smem + a.teacher_bytes);
   // ---- the share's columns
   if (HOLD) {
     for (int g = 0; g < groups; ++g) {
@@ -565,14 +658,11 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   const int c0 = rank == 0 ? 0 : sp.head + v0 * kN, c1 = rank == G - 1 ? a.cols : sp.head + v1 * kN;
   auto held = [&](int id) { return HOLD && id >= sp.head + v0 * kN && id < part; };
   const TeacherView tv = teacher_at(smem, a.K);
-  if (warp == warps - 1) {
-    float ref, lg;
-    const bool some = load_teacher(a, r, C, tv, ref, lg);
-    for (int j = lane; j < a.K; j += 32) {
-      const int id = tv.id[j];
-      if (id >= 0 && (rank == 0 || (id >= c0 && id < c1 && !held(id)))) tv.x[j] = to_f32<T>(l[id]);
-    }
-    if (lane == 0) { s_t[0] = ref; s_t[1] = lg; s_t[2] = some ? 1.f : 0.f; }
+  if (warp == warps - 1 && (GRAD || rank == 0)) {
+    const bool some = load_teacher(a, r, C, tv);
+    load_logits<T>(l, tv, a.K, [&](int id) { return rank == 0 || (id >= c0 && id < c1 && !held(id)); });
+    if (GRAD && some) mark_repeats(tv, a.K);
+    if (lane == 0) s_some = some;
   }
   // ---- maximum and sum
   Fold f;
@@ -613,19 +703,14 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
     else f.s += orr > -INFINITY ? o.y * ex2(orr - f.r) : o.y;
   }
   f = warp_fold(f, a.c);
-  const bool some = s_t[2] != 0.f, live = some && f.s != 0.f;
+  const bool live = f.s != 0.f && s_some;
   const float ls = log2f(f.s);
   if (rank == 0 && warp == 0 && a.loss) {
     float loss = 0.f;
     if (live) {
-      const float tl = s_t[0], lg = s_t[1];
       for (int j = lane; j < a.K; j += 32) {
         const float p = tv.p[j];
-        if (tv.id[j] >= 0 && p != 0.f) {
-          // log2 p_j again from the teacher's logit, which is exact where p_j is not
-          const float lp = fmaf(a.t[(size_t)r * a.K + j], a.c, -tl) - lg, lq = fmaf(tv.x[j], a.c, -f.r) - ls;
-          loss += p * (lp - lq);
-        }
+        if (tv.id[j] >= 0 && p != 0.f) loss += p * (tv.lp[j] - (fmaf(tv.x[j], a.c, -f.r) - ls));
       }
       loss = warp_sum(loss) * kLn2 * a.temperature * a.temperature;
     }
@@ -666,20 +751,11 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   for (int i = n_full + tid; i < v1 - v0; i += threads) if (zero || v0 + i != full) put(i, nothing);
   if (zero) return;
   __syncthreads();
-  // the teacher's columns, over the columns' own: k (q - sum of p), the sum by whoever holds a column's first entry
+  // the teacher's columns, over the columns' own: k (q - sum of p), by whoever has a column's first entry
   for (int j = tid; j < a.K; j += threads) {
-    const int id = tv.id[j];
-    if (id < c0 || id >= c1) continue;
-    float p = 0.f;
-    bool first = true;
-    for (int i = 0; i < a.K; i += 4) {
-      const int4 o = *reinterpret_cast<const int4*>(tv.id + i);
-      if (o.x == id) { first &= i >= j; p += tv.p[i]; }
-      if (o.y == id) { first &= i + 1 >= j; p += tv.p[i + 1]; }
-      if (o.z == id) { first &= i + 2 >= j; p += tv.p[i + 2]; }
-      if (o.w == id) { first &= i + 3 >= j; p += tv.p[i + 3]; }
-    }
-    if (!first) continue;
+    const int id = tv.id[j] & kIdMask;
+    if (tv.id[j] < 0 || (tv.id[j] & kLater) || id < c0 || id >= c1) continue;
+    const float p = tv.p_of(j, tv.id[j]);
     const float x = rank != 0 && held(id) ? to_f32<T>(reinterpret_cast<const T*>(hold)[id - sp.head - v0 * kN]) : tv.x[j];
     out[id] = from_f32<T>(k * (ex2(fmaf(x, a.c, -f.r)) / f.s - p));
   }
@@ -779,14 +855,15 @@ cudaError_t launch_loss(const DistillArgs& a, int N, cudaStream_t s) {
   }
   // Blocks per row: so many that a block's share leaves room for three on an SM, and more while all rows together do not
   // occupy the machine's SMs
+  const size_t teacher = (size_t)a.teacher_bytes;
   int G = 1;
   while (G < 8 && (row / G > kShareBytes || ((long long)N * 2 * G <= 148 && row / G > 4096))) G *= 2;
   const int vecs = (int)((row / 16 + G - 1) / G);
   int threads = (vecs / 2 + 63) / 64 * 64;                 // two vectors a thread at least
   threads = threads < 64 ? 64 : (threads > kDistillThreads ? kDistillThreads : threads);
-  const size_t teacher = teacher_bytes(a.K), share = (size_t)vecs * 16;
+  const size_t share = (size_t)vecs * 16;
   if (!a.grad) return launch_loss_typed<T, false, false>(a, N, G, threads, teacher, s);
-  if (share <= kShareMax) return launch_loss_typed<T, true, true>(a, N, G, threads, teacher + share, s);
+  if (teacher + share <= kShareMax) return launch_loss_typed<T, true, true>(a, N, G, threads, teacher + share, s);
   return launch_loss_typed<T, true, false>(a, N, G, threads, teacher, s);
 }
 
@@ -794,7 +871,7 @@ DistillArgs distill_args(const void* logits, int cols, int64_t ld, const int32_t
                          const float* weight, float* loss, float* lse, const float* old_lse, void* grad) {
   const int skew = grad && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(logits)) & 15) ? 1 : 0;
   return DistillArgs{logits, cols, ld, n_cols, ids, t, K, 1.f / temperature, temperature, (float)(1.4426950408889634 / (double)temperature),
-                     weight, loss, lse, old_lse, grad, skew};
+                     weight, loss, lse, old_lse, grad, skew, (int)teacher_bytes(K, grad != nullptr)};
 }
 }  // namespace
 

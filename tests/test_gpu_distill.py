@@ -248,6 +248,21 @@ def test_distill_of_rows_around_48_kb_of_shared_memory(K, cols):
     check(l, n, ids if K else None, t if K else None, 1.0, None, rows=[0, 1, 50, 99])
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("K,few", [(2, 1), (33, 5), (64, 64), (129, 1), (512, 300), (512, 3), (513, 300), (1024, 500), (1024, 2)])
+@pytest.mark.parametrize("N,cols", [(3, 2000), (76, 70003)])
+def test_distill_of_repeated_entries(dt, N, cols, K, few):
+    # few columns for many entries, spread over the row or side by side; left-out ones among them
+    rng = np.random.default_rng(1000 * K + few)
+    l = (torch.from_numpy(rng.standard_normal((N, cols)).astype(np.float32)) * 2).to(dt)
+    ids = np.stack([rng.choice(cols, few, replace=False)[rng.integers(0, few, K)] for _ in range(N)])
+    ids[1] = cols - 1 - rng.integers(0, min(few, cols), K)
+    ids[2, ::3] = -1
+    t = (rng.standard_normal((N, K)) * 2).astype(np.float32)
+    t[0, ::5] = -np.inf
+    check(l, [cols, cols, cols - 1] + [cols] * (N - 3), ids, t, 1.0, None, rows=[0, 1, 2] + ([40, N - 1] if N > 3 else []))
+
+
 def test_distill_without_a_teacher_list():
     l = torch.randn(4, 300)
     check(l, [300, 5, 0, 299], None, None, 1.0, None)
