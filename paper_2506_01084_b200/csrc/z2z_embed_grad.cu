@@ -6,10 +6,9 @@
 // of sequence b: V + b cap + k; a row without one: the number behind the last) and added in fp32 in the order of
 // their rows, so that the result does not depend on which block ran first.  No atomics touch a gradient.
 //
-//   k_grad_small   up to kSmallRows rows: one launch, no sort.  Every block holds all targets in shared memory; the block of
-//                  a target's first row finds the others and adds them up.  (1000 rows of 512 bf16 columns 11 us, through
-//                  the launches below 16; at 1500 rows either takes 17.  A single target for all rows is the worst case, 1024
-//                  rows one after the other.)
+//   k_grad_small   few rows (few_rows below): one launch, no sort.  Every block holds all targets in shared memory; the block of
+//                  a target's first row finds the others and adds them up.  (A single target for all rows is the worst case,
+//                  1024 rows one after the other.)
 //   k_grad_keys, k_grad_scatter (x passes), k_grad_sum, k_grad_finish otherwise:
 //     * the sort has digits of 9 bits (two passes up to 2^18 targets) over at most kTiles tiles.  A pass is one
 //       launch: every block sums the tiles' digit counts itself (a table of 2 KB per tile, from L2) instead of waiting
@@ -163,6 +162,15 @@ SumPlan sum_plan(int N, int d, int g_dtype) {
   return p;
 }
 
+// Few rows: those whose blocks' looks at all targets, by N blocks for every slab and, half of them beside the writes, by those of
+// the zeros, are fewer than 2^21.  One launch against the sort, us: 1000 rows of 512 bf16 columns 11.3 against 16.1; of 4096, 700
+// rows (2.0 million looks) 14.9 against 16.4, 1000 rows (4 million) 26 against 17; overwriting 128256 + 10101 rows of 4096 with 400 / 700
+// / 1000 rows (1.1 / 2.7 / 5.1 million) 177 / 179 / 191 against 181 / 181 / 182.
+constexpr int kZeroTargets = 64;         // of a block of zeros
+bool few_rows(int N, int slabs, int zeros) {
+  return N <= kSmallRows && ((long long)N * slabs + zeros / kZeroTargets / 2) * N <= 1 << 21;
+}
+
 struct SortPlan { int tiles, tile, passes; };
 SortPlan sort_plan(int N, int total) {
   SortPlan p{};
@@ -190,9 +198,9 @@ GradScratch scratch_at(char* base, int N, int d, int total) {
   GradScratch s{};
   size_t o = 0;
   auto take = [&](size_t bytes) { char* p = base + o; o = align_up(o + bytes, 256); return p; };
-  if (N > kSmallRows) {
-    // either type of g: the one with more chunks
-    const SumPlan a = sum_plan(N, d, Z2Z_DTYPE_FP32), b = sum_plan(N, d, Z2Z_DTYPE_BF16);
+  // either type of g: the one with more chunks and slabs
+  const SumPlan a = sum_plan(N, d, Z2Z_DTYPE_FP32), b = sum_plan(N, d, Z2Z_DTYPE_BF16);
+  if (!few_rows(N, a.slabs, total)) {
     const size_t chunks = a.chunks > b.chunks ? a.chunks : b.chunks;
     s.keys = reinterpret_cast<int32_t*>(take((size_t)N * 4));
     s.pairs[0] = reinterpret_cast<int2*>(take((size_t)N * 8));
@@ -210,7 +218,6 @@ GradScratch scratch_at(char* base, int N, int d, int total) {
 
 // ---- few rows ------------------------------------------------------------------------------------------
 // Blocks [0, N * slabs): a row and a slab of its columns; behind them (an overwriting call) blocks of kZeroTargets targets.
-constexpr int kZeroTargets = 64;
 template <typename TG, typename TO>
 __global__ void __launch_bounds__(kSumThreads) k_grad_small(CbView cb, GradTables t, const int32_t* __restrict__ codes, int N,
                                                             const int32_t* __restrict__ row_seq, const uint4* __restrict__ g, float scale,
@@ -550,7 +557,7 @@ cudaError_t launch_typed(const CbView& cb, const EmbedGradArgs& a, cudaStream_t 
   const int zero_lo = acc ? 0 : (a.gWE ? 0 : cb.V), zero_hi = acc ? 0 : (a.gEh ? t.total : cb.V);
   const uint4* g = reinterpret_cast<const uint4*>(a.g);
   const SumPlan p = sum_plan(a.N, a.d, a.g_dtype);
-  if (a.N <= kSmallRows) {
+  if (few_rows(a.N, p.slabs, zero_hi - zero_lo)) {
     const int blocks = a.N * p.slabs + (zero_hi - zero_lo + kZeroTargets - 1) / kZeroTargets;
     if (blocks == 0) return cudaSuccess;
     return launch_pdl(k_grad_small<TG, TO>, dim3(blocks), dim3(kSumThreads), 0, s, cb, t, a.codes, a.N, a.row_seq, g, a.scale, acc,

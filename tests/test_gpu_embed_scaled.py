@@ -245,7 +245,7 @@ def test_grad_of_many_targets_and_rows(N, V, cap, d):
     # targets beyond 18 bits (three passes of the sort), more rows than a block's registers hold, long chunks
     rng = np.random.default_rng(N)
     B = 5
-    n = [min(cap, V - 2), 0, min(cap, 700) // 2, 1, min(cap, 500)]
+    n = [min(cap, V - 2), 0, min(cap, 700) // 2, min(cap, 1), min(cap, 500)]
     cb = session(V, d, cap, B, "bf16", [min(x, V - 2) for x in n])
     seq = np.sort(rng.integers(0, B, N)).astype(np.int32)
     nn = np.array(n)[seq]
@@ -256,6 +256,12 @@ def test_grad_of_many_targets_and_rows(N, V, cap, d):
     g = torch.from_numpy(rng.standard_normal((N, d)).astype(np.float32)).bfloat16().to(DEV)
     check_grad(cb, codes, seq, g, n, V, cap, B, 2.0, torch.float32, False)
     check_grad(cb, codes, seq, g, n, V, cap, B, 0.5, torch.bfloat16, True)
+
+
+@pytest.mark.parametrize("N,V,cap,d", [(723, 500, 10, 4096), (725, 500, 10, 4096), (1000, 500, 10, 4096), (1000, 140000, 3, 8), (1000, 300000, 0, 8),
+                                       (300, 2000000, 2, 8), (129, 500, 10, 16384)])
+def test_grad_of_few_rows_with_many_columns_or_targets(N, V, cap, d):
+    test_grad_of_many_targets_and_rows(N, V, cap, d)
 
 
 def test_grad_on_two_streams_with_scratch_of_their_own():
