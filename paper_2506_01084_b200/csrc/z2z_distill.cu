@@ -2,12 +2,12 @@
 // q = softmax(l / T), and p = softmax(t / T) over the teacher's entries that the row can see:
 //   loss = T^2 sum_j p_j (log p_j - log q_{id_j}),     d loss / d l_c = T (q_c - sum_{id_j = c} p_j).
 //
-// Two forms of one pass.  k_distill_stream takes many long rows (at least one for every two SMs, of 128 KB or
-// more, with up to 512 entries): see there.  k_distill takes the others, a cluster of 1 to 8 blocks per row.  Every block reads its share of the columns once
-// and folds it into a running maximum and sum of exponentials; every warp sends its pair to the shared memory of all blocks; one cluster
-// barrier.  When the gradient is asked for, the share stays in shared memory until then (a thread only ever reads back
-// what it has brought itself, so that its own copies' completion is all it waits for): the logits are read once and the
-// gradient written once.  Rows longer than eight blocks hold (some 440000 fp32 columns) are read again.  The backward
+// Two forms of one pass.  k_distill_stream takes many long rows (at least one for every two SMs, of 128 KB or more, with up
+// to 512 entries): see there.  k_distill takes the others, a cluster of 1 to 8 blocks per row.  Every block reads its share of
+// the columns once and folds it into a running maximum and sum of exponentials; every warp sends its pair to the shared
+// memory of all blocks; one cluster barrier.  When the gradient is asked for, the share stays in shared memory until then (a
+// thread only ever reads back what it has brought itself, so that its own copies' completion is all it waits for): the logits
+// are read once and the gradient written once.  Rows longer than eight blocks hold (some 440000 fp32 columns) are read again.  The backward
 // pass on its own is the same with the normaliser found anew: that is no byte more, and does not depend on what a stored
 // lse has lost (2^-24 of |lse|, in every probability).
 // Bound by HBM, for bf16 rows with little left: 2 exponentials a column, at 16 per clock and SM, take 0.7 of the bytes'
