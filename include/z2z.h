@@ -302,7 +302,8 @@ int32_t z2z_embed_grad(z2z_codebook* cb, const int32_t* d_codes, int32_t N, cons
  * z2z_distill_grad is the backward pass on its own: d_grad_loss [N] is the derivative for d_loss, d_lse what
  * z2z_distill_loss left there for the same arguments (rows of -inf are not read again; the normaliser of the
  * others is found anew, since lse has lost 2^-24 of its size, and every probability with it).
- * (A wait inside the kernels that gives up leaves NaN in the row's d_loss and d_lse.)
+ * The waits inside the kernels are bounded (z2z_set_distill_wait_limit).  Where one gives up, every row that its cluster of
+ * blocks has taken is NaN throughout, whether or not it was done: d_loss, d_lse, and all cols columns of d_grad.
  *   d_grad [N, cols] of dtype, rows ld apart: every column is written, 0 from n_cols on.  A row whose
  *            weight is 0 has gradient 0 whatever its logits are.  d_grad == d_logits is allowed (the
  *            logits are then overwritten); they must not overlap in another way.                   */
@@ -315,6 +316,9 @@ int32_t z2z_distill_grad(const void* d_logits, int32_t dtype, int32_t N, int32_t
                          const int32_t* d_n_cols, const int32_t* d_teacher_ids,
                          const float* d_teacher_logits, int32_t K, float temperature,
                          const float* d_lse, const float* d_grad_loss, void* d_grad, z2z_stream stream);
+/* How long a wait inside the kernels of both calls may take before it gives up, in nanoseconds, for the calls that this process
+ * makes from now on; 0 = the default, 400 ms.  A process that shares its GPU with others in turn may have to wait longer.  */
+int32_t z2z_set_distill_wait_limit(int64_t ns);
 
 /* Beam search over the joint vocabularies (the paper decodes greedily or by sampling).  The beams of a request
  * are `beams` consecutive sequences of the session, each with its own codebook and caches: group g is the

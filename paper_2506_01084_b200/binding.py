@@ -30,7 +30,7 @@ EXPORTS = ["z2z_workspace_bytes", "z2z_codebook_init", "z2z_lzw_encode", "z2z_lz
            "z2z_profile_read", "z2z_set_tensor_cores", "z2z_logits_static_scratch",
            "z2z_lzw_decode", "z2z_embed_lookup", "z2z_upload_rows", "z2z_sample_filtered",
            "z2z_set_encoder_half_scratch", "z2z_embed_lookup_scaled", "z2z_embed_grad_scratch_bytes", "z2z_embed_grad",
-           "z2z_distill_loss", "z2z_distill_grad", "z2z_beam_select", "z2z_beam_reorder"]
+           "z2z_distill_loss", "z2z_distill_grad", "z2z_set_distill_wait_limit", "z2z_beam_select", "z2z_beam_reorder"]
 
 
 class Config(C.Structure):
@@ -53,6 +53,7 @@ _ARGTYPES = {
     "z2z_embed_grad": [_P, _P, _I, _P, _P, _F, _I, _I, _P, _P, _P, C.c_size_t, _P],
     "z2z_distill_loss": [_P, _I, _I, _I, _L, _P, _P, _P, _I, _F, _P, _P, _P, _P, _P],
     "z2z_distill_grad": [_P, _I, _I, _I, _L, _P, _P, _P, _I, _F, _P, _P, _P, _P],
+    "z2z_set_distill_wait_limit": [_L],
     "z2z_beam_select": [_P, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P],
     "z2z_beam_reorder": [_P, _P, _P, _P, _P, _P, C.POINTER(SeqRows), _I, _P],
 }
@@ -325,6 +326,11 @@ def z2z_distill_grad(logits: torch.Tensor, n_cols: Optional[torch.Tensor], teach
     N, args = _distill_args(logits, n_cols, teacher_ids, teacher_logits, temperature)
     _enqueue(lib().z2z_distill_grad, logits, *args, _dev(lse, torch.float32, N, "lse"), _dev(grad_loss, torch.float32, N, "grad_loss"),
              _like(grad, logits))
+
+
+def z2z_set_distill_wait_limit(ns: int):
+    """Nanoseconds after which a wait inside the distillation kernels gives up; 0 is the default, 400 ms."""
+    _check(lib().z2z_set_distill_wait_limit(ns))
 
 
 def z2z_beam_select(cb: Codebook, beams: int, logits: torch.Tensor, lse: torch.Tensor, scores: torch.Tensor,

@@ -18,6 +18,7 @@
 // one rounding of m / T.
 #include <cooperative_groups.h>
 
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -47,6 +48,7 @@ struct DistillArgs {
   void* grad;                   // or NULL
   int grad_skew;                // the gradient's rows are not aligned to 16 bytes where the logits' are
   int teacher_bytes;            // of shared memory in front of the columns held there
+  unsigned long long wait_ns;   // a wait gives up after
 };
 
 __device__ __forceinline__ int visible_cols(const DistillArgs& a, int r) {
@@ -372,7 +374,9 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
   __shared__ int s_rep[GRAD ? kStreamK : 1];
   __shared__ __align__(16) unsigned short s_table[GRAD ? 8 * kStreamK : 8];
   __shared__ __align__(8) unsigned long long s_full[kStages], s_empty[kStages], s_pairs[2];
-  __shared__ int s_abort;                                  // a wait has given up: no one waits any more, the losses are NaN
+  // A wait that gives up raises s_abort in all blocks of the cluster: no one waits any more, every block leaves its rows at its
+  // next exchange, and behind the barrier at the end all of the cluster's rows become NaN.
+  __shared__ int s_abort, s_sent[8];                       // exchanges that each block of the cluster has sent its pairs for
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   sm100::pdl_wait();
@@ -403,24 +407,39 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
   if (G > 1) cluster.sync();                               // all blocks are there before anything is sent to them
   else __syncthreads();
   if (rows == 0) return;
-  auto wait = [&](unsigned long long* bar, int parity) {   // by a whole warp
-    if (!*reinterpret_cast<volatile int*>(&s_abort)) sm100::mbar_wait(sm100::smem_u32(bar), (uint32_t)parity, &s_abort);
-    __syncwarp();
+  auto to_block = [&](int* word, int value) {              // lane j: into block j's shared memory
+    if (lane < G)
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(sm100::map_to_cta(sm100::smem_u32(word), lane)), "r"(value) : "memory");
+  };
+  auto wait = [&](unsigned long long* bar, int parity) {   // by a whole warp; false: given up, here or elsewhere
+    bool ok = *reinterpret_cast<volatile int*>(&s_abort) == 0;
+    ok = ok && sm100::mbar_wait(sm100::smem_u32(bar), (uint32_t)parity, &s_abort, a.wait_ns);
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) to_block(&s_abort, 1);
+    return ok;
+  };
+  auto send = [&](int i, float m, float sum) {             // (G > 1)
+    if (warp == kStreamWarps && lane == 0) sm100::mbar_expect_tx(sm100::smem_u32(&s_pairs[i & 1]), (uint32_t)(G * kPairs * 8));
+    if (lane < G)
+      asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                   ::"r"(sm100::map_to_cta(sm100::smem_u32(&s_all[i & 1][rank * kPairs + warp]), lane)), "f"(m), "f"(sum),
+                     "r"(sm100::map_to_cta(sm100::smem_u32(&s_pairs[i & 1]), lane)) : "memory");
   };
   // one exchange per row: every warp's pair to all blocks of the cluster.  Behind it all that the block's warps did ahead of
-  // it is done.
-  auto exchange = [&](int i, Fold f) {
+  // it is done.  False, for all warps of the block alike, once s_abort is seen: all have sent their pairs for `sent` rows.
+  int sent = 0;
+  auto exchange = [&](int i, Fold& f) {
     f = warp_fold(f, a.c);
     if (G == 1) {
       if (lane == 0) s_all[i & 1][warp] = make_float2(f.m, f.s);
     } else {
-      if (warp == kStreamWarps && lane == 0) sm100::mbar_expect_tx(sm100::smem_u32(&s_pairs[i & 1]), (uint32_t)(G * kPairs * 8));
-      if (lane < G)
-        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
-                     ::"r"(sm100::map_to_cta(sm100::smem_u32(&s_all[i & 1][rank * kPairs + warp]), lane)), "f"(f.m), "f"(f.s),
-                       "r"(sm100::map_to_cta(sm100::smem_u32(&s_pairs[i & 1]), lane)) : "memory");
+      send(i, f.m, f.s);
     }
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * kPairs) : "memory");
+    sent = i + 1;
+    int lost = *reinterpret_cast<volatile int*>(&s_abort);
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %0, 0;\n\tbar.red.or.pred q, 1, %1, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+                 : "+r"(lost) : "n"(32 * kPairs) : "memory");
+    if (lost) return false;
     if (G > 1) wait(&s_pairs[i & 1], (i >> 1) & 1);
     f = Fold();
     for (int j = lane; j < G * kPairs; j += 32) {
@@ -429,7 +448,8 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
       if (o.x > f.m) { f.s = o.y + (f.r > -INFINITY ? f.s * ex2(f.r - orr) : f.s); f.m = o.x; f.r = orr; }
       else f.s += orr > -INFINITY ? o.y * ex2(orr - f.r) : o.y;
     }
-    return warp_fold(f, a.c);
+    f = warp_fold(f, a.c);
+    return true;
   };
   if (warp < kStreamWarps) {
     // ---- the columns
@@ -440,18 +460,19 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
     // what lies behind a part of one is -inf.
     using Vecs = uint4[kStreamFold];
     auto take = [&](auto whole, Vecs& v, int m) {
-      wait(&s_full[stage], phase);
+      const bool here = wait(&s_full[stage], phase);
       const uint4* from = ring + stage * kChunk;
 #pragma unroll
       for (int u = 0; u < kStreamFold; ++u)
         v[u] = decltype(whole)::value || u * kStreamThreads + tid < m ? from[u * kStreamThreads] : make_uint4(none, none, none, none);
       __syncwarp();
-      if (lane == 0) sm100::mbar_arrive(sm100::smem_u32(&s_empty[stage]));
+      if (here && lane == 0) sm100::mbar_arrive(sm100::smem_u32(&s_empty[stage]));     // (otherwise its copy may be under way)
       if (++stage == kStages) { stage = 0; phase ^= 1; }
     };
     auto has = [&](auto whole, int u, int m) { return decltype(whole)::value || u * kStreamThreads + warp * 32 < m; };       // any of the warp
     int C1 = cols_of(1);
     RowPart<T> q = part_of(0, cols_of(0));
+    bool on = true;
     for (int i = 0; i < rows; ++i) {
       const int r = row_at(i), n = q.full - q.v0;
       const float w = GRAD && a.weight ? a.weight[r] : 1.f;
@@ -467,7 +488,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
       int v0 = 0;
       for (; v0 + kChunk <= n; v0 += kChunk) fold(std::true_type(), kChunk);
       if (v0 < n || n == 0) fold(std::false_type(), n - v0);                   // (a part without columns has a chunk, too)
-      f = exchange(i, f);
+      if (!exchange(i, f)) { on = false; break; }
       if (GRAD) {
         const bool zero = !s_teacher[i & 1].some || f.s == 0.f || w == 0.f;
         const float k = w * a.temperature;
@@ -515,7 +536,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
       }
       if (i + 1 < rows) { q = part_of(i + 1, C1); C1 = cols_of(i + 2); }
     }
-    if (GRAD) asm volatile("bar.sync 1, %0;" ::"n"(32 * kPairs) : "memory");
+    if (GRAD && on) asm volatile("bar.sync 1, %0;" ::"n"(32 * kPairs) : "memory");
   } else if (warp == kStreamWarps) {
     // ---- everything else
     // columns outside the vectors, one a lane: in front of them, of the one that the row ends in, behind them
@@ -542,6 +563,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
     int C = cols_of(0), C1 = cols_of(1);
     RowPart<T> q = part_of(0, C);
     prepare(0, C, q);
+    bool on = true;
     for (int i = 0; i < rows; ++i) {
       const int r = row_at(i);
       const float w = GRAD && a.weight ? a.weight[r] : 1.f;
@@ -549,7 +571,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
       const float two[2] = {edge_x, -INFINITY};
       f.raise(edge_x, a.c);
       f.add(two, a.c);
-      f = exchange(i, f);
+      if (!exchange(i, f)) { on = false; break; }
       // (all warps of the block have written the row before's gradient)
       if (GRAD && i > 0) put_teacher<T>(a, s_teacher[(i - 1) & 1], reinterpret_cast<T*>(a.grad) + (size_t)row_at(i - 1) * a.ld);
       StreamTeacher& t = s_teacher[i & 1];
@@ -563,8 +585,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
             if (t.id[j] >= 0 && p != 0.f) loss += p * (t.lp[j] - (fmaf(t.x[j], a.c, -f.r) - ls));
           }
         loss = warp_sum(loss) * kLn2 * a.temperature * a.temperature;
-        const bool lost = *reinterpret_cast<volatile int*>(&s_abort) != 0;
-        if (lane == 0) { a.loss[r] = lost ? NAN : loss; a.lse[r] = lost ? NAN : f.s == 0.f ? -INFINITY : fmaf(f.m, a.inv_t, ls * kLn2); }
+        if (lane == 0) { a.loss[r] = loss; a.lse[r] = f.s == 0.f ? -INFINITY : fmaf(f.m, a.inv_t, ls * kLn2); }
       }
       if (GRAD) {
         const bool zero = !live || w == 0.f;
@@ -579,7 +600,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
         prepare(i + 1, C, q);
       }
     }
-    if (GRAD) {
+    if (GRAD && on) {
       asm volatile("bar.sync 1, %0;" ::"n"(32 * kPairs) : "memory");
       put_teacher<T>(a, s_teacher[(rows - 1) & 1], reinterpret_cast<T*>(a.grad) + (size_t)row_at(rows - 1) * a.ld);
     }
@@ -587,29 +608,62 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
     // ---- the copies
     int stage = 0, phase = 1;                              // (a stage that was never filled is empty)
     int C1 = cols_of(0);
-    for (int i = 0; i < rows; ++i) {
+    bool on = true;
+    unsigned filled = 0;                                   // chunks; chunk k is in stage k % kStages
+    for (int i = 0; i < rows && on; ++i) {
       const RowPart<T> q = part_of(i, C1);
       C1 = cols_of(i + 1);
       const uint4* lv = reinterpret_cast<const uint4*>(q.l + q.head) + q.v0;
       const int n = q.full - q.v0;
-      for (int pass = 0; pass < (GRAD ? 2 : 1); ++pass)
+      for (int pass = 0; pass < (GRAD ? 2 : 1) && on; ++pass)
         for (int v0 = 0; v0 < n || (n == 0 && v0 == 0); v0 += kChunk) {
-          wait(&s_empty[stage], phase);
+          on = wait(&s_empty[stage], phase);
+          if (!on) break;
           const int m = min(kChunk, n - v0);
           if (lane == 0) {
             const uint32_t bar = sm100::smem_u32(&s_full[stage]);
             if (m <= 0) sm100::mbar_arrive(bar);           // (a part without columns)
-            else if (!*reinterpret_cast<volatile int*>(&s_abort)) {
+            else {
               sm100::mbar_expect_tx(bar, (uint32_t)m * 16u);
               asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                            ::"r"(sm100::smem_u32(smem) + (uint32_t)(stage * kChunk) * 16u), "l"(lv + v0), "r"((uint32_t)m * 16u), "r"(bar) : "memory");
             }
           }
           __syncwarp();
+          ++filled;
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
     }
-    // (the block's shared memory outlives the copies: the columns' warps wait for each of them)
+    // the block's shared memory outlives the copies, whether or not the columns' warps still wait for them
+    for (unsigned k = filled < kStages ? 0u : filled - kStages; k < filled; ++k) sm100::mbar_drain(sm100::smem_u32(&s_full[k % kStages]), (k / kStages) & 1u);
+  }
+  // ---- the end: no block leaves before all of its cluster have stopped sending to it
+  __syncwarp();
+  if (G > 1) {
+    if (warp == 0) { to_block(&s_sent[rank], sent); __syncwarp(); }
+    sm100::cluster_sync_all();
+  } else {
+    __syncthreads();
+  }
+  if (!s_abort) return;
+  if (G > 1 && warp < kPairs) {
+    // A block has sent its pairs for at most two rows more than another (the first of them is not waited for successfully).
+    // All send what is missing, so that every exchange that was begun completes, and wait for the last two: what is
+    // under way to a block then has arrived.
+    int last = 0;
+    for (int j = 0; j < G; ++j) last = max(last, s_sent[j]);
+    for (int i = sent; i < last; ++i) {
+      if (i >= 2) sm100::mbar_drain(sm100::smem_u32(&s_pairs[i & 1]), (uint32_t)((i - 2) >> 1) & 1u);
+      __syncwarp();
+      send(i, NAN, NAN);
+    }
+    for (int i = max(0, last - 2); i < last; ++i) sm100::mbar_drain(sm100::smem_u32(&s_pairs[i & 1]), (uint32_t)(i >> 1) & 1u);
+  }
+  for (int i = 0; i < rows; ++i) {
+    const int r = row_at(i);
+    const RowPart<T> q = part_of(i, 0);
+    if (GRAD) for (int c = q.c0 + tid; c < q.c1; c += kStreamThreads + 64) (reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld)[c] = from_f32<T>(NAN);
+    if (rank == 0 && tid == 0 && a.loss) a.loss[r] = a.lse[r] = NAN;
   }
 }
 
@@ -763,6 +817,8 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
 
 namespace {
 
+std::atomic<unsigned long long> g_wait_ns{sm100::kWaitLimitNs};
+
 int fail_arg(const char* msg) { set_last_error(msg); return Z2Z_ERR_INVALID_ARG; }
 
 int check_distill(const void* logits, int dtype, int N, int cols, int64_t ld, const int32_t* ids, const float* t, int K, float temperature,
@@ -871,13 +927,19 @@ DistillArgs distill_args(const void* logits, int cols, int64_t ld, const int32_t
                          const float* weight, float* loss, float* lse, const float* old_lse, void* grad) {
   const int skew = grad && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(logits)) & 15) ? 1 : 0;
   return DistillArgs{logits, cols, ld, n_cols, ids, t, K, 1.f / temperature, temperature, (float)(1.4426950408889634 / (double)temperature),
-                     weight, loss, lse, old_lse, grad, skew, (int)teacher_bytes(K, grad != nullptr)};
+                     weight, loss, lse, old_lse, grad, skew, (int)teacher_bytes(K, grad != nullptr), g_wait_ns.load(std::memory_order_relaxed)};
 }
 }  // namespace
 
 }  // namespace z2z
 
 extern "C" {
+
+int32_t z2z_set_distill_wait_limit(int64_t ns) {
+  if (ns < 0) return z2z::fail_arg("ns < 0");
+  z2z::g_wait_ns.store(ns ? (unsigned long long)ns : z2z::sm100::kWaitLimitNs, std::memory_order_relaxed);
+  return Z2Z_OK;
+}
 
 int32_t z2z_distill_loss(const void* d_logits, int32_t dtype, int32_t N, int32_t cols, int64_t ld,
                          const int32_t* d_n_cols, const int32_t* d_teacher_ids,

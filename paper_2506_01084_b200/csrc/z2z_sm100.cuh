@@ -63,24 +63,33 @@ __device__ __forceinline__ unsigned long long global_ns() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// Bounded wait: gives up after kWaitLimitNs (or kSpinLimit probes), or once another role raised
+// Bounded wait: gives up after limit_ns (or kSpinLimit probes), or once another role raised
 // the abort flag.  Returns false on give-up (and raises the flag), so that every role can leave
 // its loop, the CTA can free its tensor memory and the kernel can end with an error word instead
 // of hanging.
 constexpr uint32_t kSpinLimit = 1u << 26;
 constexpr unsigned long long kWaitLimitNs = 400ull * 1000 * 1000;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                          unsigned long long limit_ns = kWaitLimitNs) {
   if (mbar_try_wait(bar, parity)) return true;
-  const unsigned long long t0 = global_ns();
-  for (uint32_t it = 0; it < kSpinLimit; ++it) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if ((it & 31u) == 31u) {
-      if (*abort_flag) return false;
-      if (global_ns() - t0 > kWaitLimitNs) break;
+  if (limit_ns >= 1000) {                           // (a probe itself may take a microsecond)
+    const uint32_t every = limit_ns < 1000000 ? 0u : 31u;
+    const unsigned long long t0 = global_ns();
+    for (uint32_t it = 0; it < kSpinLimit; ++it) {
+      if (mbar_try_wait(bar, parity)) return true;
+      if ((it & every) == every) {
+        if (*abort_flag) return false;
+        if (global_ns() - t0 > limit_ns) break;
+      }
     }
   }
   *abort_flag = 1;
   return false;
+}
+// Bounded wait of a role that is leaving anyway: for copies that must have ended before the block does.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+  int left = 0;
+  mbar_wait(bar, parity, &left);
 }
 
 // The same for a whole warp, with one answer for all lanes.
