@@ -15,7 +15,7 @@
 // the exponent.
 // Exponents are kept base 2: z = c x - r with c = log2(e) / T, one fused operation, and r the rounded product of c with
 // the maximum.  What r's rounding does to the terms it does to their sum, so that it drops out of q; it stays in lse, at
-// one rounding of m / T.
+// one rounding of m / T.  Where |r| reaches kFar, whose rounding may be any number of powers of two, z = c (x - m) in two.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -113,35 +113,59 @@ template <typename T, int n> __device__ __forceinline__ float max_of(const uint4
   return fmaxf(__low2float(t), __high2float(t));
 }
 
-// Running maximum m and s = sum of 2^(c x - c m).  What is at or below kMasked (the lowest value of either type, -inf),
-// or has a product with c beyond the type's range, adds nothing; NaN and +inf make s NaN.  As long as there is nothing
-// visible m is kMasked and s 0, or NaN.
+// Running maximum m and s = sum of 2^(c x - c m).  What is at or below kMasked (the lowest value of either type, -inf) adds
+// nothing; NaN and +inf make s NaN.  As long as there is nothing visible m is kMasked and s 0, or NaN.
 constexpr float kMasked = -8.507059173023462e37f;          // -2^126
-__device__ __forceinline__ float ref_of(float m, float c) { return m > kMasked ? c * m : -INFINITY; }
+constexpr float kFar = 4096.f;
+__device__ __forceinline__ float ref_of(float m, float c) {
+  const float r = c * m;
+  return !(m > kMasked) ? -INFINITY : fabsf(r) < kFar ? r : NAN;
+}
 struct Fold {
-  float m = kMasked, r = -INFINITY, s = 0.f;               // r = ref_of(m, c)
+  float m = kMasked, r = -INFINITY, s = 0.f;               // r = ref_of(m, c): -inf without anything visible, NaN for a far maximum
+  __device__ __forceinline__ bool near() const { return fabsf(r) < kFar; }
+  // c (x - m)
+  __device__ __forceinline__ float z(float x, float c) const { return near() ? fmaf(x, c, -r) : (x - m) * c; }
+  // What a sum that goes by this maximum becomes by that one, not below it (near sums go by r itself).
+  __device__ __forceinline__ float to(float m2, float r2, float c) const {
+    if (near() && fabsf(r2) < kFar) return ex2(r - r2);
+    return ex2((m - m2) * c - (near() ? fmaf(m, c, -r) : 0.f) + (fabsf(r2) < kFar ? fmaf(m2, c, -r2) : 0.f));
+  }
   __device__ __forceinline__ void raise(float top, float c) {
-    if (top > m && c * top > -INFINITY) {
-      const float r2 = c * top;
-      if (r > -INFINITY) s *= ex2(r - r2);
-      m = top; r = r2;
+    if (!(top > m)) return;
+    float r2 = c * top;
+    if (near() && fabsf(r2) < kFar) {
+      s *= ex2(r - r2);
+    } else {
+      r2 = ref_of(top, c);
+      if (m > kMasked) s *= to(top, r2, c);
     }
+    m = top; r = r2;
   }
   // (behind raise: no x is above m)
-  template <int n> __device__ __forceinline__ void add(const float (&x)[n], float c) {
-    if (r == -INFINITY) {
-#pragma unroll
-      for (int i = 0; i < n; ++i) s += x[i] == x[i] ? 0.f : x[i];
-      return;
-    }
+  template <bool NEAR, int n> __device__ __forceinline__ void add(const float (&x)[n], float c) {
     float e[n];
 #pragma unroll
-    for (int i = 0; i < n; ++i) e[i] = ex2(fmaf(x[i], c, -r));
+    for (int i = 0; i < n; ++i) e[i] = NEAR ? ex2(fmaf(x[i], c, -r)) : m > kMasked ? ex2(z(x[i], c)) : x[i] == x[i] ? 0.f : x[i];
 #pragma unroll
     for (int w = n / 2; w > 0; w /= 2)
 #pragma unroll
       for (int i = 0; i < w; ++i) e[i] += e[i + w];
     s += e[0];
+  }
+  // The vectors that `has` names, all of one kind of maximum.
+  template <typename T, int n, typename H> __device__ __forceinline__ void add_vecs(const uint4 (&v)[n], float c, H has) {
+    auto all = [&](auto is_near) {
+#pragma unroll
+      for (int u = 0; u < n; ++u)
+        if (has(u)) { float x[kPer<T>]; unpack<T>(v[u], x); add<decltype(is_near)::value>(x, c); }
+    };
+    if (near()) all(std::true_type()); else all(std::false_type());
+  }
+  __device__ __forceinline__ void merge(const float2& o, float c) {            // o: another one's m and s
+    const Fold b{o.x, ref_of(o.x, c), o.y};
+    if (b.m > m) { s = b.s + (m > kMasked ? s * to(b.m, b.r, c) : s); m = b.m; r = b.r; }
+    else s += b.m > kMasked ? b.s * b.to(m, r, c) : b.s;
   }
 };
 __device__ __forceinline__ float warp_max(float v) {
@@ -159,7 +183,7 @@ __device__ __forceinline__ Fold warp_fold(Fold f, float c) {
   Fold t;
   t.m = warp_max(f.m);
   t.r = ref_of(t.m, c);
-  t.s = warp_sum(f.r > -INFINITY ? f.s * ex2(f.r - t.r) : f.s);
+  t.s = warp_sum(f.m > kMasked ? f.s * f.to(t.m, t.r, c) : f.s);
   return t;
 }
 
@@ -351,7 +375,7 @@ __device__ __forceinline__ void finish_teacher(const DistillArgs& a, StreamTeach
   for (int j = lane, b = 0; j < a.K; j += 32, ++b) {
     const int id = t.id[j] & kIdMask;
     if (zero || t.id[j] < 0 || (t.id[j] & kLater) || id < t.c0 || id >= t.c1) continue;
-    t.x[j] = k * (ex2(fmaf(t.x[j], a.c, -f.r)) / f.s - v.p_of(j, t.id[j]));
+    t.x[j] = k * (ex2(f.z(t.x[j], a.c)) / f.s - v.p_of(j, t.id[j]));
     write |= 1u << b;
   }
   __syncwarp();
@@ -442,12 +466,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
     if (lost) return false;
     if (G > 1) wait(&s_pairs[i & 1], (i >> 1) & 1);
     f = Fold();
-    for (int j = lane; j < G * kPairs; j += 32) {
-      const float2 o = s_all[i & 1][j];
-      const float orr = ref_of(o.x, a.c);
-      if (o.x > f.m) { f.s = o.y + (f.r > -INFINITY ? f.s * ex2(f.r - orr) : f.s); f.m = o.x; f.r = orr; }
-      else f.s += orr > -INFINITY ? o.y * ex2(orr - f.r) : o.y;
-    }
+    for (int j = lane; j < G * kPairs; j += 32) f.merge(s_all[i & 1][j], a.c);
     f = warp_fold(f, a.c);
     return true;
   };
@@ -481,9 +500,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
         Vecs v;
         take(whole, v, m);
         f.raise(max_of<T>(v), a.c);
-#pragma unroll
-        for (int u = 0; u < kStreamFold; ++u)
-          if (has(whole, u, m)) { float x[kN]; unpack<T>(v[u], x); f.add(x, a.c); }
+        f.add_vecs<T>(v, a.c, [&](int u) { return has(whole, u, m); });
       };
       int v0 = 0;
       for (; v0 + kChunk <= n; v0 += kChunk) fold(std::true_type(), kChunk);
@@ -492,8 +509,9 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
       if (GRAD) {
         const bool zero = !s_teacher[i & 1].some || f.s == 0.f || w == 0.f;
         const float k = w * a.temperature;
-        // k q: in bf16 with the factor in the exponent (an error of some 2^-19, to a step of 2^-8), otherwise as a product
-        const bool in_exponent = sizeof(T) == 2 && k > 0.f;
+        // k q: in bf16 with the factor in the exponent, otherwise as a product.  (The sum of r and the factor's logarithm is rounded once
+        // more than the normaliser's r: an error of 2^-24 of it, at most 2^-12 of q below kFar, to a rounding of 2^-8.)
+        const bool far = !f.near(), in_exponent = sizeof(T) == 2 && k > 0.f && !far;
         const float kq = zero ? 0.f : in_exponent ? 1.f : k / f.s;
         const float off = in_exponent ? f.r + (log2f(f.s) - log2f(k)) : f.r;
         T* out = reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld + q.head;
@@ -513,7 +531,10 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
             float x[kN];
             unpack<T>(v[u], x);
 #pragma unroll
-            for (int e = 0; e < kN; ++e) { x[e] = ex2(fmaf(x[e], a.c, -off)); if (decltype(scaled)::value) x[e] *= kq; }
+            for (int e = 0; e < kN; ++e) {
+              x[e] = ex2(!decltype(whole)::value && far ? (x[e] - f.m) * a.c : fmaf(x[e], a.c, -off));
+              if (decltype(scaled)::value) x[e] *= kq;
+            }
             if (!decltype(whole)::value) {
               if (zero) {
 #pragma unroll
@@ -526,7 +547,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
           }
         };
         v0 = 0;
-        const bool plain = !zero && !a.grad_skew;          // (rows of zeros, and gradients aligned otherwise, take the chunks in part)
+        const bool plain = !zero && !a.grad_skew && !far;  // (the other rows take the chunks in part)
         for (; plain && v0 + kChunk <= n; v0 += kChunk) {
           if (in_exponent) columns(std::true_type(), std::integral_constant<bool, sizeof(T) == 4>(), kChunk);
           else columns(std::true_type(), std::true_type(), kChunk);
@@ -570,7 +591,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
       Fold f;
       const float two[2] = {edge_x, -INFINITY};
       f.raise(edge_x, a.c);
-      f.add(two, a.c);
+      f.add<false>(two, a.c);
       if (!exchange(i, f)) { on = false; break; }
       // (all warps of the block have written the row before's gradient)
       if (GRAD && i > 0) put_teacher<T>(a, s_teacher[(i - 1) & 1], reinterpret_cast<T*>(a.grad) + (size_t)row_at(i - 1) * a.ld);
@@ -582,7 +603,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
         if (live)
           for (int j = lane; j < a.K; j += 32) {
             const float p = t.p[j];
-            if (t.id[j] >= 0 && p != 0.f) loss += p * (t.lp[j] - (fmaf(t.x[j], a.c, -f.r) - ls));
+            if (t.id[j] >= 0 && p != 0.f) loss += p * (t.lp[j] - (f.z(t.x[j], a.c) - ls));
           }
         loss = warp_sum(loss) * kLn2 * a.temperature * a.temperature;
         if (lane == 0) { a.loss[r] = loss; a.lse[r] = f.s == 0.f ? -INFINITY : fmaf(f.m, a.inv_t, ls * kLn2); }
@@ -591,7 +612,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
         const bool zero = !live || w == 0.f;
         const float k = w * a.temperature;
         const int e = edge_of(q);
-        if (e >= 0) (reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld)[e] = from_f32<T>(zero || e >= C ? 0.f : k * (ex2(fmaf(edge_x, a.c, -f.r)) / f.s));
+        if (e >= 0) (reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld)[e] = from_f32<T>(zero || e >= C ? 0.f : k * (ex2(f.z(edge_x, a.c)) / f.s));
         finish_teacher(a, t, view_of(t), zero, k, f);
       }
       if (i + 1 < rows) {
@@ -724,7 +745,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   {
     const float two[2] = {my_x, part_x};
     f.raise(fmaxf(my_x, part_x), a.c);
-    f.add(two, a.c);
+    f.add<false>(two, a.c);
   }
   for (int g = 0; g < groups; ++g) {
     uint4 v[kFold];
@@ -735,10 +756,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
       v[u] = v0 + i < full ? (HOLD ? hold[i] : lv[v0 + i]) : make_uint4(none, none, none, none);
     }
     f.raise(max_of<T>(v), a.c);
-#pragma unroll
-    for (int u = 0; u < kFold; ++u) {
-      if (v0 + (g * kFold + u) * threads + tid < full) { float x[kN]; unpack<T>(v[u], x); f.add(x, a.c); }
-    }
+    f.add_vecs<T>(v, a.c, [&](int u) { return v0 + (g * kFold + u) * threads + tid < full; });
   }
   f = warp_fold(f, a.c);
   if (G > 1) {
@@ -750,12 +768,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
     __syncthreads();
   }
   f = Fold();
-  for (int i = lane; i < G * warps; i += 32) {
-    const float2 o = s_all[i];
-    const float orr = ref_of(o.x, a.c);
-    if (o.x > f.m) { f.s = o.y + (f.r > -INFINITY ? f.s * ex2(f.r - orr) : f.s); f.m = o.x; f.r = orr; }
-    else f.s += orr > -INFINITY ? o.y * ex2(orr - f.r) : o.y;
-  }
+  for (int i = lane; i < G * warps; i += 32) f.merge(s_all[i], a.c);
   f = warp_fold(f, a.c);
   const bool live = f.s != 0.f && s_some;
   const float ls = log2f(f.s);
@@ -764,7 +777,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
     if (live) {
       for (int j = lane; j < a.K; j += 32) {
         const float p = tv.p[j];
-        if (tv.id[j] >= 0 && p != 0.f) loss += p * (tv.lp[j] - (fmaf(tv.x[j], a.c, -f.r) - ls));
+        if (tv.id[j] >= 0 && p != 0.f) loss += p * (tv.lp[j] - (f.z(tv.x[j], a.c) - ls));
       }
       loss = warp_sum(loss) * kLn2 * a.temperature * a.temperature;
     }
@@ -775,10 +788,10 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   const float w = a.weight ? a.weight[r] : 1.f, k = w * a.temperature;
   const bool zero = !live || w == 0.f;
   T* out = reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld;
-  // k q: in bf16 with the factor in the exponent (an error of some 2^-19, to a step of 2^-8), otherwise as a product
-  const bool in_exponent = sizeof(T) == 2 && k > 0.f;
+  // k q: in bf16 with the factor in the exponent, otherwise as a product (see k_distill_stream)
+  const bool in_exponent = sizeof(T) == 2 && k > 0.f && f.near();
   const float kq = in_exponent ? 1.f : k / f.s, off = in_exponent ? f.r + (ls - log2f(k)) : f.r;
-  auto value = [&](float x) { return ex2(fmaf(x, a.c, -off)) * kq; };
+  auto value = [&](float x) { return ex2(in_exponent ? fmaf(x, a.c, -off) : f.z(x, a.c)) * kq; };
   if (my_col >= 0) out[my_col] = from_f32<T>(zero || my_col >= C ? 0.f : value(my_x));
   if (full < v1 && tid < kN) out[part + tid] = from_f32<T>(zero || tid >= part_n ? 0.f : value(part_x));
   uint4* ov = reinterpret_cast<uint4*>(out + sp.head) + v0;
@@ -790,17 +803,22 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
       for (int u = 0; u < kN; ++u) out[sp.head + (v0 + i) * kN + u] = from_f32<T>(x[u]);
     }
   };
-  auto columns = [&](auto scaled) {
+  auto columns = [&](auto scaled, auto far) {
 #pragma unroll 4
     for (int i = tid; i < n_full; i += threads) {
       float x[kN];
       unpack<T>(HOLD ? hold[i] : lv[v0 + i], x);
 #pragma unroll
-      for (int u = 0; u < kN; ++u) x[u] = decltype(scaled)::value ? value(x[u]) : ex2(fmaf(x[u], a.c, -off));
+      for (int u = 0; u < kN; ++u) {
+        x[u] = ex2(decltype(far)::value ? (x[u] - f.m) * a.c : fmaf(x[u], a.c, -off));
+        if (decltype(scaled)::value) x[u] *= kq;
+      }
       put(i, x);
     }
   };
-  if (in_exponent) columns(std::false_type()); else columns(std::true_type());
+  if (!f.near()) columns(std::true_type(), std::true_type());
+  else if (in_exponent) columns(std::false_type(), std::false_type());
+  else columns(std::true_type(), std::false_type());
   const float nothing[kN] = {};
   for (int i = n_full + tid; i < v1 - v0; i += threads) if (zero || v0 + i != full) put(i, nothing);
   if (zero) return;
@@ -811,7 +829,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
     if (tv.id[j] < 0 || (tv.id[j] & kLater) || id < c0 || id >= c1) continue;
     const float p = tv.p_of(j, tv.id[j]);
     const float x = rank != 0 && held(id) ? to_f32<T>(reinterpret_cast<const T*>(hold)[id - sp.head - v0 * kN]) : tv.x[j];
-    out[id] = from_f32<T>(k * (ex2(fmaf(x, a.c, -f.r)) / f.s - p));
+    out[id] = from_f32<T>(k * (ex2(f.z(x, a.c)) / f.s - p));
   }
 }
 
