@@ -236,15 +236,14 @@ __device__ __forceinline__ bool load_teacher(const DistillArgs& a, int r, int C,
   }
   tm = warp_max(tm);
   if (tm == -INFINITY) { __syncwarp(); return false; }
-  const float ref = a.c * tm;
   float s = 0.f;
-  for (int j = lane; j < a.K; j += 32) if (v.id[j] >= 0) s += ex2(fmaf(v.p[j], a.c, -ref));
+  for (int j = lane; j < a.K; j += 32) if (v.id[j] >= 0) s += ex2((v.p[j] - tm) * a.c);
   s = warp_sum(s);
   const float lg = log2f(s), inv = 1.f / s;
   for (int j = lane; j < a.K; j += 32)
     if (v.id[j] >= 0) {
       // (log2 p_j from the teacher's logit, which is exact where p_j is not)
-      const float z = fmaf(v.p[j], a.c, -ref);
+      const float z = (v.p[j] - tm) * a.c;
       v.p[j] = ex2(z) * inv; v.lp[j] = z - lg;
     }
   __syncwarp();
