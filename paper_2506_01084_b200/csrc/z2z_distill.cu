@@ -364,6 +364,25 @@ constexpr int kPairs = kStreamWarps + 1;                   // warps that meet in
 constexpr int kChunk = kStreamFold * kStreamThreads;       // vectors of a chunk, at most
 constexpr size_t kLiveBytes = (size_t)40 << 20;
 
+// One warp: the row's loss, T^2 sum_j p_j (log p_j - log q_j), with ls = log2 s.  The logarithm of a column of the lowest value fits
+// its type, but not in base 2: a sum that becomes infinite is taken again in nats.
+__device__ __forceinline__ float loss_of(const DistillArgs& a, const int* id, const float* p, const float* lp, const float* x, const Fold& f, float ls) {
+  float loss = 0.f;
+  for (int j = threadIdx.x & 31; j < a.K; j += 32) {
+    const float pj = p[j];
+    if (id[j] >= 0 && pj != 0.f) loss += pj * (lp[j] - (f.z(x[j], a.c) - ls));
+  }
+  loss = warp_sum(loss) * kLn2;
+  if (loss == INFINITY) {
+    loss = 0.f;
+#pragma unroll 1
+    for (int j = threadIdx.x & 31; j < a.K; j += 32)
+      if (id[j] >= 0 && p[j] != 0.f) loss += p[j] * ((lp[j] + ls) * kLn2 - (x[j] - f.m) * a.inv_t);
+    loss = warp_sum(loss);
+  }
+  return loss * a.temperature * a.temperature;
+}
+
 struct StreamTeacher { int id[kStreamK]; float p[kStreamK], lp[kStreamK], x[kStreamK]; int some, c0, c1; };
 
 // One warp: x becomes the gradient in this block's teacher columns, k (q - sum of p), with the sum in a column's first entry;
@@ -598,13 +617,7 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
       const bool live = t.some && f.s != 0.f;
       const float ls = log2f(f.s);
       if (rank == 0 && a.loss) {
-        float loss = 0.f;
-        if (live)
-          for (int j = lane; j < a.K; j += 32) {
-            const float p = t.p[j];
-            if (t.id[j] >= 0 && p != 0.f) loss += p * (t.lp[j] - (f.z(t.x[j], a.c) - ls));
-          }
-        loss = warp_sum(loss) * kLn2 * a.temperature * a.temperature;
+        const float loss = live ? loss_of(a, t.id, t.p, t.lp, t.x, f, ls) : 0.f;
         if (lane == 0) { a.loss[r] = loss; a.lse[r] = f.s == 0.f ? -INFINITY : fmaf(f.m, a.inv_t, ls * kLn2); }
       }
       if (GRAD) {
@@ -772,14 +785,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   const bool live = f.s != 0.f && s_some;
   const float ls = log2f(f.s);
   if (rank == 0 && warp == 0 && a.loss) {
-    float loss = 0.f;
-    if (live) {
-      for (int j = lane; j < a.K; j += 32) {
-        const float p = tv.p[j];
-        if (tv.id[j] >= 0 && p != 0.f) loss += p * (tv.lp[j] - (f.z(tv.x[j], a.c) - ls));
-      }
-      loss = warp_sum(loss) * kLn2 * a.temperature * a.temperature;
-    }
+    const float loss = live ? loss_of(a, tv.id, tv.p, tv.lp, tv.x, f, ls) : 0.f;
     if (lane == 0) { a.loss[r] = loss; a.lse[r] = f.s == 0.f ? -INFINITY : fmaf(f.m, a.inv_t, ls * kLn2); }
   }
   if (!GRAD) return;

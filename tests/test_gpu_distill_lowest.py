@@ -53,3 +53,24 @@ def test_teachers_logits_at_the_ends_of_the_type(dt, T, N, cols):
     t[5, 0] = TOP
     t[6] = [-1e30, -1e30, LOW, LOW, -np.inf]
     check(l, ids, t, T)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [1.0, 2.0])
+@pytest.mark.parametrize("N,cols", [(8, 1003), (80, 70003)])
+def test_teachers_columns_that_the_student_masks_with_the_lowest_value(dt, T, N, cols):
+    rng = np.random.default_rng(cols + 1)
+    l = (torch.from_numpy(rng.standard_normal((N, cols)).astype(np.float32))).to(dt)
+    ids = np.stack([rng.choice(cols, 6, replace=False) for _ in range(N)])
+    t = rng.standard_normal((N, 6)) * 0.1                    # a sixth each, about
+    low = torch.finfo(dt).min
+    l[0, ids[0, 2]] = low
+    l[1, ids[1, :2]] = low
+    l[3] = low
+    l[3, ids[3, 5]] = 2.0                                    # one column left
+    t[3, :5] -= 20.0
+    l[4] = low
+    l[4, (ids[4, 0] + 1) % cols] = -5.0
+    ids[4, 1] = (ids[4, 0] + 1) % cols
+    t[4] = [-1.0, 0.0, -np.inf, -np.inf, -np.inf, -np.inf]
+    check(l, ids, t, T)
