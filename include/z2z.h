@@ -325,7 +325,7 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  * sequences g * beams .. (g + 1) * beams - 1; B is a multiple of beams, 1 <= beams <= 32.
  * z2z_beam_select picks the `beams` best continuations of every group.  A live beam b offers its columns c in
  * [0, V + n_b) with s = score_b + (l_c - lse_b), computed in fp64; a finished one offers itself, unchanged.
- * What has s = -inf or NaN is no candidate (a dead beam has score -inf).  Order: higher s, then lower
+ * What has s = -inf, once rounded to fp32, or NaN is no candidate (a dead beam has score -inf).  Order: higher s, then lower
  * sequence, then higher logit, then lower column.
  * The winners are dealt to the group's slots so that the best continuation of a beam stays in its slot and the
  * others, in order, take the slots of beams that have none: what z2z_beam_reorder then has to copy is never

@@ -1,7 +1,7 @@
 """CPU oracle: one step of beam search over joint vocabularies (TEST INFRASTRUCTURE ONLY).
 
 A live beam b offers its columns c with s = score_b + (l_c - lse_b) in fp64, a finished one offers itself; what has
-s = -inf or NaN is no candidate.  The best `beams` of a group win, ordered by higher s, lower beam, higher logit,
+s = -inf, once rounded to fp32, or NaN is no candidate.  The best `beams` of a group win, ordered by higher s, lower beam, higher logit,
 lower column.  A parent's best continuation stays in the parent's slot, the others take the group's free slots in
 order; slots without one are dead.
 
@@ -28,9 +28,9 @@ def select(beams: int, rows: Sequence[np.ndarray], lse, scores, finished: Option
                     cand.append((-float(scores[b]), b, 0.0, -1))
                 continue
             l = np.asarray(rows[b]).astype(np.float64)
-            with np.errstate(invalid="ignore"):
+            with np.errstate(invalid="ignore", over="ignore"):
                 s = float(scores[b]) + (l - float(lse[b]))
-            s = np.where(s > -np.inf, s, -np.inf)                # (NaN)
+                s = np.where(s.astype(np.float32) > -np.inf, s, -np.inf)         # (NaN, and sums below fp32's range)
             least = -np.partition(-s, beams - 1)[beams - 1] if s.size > beams else -np.inf
             for c in np.flatnonzero((s > -np.inf) & (s >= least)):            # what `beams` others beat cannot win
                 cand.append((-s[c], b, -l[c], int(c)))

@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelBlocks) k_beam_select(CbView 
       c.l = q.x; c.col = __float_as_int(q.y);
       if (c.col >= 0) c.s = sh.score[c.beam] + ((double)c.l - (double)sh.lse[c.beam]);
     }
-    if (!(c.s > -INFINITY)) c.s = -INFINITY;                                   // NaN
+    if (!((float)c.s > -INFINITY)) c.s = -INFINITY;                            // NaN, and what is stored as a dead slot's score
     return c;
   };
   // (the lists' best ones come first: spread over the warps they give a bound that W candidates reach)
