@@ -292,7 +292,8 @@ int32_t z2z_embed_grad(z2z_codebook* cb, const int32_t* d_codes, int32_t N, cons
  *   d_teacher_ids, d_teacher_logits [N, K]: the teacher's columns and its logits for them, in any
  *            order, 0 <= K <= 1024.  An id outside the row's columns (Z2Z_CODE_NONE for shorter lists) is
  *            left out, a logit of -inf has no probability, and what the same column is given twice adds up;
- *   temperature > 0, finite; logits / temperature stay within fp32's range;
+ *   temperature > 0, finite, and log2(e) / temperature finite in fp32 (from 4.3e-39 on); logits / temperature stay within
+ *            fp32's range;
  *   d_loss [N] out, d_lse [N] out: log sum_c exp(l_c / T).
  * A row without columns, or masked throughout (nothing but -inf or values at or below -2^126, such as the
  * lowest of the type: lse = -inf), and a row that is left no teacher entry, has loss 0 and gradient 0.

@@ -842,6 +842,9 @@ namespace {
 
 std::atomic<unsigned long long> g_wait_ns{sm100::kWaitLimitNs};
 
+// c of DistillArgs
+float exponent_of(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
+
 int fail_arg(const char* msg) { set_last_error(msg); return Z2Z_ERR_INVALID_ARG; }
 
 int check_distill(const void* logits, int dtype, int N, int cols, int64_t ld, const int32_t* ids, const float* t, int K, float temperature,
@@ -851,7 +854,7 @@ int check_distill(const void* logits, int dtype, int N, int cols, int64_t ld, co
   if (cols < 1 || cols > (1 << 24)) return fail_arg("need 1 <= cols <= 2^24");
   if (ld < cols) return fail_arg("ld < cols");
   if (K < 0 || K > kDistillMaxK) return fail_arg("need 0 <= K <= 1024");
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return fail_arg("temperature must be > 0 and finite");
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(exponent_of(temperature))) return fail_arg("temperature must be > 0 and finite");
   if (N == 0) return Z2Z_OK;
   if (!logits) return fail_arg("d_logits is NULL");
   if (K > 0 && (!ids || !t)) return fail_arg("d_teacher_ids / d_teacher_logits is NULL");
@@ -949,7 +952,7 @@ cudaError_t launch_loss(const DistillArgs& a, int N, cudaStream_t s) {
 DistillArgs distill_args(const void* logits, int cols, int64_t ld, const int32_t* n_cols, const int32_t* ids, const float* t, int K, float temperature,
                          const float* weight, float* loss, float* lse, const float* old_lse, void* grad) {
   const int skew = grad && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(logits)) & 15) ? 1 : 0;
-  return DistillArgs{logits, cols, ld, n_cols, ids, t, K, 1.f / temperature, temperature, (float)(1.4426950408889634 / (double)temperature),
+  return DistillArgs{logits, cols, ld, n_cols, ids, t, K, 1.f / temperature, temperature, exponent_of(temperature),
                      weight, loss, lse, old_lse, grad, skew, (int)teacher_bytes(K, grad != nullptr), g_wait_ns.load(std::memory_order_relaxed)};
 }
 }  // namespace
