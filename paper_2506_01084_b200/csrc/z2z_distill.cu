@@ -907,12 +907,15 @@ cudaError_t launch_stream(const DistillArgs& a, int N, int log_g, cudaStream_t s
   at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[1].val.programmaticStreamSerializationAllowed = 1;
   lc.attrs = at; lc.numAttrs = 1;
-  // clusters that are resident at one time (those of four and eight leave the rest of a GPC without one)
-  static int fit[4] = {0, 0, 0, 0};
+  // clusters that are resident at one time (those of four and eight leave the rest of a GPC without one); found by the first call,
+  // or by each of several threads that come first
+  static std::atomic<int> fit[4];
   int most = kStreamSlots >> log_g;
   if (log_g > 1) {
-    if (!fit[log_g] && (e = cudaOccupancyMaxActiveClusters(&fit[log_g], kern, &lc)) != cudaSuccess) return e;
-    if (fit[log_g] >= 1 && fit[log_g] < most) most = fit[log_g];
+    int n = fit[log_g].load(std::memory_order_relaxed);
+    if (!n && (e = cudaOccupancyMaxActiveClusters(&n, kern, &lc)) != cudaSuccess) return e;
+    fit[log_g].store(n, std::memory_order_relaxed);
+    if (n >= 1 && n < most) most = n;
   }
   lc.gridDim = dim3((unsigned)((N < most ? N : most) << log_g));
   lc.numAttrs = 2;

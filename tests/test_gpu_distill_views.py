@@ -1,4 +1,7 @@
-"""Gradients whose rows are aligned otherwise than the logits', and calls captured into a graph, in each form: the same bits."""
+"""Gradients whose rows are aligned otherwise than the logits', calls captured into a graph, and calls of several threads at
+once: the same bits."""
+import threading
+
 import pytest
 import torch
 
@@ -69,3 +72,30 @@ def test_the_persistent_form_replayed_from_a_graph(N, cols):
         zb.z2z_distill_loss(l, *args, w, out[2], out[3], g[2])
         zb.z2z_distill_grad(l, *args, out[3], w, g[3])
         assert torch.equal(out[:2], out[2:]) and torch.equal(g[:2], g[2:])
+
+
+def test_calls_of_several_threads_at_once():
+    jobs = [inputs(dt, N, cols) for dt in (torch.bfloat16, torch.float32) for N, cols in ((76, 300007), (81, 580003), (7, 33001))]
+
+    def run(l, args, w):
+        out, g = torch.empty(2, l.shape[0], device=DEV), torch.empty_like(l)
+        zb.z2z_distill_loss(l, *args, w, out[0], out[1], g)
+        return out, g
+
+    want = [run(*j) for j in jobs]
+    torch.cuda.synchronize()
+    got, start = [None] * len(jobs), threading.Barrier(len(jobs))
+
+    def thread(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            start.wait(timeout=30)
+            got[k] = [run(*jobs[k]) for _ in range(3)]
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=thread, args=(k,)) for k in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(timeout=60)
+    for a, many in zip(want, got):
+        assert all(torch.equal(x, y) for b in many for x, y in zip(a, b))
