@@ -121,11 +121,14 @@ __device__ __forceinline__ float ref_of(float m, float c) {
   const float r = c * m;
   return !(m > kMasked) ? -INFINITY : fabsf(r) < kFar ? r : NAN;
 }
+struct Exponent {                                          // z of either form: the product of a near row is one operation on x itself
+  float a, c, b;
+  __device__ __forceinline__ float operator()(float x) const { return fmaf(x - a, c, -b); }
+};
 struct Fold {
   float m = kMasked, r = -INFINITY, s = 0.f;               // r = ref_of(m, c): -inf without anything visible, NaN for a far maximum
   __device__ __forceinline__ bool near() const { return fabsf(r) < kFar; }
-  // c (x - m)
-  __device__ __forceinline__ float z(float x, float c) const { return near() ? fmaf(x, c, -r) : (x - m) * c; }
+  __device__ __forceinline__ Exponent exponent(float c) const { return near() ? Exponent{0.f, c, r} : Exponent{m, c, 0.f}; }
   // What a sum that goes by this maximum becomes by that one, not below it (near sums go by r itself).
   __device__ __forceinline__ float to(float m2, float r2, float c) const {
     if (near() && fabsf(r2) < kFar) return ex2(r - r2);
@@ -146,7 +149,7 @@ struct Fold {
   template <bool NEAR, int n> __device__ __forceinline__ void add(const float (&x)[n], float c) {
     float e[n];
 #pragma unroll
-    for (int i = 0; i < n; ++i) e[i] = NEAR ? ex2(fmaf(x[i], c, -r)) : m > kMasked ? ex2(z(x[i], c)) : x[i] == x[i] ? 0.f : x[i];
+    for (int i = 0; i < n; ++i) e[i] = NEAR ? ex2(fmaf(x[i], c, -r)) : m > kMasked ? ex2(exponent(c)(x[i])) : x[i] == x[i] ? 0.f : x[i];
 #pragma unroll
     for (int w = n / 2; w > 0; w /= 2)
 #pragma unroll
@@ -237,15 +240,14 @@ __device__ __forceinline__ bool load_teacher(const DistillArgs& a, int r, int C,
   tm = warp_max(tm);
   if (tm == -INFINITY) { __syncwarp(); return false; }
   float s = 0.f;
-  for (int j = lane; j < a.K; j += 32) if (v.id[j] >= 0) s += ex2((v.p[j] - tm) * a.c);
+  for (int j = lane; j < a.K; j += 32) s += ex2((v.p[j] - tm) * a.c);                    // (entries that are left out are -inf)
   s = warp_sum(s);
   const float lg = log2f(s), inv = 1.f / s;
-  for (int j = lane; j < a.K; j += 32)
-    if (v.id[j] >= 0) {
-      // (log2 p_j from the teacher's logit, which is exact where p_j is not)
-      const float z = (v.p[j] - tm) * a.c;
-      v.p[j] = ex2(z) * inv; v.lp[j] = z - lg;
-    }
+  for (int j = lane; j < a.K; j += 32) {
+    // (log2 p_j from the teacher's logit, which is exact where p_j is not)
+    const float z = (v.p[j] - tm) * a.c;
+    v.p[j] = ex2(z) * inv; v.lp[j] = z - lg;
+  }
   __syncwarp();
   return true;
 }
@@ -366,18 +368,19 @@ constexpr size_t kLiveBytes = (size_t)40 << 20;
 
 // One warp: the row's loss, T^2 sum_j p_j (log p_j - log q_j), with ls = log2 s.  The logarithm of a column of the lowest value fits
 // its type, but not in base 2: a sum that becomes infinite is taken again in nats.
-__device__ __forceinline__ float loss_of(const DistillArgs& a, const int* id, const float* p, const float* lp, const float* x, const Fold& f, float ls) {
+__device__ __forceinline__ float loss_of(const DistillArgs& a, const float* p, const float* lp, const float* x, const Fold& f, float ls) {
+  const Exponent z = f.exponent(a.c);
   float loss = 0.f;
   for (int j = threadIdx.x & 31; j < a.K; j += 32) {
-    const float pj = p[j];
-    if (id[j] >= 0 && pj != 0.f) loss += pj * (lp[j] - (f.z(x[j], a.c) - ls));
+    const float pj = p[j], term = pj * (lp[j] - (z(x[j]) - ls));
+    loss += pj != 0.f ? term : 0.f;
   }
   loss = warp_sum(loss) * kLn2;
   if (loss == INFINITY) {
     loss = 0.f;
 #pragma unroll 1
     for (int j = threadIdx.x & 31; j < a.K; j += 32)
-      if (id[j] >= 0 && p[j] != 0.f) loss += p[j] * ((lp[j] + ls) * kLn2 - (x[j] - f.m) * a.inv_t);
+      if (p[j] != 0.f) loss += p[j] * ((lp[j] + ls) * kLn2 - (x[j] - f.m) * a.inv_t);
     loss = warp_sum(loss);
   }
   return loss * a.temperature * a.temperature;
@@ -389,11 +392,12 @@ struct StreamTeacher { int id[kStreamK]; float p[kStreamK], lp[kStreamK], x[kStr
 // id becomes -1 where nothing is to be written.
 __device__ __forceinline__ void finish_teacher(const DistillArgs& a, StreamTeacher& t, const TeacherView& v, bool zero, float k, const Fold& f) {
   const int lane = threadIdx.x & 31;
+  const Exponent z = f.exponent(a.c);
   unsigned write = 0u;                                     // bit per entry of this lane
   for (int j = lane, b = 0; j < a.K; j += 32, ++b) {
     const int id = t.id[j] & kIdMask;
     if (zero || t.id[j] < 0 || (t.id[j] & kLater) || id < t.c0 || id >= t.c1) continue;
-    t.x[j] = k * (ex2(f.z(t.x[j], a.c)) / f.s - v.p_of(j, t.id[j]));
+    t.x[j] = k * (ex2(z(t.x[j])) / f.s - v.p_of(j, t.id[j]));
     write |= 1u << b;
   }
   __syncwarp();
@@ -617,14 +621,14 @@ __global__ void __launch_bounds__(kStreamThreads + 64, 1) k_distill_stream(Disti
       const bool live = t.some && f.s != 0.f;
       const float ls = log2f(f.s);
       if (rank == 0 && a.loss) {
-        const float loss = live ? loss_of(a, t.id, t.p, t.lp, t.x, f, ls) : 0.f;
+        const float loss = live ? loss_of(a, t.p, t.lp, t.x, f, ls) : 0.f;
         if (lane == 0) { a.loss[r] = loss; a.lse[r] = f.s == 0.f ? -INFINITY : fmaf(f.m, a.inv_t, ls * kLn2); }
       }
       if (GRAD) {
         const bool zero = !live || w == 0.f;
         const float k = w * a.temperature;
         const int e = edge_of(q);
-        if (e >= 0) (reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld)[e] = from_f32<T>(zero || e >= C ? 0.f : k * (ex2(f.z(edge_x, a.c)) / f.s));
+        if (e >= 0) (reinterpret_cast<T*>(a.grad) + (size_t)r * a.ld)[e] = from_f32<T>(zero || e >= C ? 0.f : k * (ex2(f.exponent(a.c)(edge_x)) / f.s));
         finish_teacher(a, t, view_of(t), zero, k, f);
       }
       if (i + 1 < rows) {
@@ -785,7 +789,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   const bool live = f.s != 0.f && s_some;
   const float ls = log2f(f.s);
   if (rank == 0 && warp == 0 && a.loss) {
-    const float loss = live ? loss_of(a, tv.id, tv.p, tv.lp, tv.x, f, ls) : 0.f;
+    const float loss = live ? loss_of(a, tv.p, tv.lp, tv.x, f, ls) : 0.f;
     if (lane == 0) { a.loss[r] = loss; a.lse[r] = f.s == 0.f ? -INFINITY : fmaf(f.m, a.inv_t, ls * kLn2); }
   }
   if (!GRAD) return;
@@ -796,7 +800,8 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
   // k q: in bf16 with the factor in the exponent, otherwise as a product (see k_distill_stream)
   const bool in_exponent = sizeof(T) == 2 && k > 0.f && f.near();
   const float kq = in_exponent ? 1.f : k / f.s, off = in_exponent ? f.r + (ls - log2f(k)) : f.r;
-  auto value = [&](float x) { return ex2(in_exponent ? fmaf(x, a.c, -off) : f.z(x, a.c)) * kq; };
+  const Exponent z = f.exponent(a.c);
+  auto value = [&](float x) { return ex2(in_exponent ? fmaf(x, a.c, -off) : z(x)) * kq; };
   if (my_col >= 0) out[my_col] = from_f32<T>(zero || my_col >= C ? 0.f : value(my_x));
   if (full < v1 && tid < kN) out[part + tid] = from_f32<T>(zero || tid >= part_n ? 0.f : value(part_x));
   uint4* ov = reinterpret_cast<uint4*>(out + sp.head) + v0;
@@ -834,7 +839,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(DistillArgs a) {
     if (tv.id[j] < 0 || (tv.id[j] & kLater) || id < c0 || id >= c1) continue;
     const float p = tv.p_of(j, tv.id[j]);
     const float x = rank != 0 && held(id) ? to_f32<T>(reinterpret_cast<const T*>(hold)[id - sp.head - v0 * kN]) : tv.x[j];
-    out[id] = from_f32<T>(k * (ex2(f.z(x, a.c)) / f.s - p));
+    out[id] = from_f32<T>(k * (ex2(z(x)) / f.s - p));
   }
 }
 
