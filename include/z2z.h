@@ -171,7 +171,8 @@ int32_t z2z_hyper_embed(z2z_codebook* cb, int32_t which, const void* d_table,
  *            (column/4, row, step), u = ((x >> 9) + 0.5) * 2^-23, g = -log(-log u));
  *   d_targets [N] or NULL -> d_target_logit [N] = logit of that column (NaN if not visible);
  *   d_lse [N], d_argmax [N], d_max_logit [N]; d_sample [N] (required iff select == GUMBEL);
- *   d_logits_debug [N, V + cap] fp32 or NULL: every logit, for tests.                         */
+ *   d_logits_debug [N, V + cap] fp32 or NULL: every logit, for z2z_sample_filtered, z2z_beam_select,
+ *            z2z_distill_loss (columns from V + n_vis on: undefined).                               */
 int32_t z2z_dynamic_logits(z2z_codebook* cb, const void* d_hidden, int32_t N,
                            const int32_t* d_row_seq, const int32_t* d_row_nvis, const void* d_WU,
                            const void* d_Uh, int32_t select, float temperature, uint64_t seed,

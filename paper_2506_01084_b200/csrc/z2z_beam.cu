@@ -10,8 +10,8 @@
 //      maximum reaches it, `beams` of 256 unless logits are equal, have any of them: their columns are read again (from L2),
 //      by a warp for each, and what reaches the bound goes to a list in shared memory;
 //   3. ranks are counted among the list.
-// (Offering every column to the list as it comes, against a bound from the first tile, cost 55 us for 256 beams of 128 k
-// columns instead of 32: nearly every warp has a candidate in nearly every tile.)  Where the list overflows, because many
+// (256 beams of 128 k columns take 32 us; where every column is offered to the list as it comes, against a bound from the first
+// tile, nearly every warp has a candidate in nearly every tile: 55.)  Where the list overflows, because many
 // logits are equal or the best ones lie in few threads, the bound is tightened to the `beams`-th best of what was caught, and
 // step 2 done again.  The last block of a group to finish takes the best of the group's lists and deals them to the slots.
 // Bound by HBM, 4 (V + n_b) bytes a beam; small calls by a chain of some ten reads, barriers and the ticket.
@@ -270,8 +270,8 @@ __global__ void __launch_bounds__(kSelThreads, kSelBlocks) k_beam_select(CbView 
 // ---- reordering ---------------------------------------------------------------------------------------------
 // What moves is cut into pieces of kPiece bytes, whatever it is part of, and dealt to all blocks: only the device knows
 // which sequences move and how long their codebooks are, so that every block numbers the pieces for itself (two reads and a
-// scan of at most 1024 sequences).  Bound by HBM, twice the bytes that move.  (With sixteen blocks for every sequence of the
-// session 96 sequences took 193 us instead of 166, and four 30 instead of 9: most blocks had nothing to do.)
+// scan of at most 1024 sequences).  Bound by HBM, twice the bytes that move.  (96 sequences, half of
+// which move, take 165 us and four 10; with sixteen blocks for every sequence of the session, most of them idle, 193 and 30.)
 namespace {
 constexpr int kMoveThreads = 256;
 constexpr int kPiece = kMoveThreads * 4 * 16;

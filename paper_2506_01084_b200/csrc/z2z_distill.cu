@@ -269,8 +269,8 @@ __device__ __forceinline__ void load_logits(const T* l, const TeacherView& v, in
 // which has one value there, and adds their p up, in order.  Every entry writes its number to a slot that its id gives, and
 // looks who stands there afterwards: an entry of the same column represents it, and with one of another column both
 // of that column's entries go to the next round, with other slots.  A round ends it for a column in every slot that was written.
-// (1024 bf16 rows of 132352 columns with 256 / 512 entries take 121 / 144 us this way, 115 / 120 without looking; 130 / 183 with a
-// table filled by compare-and-swap, 241 / 538 where every entry looked at all others.)
+// (1024 bf16 rows of 132352 columns with 256 / 512 entries take 128 / 148 us, some 6 / 24 of them for this; with a table filled by
+// compare-and-swap it is 15 / 63, where every entry looks at all others 126 / 418.)
 __device__ __forceinline__ void mark_repeats(const TeacherView& v, int K) {
   const int lane = threadIdx.x & 31, shift = 32 - table_bits(K), steps = (K + 31) / 32;
   constexpr unsigned kMul = 2654435769u;                   // (odd, as all the later rounds' are)
@@ -354,13 +354,12 @@ __device__ __forceinline__ void copy_wait(int left) {
 // from the first pass into the second and from there into the next row.  Fifteen warps have the columns, eight vectors of
 // a chunk each; one more has, a row ahead, the teacher, the columns outside the vectors and the loss, and, behind the
 // barrier of the following row, the teacher's columns of the gradient.
-// 2048 bf16 rows of 132352 columns 214 to 226 us by the board, of which the bytes need 163; 700 fp32 rows of 132347, loss and backward
-// pass, 225 (168).  Measured on the way there, us: rows held in the shared memory of clusters of four 291 (a fourth of a row's time
-// in its barrier, a seventh of the SMs without work); two blocks per SM with a row each, 78 MB of live rows, half of whose
-// second read misses L2, 250; the first pass of the next row chunk by chunk in turn with the second one of this, no barrier
-// to wait for but the gradient's lines between a row's two reads, 247; sixteen warps 215 and 237, with chunks of even size 217
-// and 231; thirty warps with four vectors 226; packed pairs of fp32 225.  The loss alone of bf16 rows takes 105, half of
-// which the exponentials need.
+// 2048 bf16 rows of 132352 columns, loss and gradient, 219 to 227 us by the board, of which the bytes need 163; 700 fp32 rows of
+// 132347, loss and backward pass, 228 (168); the loss alone of those bf16 rows 105, half of which the exponentials need.  A row per
+// block and 39 MB of live rows: two blocks per SM with a row each are 78 MB, half of whose second read misses L2 (14 % more
+// time), and rows held in the shared memory of clusters of four leave a seventh of the SMs without work and a fourth of a row's
+// time in its barrier (35 % more).  Fifteen warps of columns beside the two others: sixteen make the fp32 pair 5 % slower, and
+// thirty with four vectors each the bf16 rows 5 %.
 constexpr int kStreamWarps = 15, kStreamThreads = 32 * kStreamWarps, kStreamFold = 8, kStreamK = 512, kStages = 3;
 constexpr int kPairs = kStreamWarps + 1;                   // warps that meet in a row's exchange
 constexpr int kChunk = kStreamFold * kStreamThreads;       // vectors of a chunk, at most
@@ -931,10 +930,11 @@ template <typename T>
 cudaError_t launch_loss(const DistillArgs& a, int N, cudaStream_t s) {
   const size_t row = (size_t)a.cols * sizeof(T);
   // The persistent form from rows on whose exchange is short beside their bytes, and from a row for every two SMs on.  Clusters
-  // against it, us, bf16, loss alone / with the gradient: 1024 rows of 32 KB 15 / 24 against 26 / 53, of 64 KB 22 / 44 against
-  // 32 / 61, of 128 KB 38 / 76 against 38 / 70, of 258 KB 73 / 149 against 56 / 114; 148 rows of 258 KB 14 / 32 against 13 / 23, 74
-  // rows 11 / 17 against 10 / 15, 37 rows 10 / 14 against 10 / 18.  (A longer teacher's list than kStreamK has no room beside
-  // the ring.)
+  // against it, us, loss alone / with the gradient, bf16: 1024 rows of 32 KB 14 / 23 against 24 / 49, of 64 KB 21 / 41 against
+  // 30 / 55, of 128 KB 35 / 71 against 37 / 73, of 258 KB 63 / 138 against 55 / 117; 148 rows of 258 KB 16 / 29 against 13 / 23, 74
+  // rows 11 / 17 against 10 / 16, 37 rows 9 / 13 against 11 / 17.  fp32, in the same order: 13 / 21 against 23 / 42, 20 / 38
+  // against 28 / 49, 34 / 67 against 32 / 62, 59 / 124 against 44 / 102; 13 / 27 against 12 / 20, 9 / 15 against 9 / 14, 8 / 12
+  // against 10 / 16.  (A longer teacher's list than kStreamK has no room beside the ring.)
   if (a.K <= kStreamK && row >= kStreamRow && N >= kStreamSlots / 2) {
     // blocks per row: so many that the rows in work stay in L2, and more where the last round would leave much of the machine idle
     int log_g = 0;

@@ -66,9 +66,9 @@ template <> __device__ __forceinline__ uint4 scaled<__nv_bfloat16>(uint4 v, floa
 }  // namespace
 
 // out[r] = scale * row(codes[r]).  A warp takes kLookupUnroll vectors per lane of a row, all under way at once, so that the
-// few rows of a decode step are spread over as many SMs as they have pieces, and one such piece: with a grid of the
-// resident blocks and a loop every warp waits for its own chain of reads again and again (52800 rows of 4096 bf16 columns
-// 121 us, now 100: 0.95 of the copy rate).
+// few rows of a decode step are spread over as many SMs as they have pieces, and one such piece: in a grid of the
+// resident blocks with a loop every warp waits for its own chain of reads again and again (52800 rows of 4096 bf16 columns
+// take 121 us that way, 100 this way: 0.95 of the copy rate).
 template <typename T>
 __global__ void __launch_bounds__(kLookupThreads) k_embed_lookup_scaled(
     CbView cb, const int32_t* __restrict__ codes, int N, const int32_t* __restrict__ row_seq, const uint4* __restrict__ WE,
