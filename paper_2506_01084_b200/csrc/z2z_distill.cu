@@ -354,7 +354,7 @@ __device__ __forceinline__ void copy_wait(int left) {
 // from the first pass into the second and from there into the next row.  Fifteen warps have the columns, eight vectors of
 // a chunk each; one more has, a row ahead, the teacher, the columns outside the vectors and the loss, and, behind the
 // barrier of the following row, the teacher's columns of the gradient.
-// 2048 bf16 rows of 132352 columns, loss and gradient, 219 to 227 us by the board, of which the bytes need 163; 700 fp32 rows of
+// 2048 bf16 rows of 132352 columns, loss and gradient, 219 to 229 us by the board, of which the bytes need 163; 700 fp32 rows of
 // 132347, loss and backward pass, 228 (168); the loss alone of those bf16 rows 105, half of which the exponentials need.  A row per
 // block and 39 MB of live rows: two blocks per SM with a row each are 78 MB, half of whose second read misses L2 (14 % more
 // time), and rows held in the shared memory of clusters of four leave a seventh of the SMs without work and a fourth of a row's
