@@ -322,6 +322,71 @@ int32_t z2z_distill_grad(const void* d_logits, int32_t dtype, int32_t N, int32_t
  * makes from now on; 0 = the default, 400 ms.  A process that shares its GPU with others in turn may have to wait longer.  */
 int32_t z2z_set_distill_wait_limit(int64_t ns);
 
+/* Cross entropy over the joint vocabulary, from hidden rows and without stored logits: with the columns of row r
+ * (W_U, then the first n_vis rows of its sequence's U_h) as for z2z_dynamic_logits and l its logits,
+ *   loss_r = lse_r - l_{t_r},  lse_r = log sum_c exp(l_c),      d loss_r / d l_c = exp(l_c - lse_r) - [c = t_r].
+ * z2z_xent_loss gives the losses.  z2z_xent_grad is the backward pass on its own: d_grad_loss [N] = w is the
+ * derivative for d_loss, d_lse what z2z_xent_loss left there for the same arguments; it computes the logits again,
+ * in pieces of the vocabulary.  z2z_xent_step is both in one call, with w = d_row_weight (d_loss stays unweighted).
+ *   d_grad_hidden [N, d]       = w_r sum_c (d loss_r / d l_c) row c        in the configured dtype, every row written
+ *   d_grad_WU[v]        (+)= sum_r w_r (d loss_r / d l_v) d_hidden[r]      [V, d] of grad_dtype
+ *   d_grad_Uh[b][k]     (+)= the same over the rows of sequence b          [B, cap, d] of grad_dtype
+ *   d_hidden [N, d], d_row_seq, d_row_nvis, d_WU, d_Uh: as for z2z_dynamic_logits, 16-byte aligned;
+ *   d_targets [N]: a code the row sees.  A row with Z2Z_CODE_NONE, or of no sequence of the session, takes no part:
+ *            loss 0, lse 0, gradient 0, whatever its hidden row holds, and no time.  So does a code that the row
+ *            does not see; it sets Z2Z_ST_BAD_TOKEN for its sequence;
+ *   w [N] or NULL = 1: a row whose weight is 0 has gradient 0 whatever its logits are;
+ *   accumulate  1: added to what the tables' gradients hold, rounded once.  0: every row of d_grad_WU and the n_b
+ *            rows of every sequence of d_grad_Uh are written; rows from n_b on stay as they are either way;
+ *   d_grad_hidden, d_grad_WU, d_grad_Uh: 16-byte aligned, apart from all inputs and one another; each may be NULL.
+ * The row of a NaN or +inf logit has a NaN loss and, with a weight, NaN gradients, which reach the tables' too.
+ * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]) is rounded to bf16 for gradients stored in
+ * bf16 and has 24 bits for fp32 gradients of the tables.  fp32 sessions: fp32's precision throughout.  The same call
+ * gives the same bits.
+ *   d_scratch: 256-byte aligned, at least *out_least bytes of z2z_xent_scratch_bytes (for the session's configuration,
+ *            N and grad_dtype, -1 for z2z_xent_loss alone); up to *out_most, more makes the pieces larger and the call
+ *            faster.  How the sums are cut depends on it.  Its contents need not be kept between calls; calls that
+ *            share it must be ordered by the caller.
+ * N <= 2^20.                                                                                            */
+int32_t z2z_xent_scratch_bytes(const z2z_config* cfg, int32_t N, int32_t grad_dtype, size_t* out_least,
+                               size_t* out_most);
+int32_t z2z_xent_loss(z2z_codebook* cb, const void* d_hidden, int32_t N, const int32_t* d_row_seq,
+                      const int32_t* d_row_nvis, const void* d_WU, const void* d_Uh, const int32_t* d_targets,
+                      float* d_loss, float* d_lse, void* d_scratch, size_t scratch_bytes, z2z_stream stream);
+int32_t z2z_xent_grad(z2z_codebook* cb, const void* d_hidden, int32_t N, const int32_t* d_row_seq,
+                      const int32_t* d_row_nvis, const void* d_WU, const void* d_Uh, const int32_t* d_targets,
+                      const float* d_lse, const float* d_grad_loss, int32_t grad_dtype, int32_t accumulate,
+                      void* d_grad_hidden, void* d_grad_WU, void* d_grad_Uh, void* d_scratch, size_t scratch_bytes,
+                      z2z_stream stream);
+int32_t z2z_xent_step(z2z_codebook* cb, const void* d_hidden, int32_t N, const int32_t* d_row_seq,
+                      const int32_t* d_row_nvis, const void* d_WU, const void* d_Uh, const int32_t* d_targets,
+                      const float* d_row_weight, float* d_loss, float* d_lse, int32_t grad_dtype, int32_t accumulate,
+                      void* d_grad_hidden, void* d_grad_WU, void* d_grad_Uh, void* d_scratch, size_t scratch_bytes,
+                      z2z_stream stream);
+
+/* Global norm of the gradients of a step, and the gradients scaled to a largest norm:
+ *   norm = |scale| sqrt(sum of the squares of all elements of all tensors),
+ *   out = scale min(1, max_norm / (norm + 1e-6)) g, the product taken in fp32 and rounded once.
+ *   h_tensors: n (0 .. 65536) HOST records, read during the call: numel contiguous elements of grad_dtype (Z2Z_DTYPE_*) at
+ *            d_grad, aligned to their elements; d_out: as many of out_dtype, d_grad itself (of the same type; where
+ *            the factor is 1 nothing is written), or NULL: the tensor counts for the norm alone.  Up to 2^43
+ *            elements in all.  Tensors do not overlap one another or another's output;
+ *   scale    finite: what the tensors hold times it is the gradient (1 / micro batches, 1 / loss scale);
+ *   max_norm > 0, +inf: only scaled;
+ *   d_norm [1] out or NULL.
+ * If the norm is not finite (an element is not, or the sum leaves fp32's range) no output is written: the caller sees
+ * it in d_norm and skips the step.  Sums are fp64, in an order fixed by the sizes and alignments.
+ *   d_scratch: 8-byte aligned, at least z2z_grad_clip_scratch_bytes; not kept between calls.               */
+typedef struct {
+  const void* d_grad;
+  void* d_out;
+  int64_t numel;
+  int32_t grad_dtype, out_dtype;
+} z2z_grad_tensor;
+int32_t z2z_grad_clip_scratch_bytes(int32_t n, size_t* out_bytes);
+int32_t z2z_grad_clip(const z2z_grad_tensor* h_tensors, int32_t n, float scale, float max_norm, float* d_norm,
+                      void* d_scratch, size_t scratch_bytes, z2z_stream stream);
+
 /* Beam search over the joint vocabularies (the paper decodes greedily or by sampling).  The beams of a request
  * are `beams` consecutive sequences of the session, each with its own codebook and caches: group g is the
  * sequences g * beams .. (g + 1) * beams - 1; B is a multiple of beams, 1 <= beams <= 32.

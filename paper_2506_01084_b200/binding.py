@@ -30,7 +30,8 @@ EXPORTS = ["z2z_workspace_bytes", "z2z_codebook_init", "z2z_lzw_encode", "z2z_lz
            "z2z_profile_read", "z2z_set_tensor_cores", "z2z_logits_static_scratch",
            "z2z_lzw_decode", "z2z_embed_lookup", "z2z_upload_rows", "z2z_sample_filtered",
            "z2z_set_encoder_half_scratch", "z2z_embed_lookup_scaled", "z2z_embed_grad_scratch_bytes", "z2z_embed_grad",
-           "z2z_distill_loss", "z2z_distill_grad", "z2z_set_distill_wait_limit", "z2z_beam_select", "z2z_beam_reorder"]
+           "z2z_distill_loss", "z2z_distill_grad", "z2z_set_distill_wait_limit", "z2z_beam_select", "z2z_beam_reorder",
+           "z2z_xent_scratch_bytes", "z2z_xent_loss", "z2z_xent_grad", "z2z_xent_step", "z2z_grad_clip_scratch_bytes", "z2z_grad_clip"]
 
 
 class Config(C.Structure):
@@ -46,6 +47,10 @@ class SeqRows(C.Structure):
     _fields_ = [("d_base", C.c_void_p), ("stride", C.c_size_t), ("bytes", C.c_size_t)]
 
 
+class GradTensor(C.Structure):
+    _fields_ = [("d_grad", C.c_void_p), ("d_out", C.c_void_p), ("numel", C.c_int64), ("grad_dtype", C.c_int32), ("out_dtype", C.c_int32)]
+
+
 _P, _I, _F, _L = C.c_void_p, C.c_int32, C.c_float, C.c_int64
 # Argument types of the calls that are made with plain Python numbers (an address of 0 is None).
 _ARGTYPES = {
@@ -54,6 +59,12 @@ _ARGTYPES = {
     "z2z_distill_loss": [_P, _I, _I, _I, _L, _P, _P, _P, _I, _F, _P, _P, _P, _P, _P],
     "z2z_distill_grad": [_P, _I, _I, _I, _L, _P, _P, _P, _I, _F, _P, _P, _P, _P],
     "z2z_set_distill_wait_limit": [_L],
+    "z2z_xent_scratch_bytes": [C.POINTER(Config), _I, _I, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+    "z2z_xent_loss": [_P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P],
+    "z2z_xent_grad": [_P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _I, _I, _P, _P, _P, _P, C.c_size_t, _P],
+    "z2z_xent_step": [_P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _P, _P, _P, _P, C.c_size_t, _P],
+    "z2z_grad_clip_scratch_bytes": [_I, C.POINTER(C.c_size_t)],
+    "z2z_grad_clip": [C.POINTER(GradTensor), _I, _F, _F, _P, _P, C.c_size_t, _P],
     "z2z_beam_select": [_P, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P],
     "z2z_beam_reorder": [_P, _P, _P, _P, _P, _P, C.POINTER(SeqRows), _I, _P],
 }
@@ -331,6 +342,101 @@ def z2z_distill_grad(logits: torch.Tensor, n_cols: Optional[torch.Tensor], teach
 def z2z_set_distill_wait_limit(ns: int):
     """Nanoseconds after which a wait inside the distillation kernels gives up; 0 is the default, 400 ms."""
     _check(lib().z2z_set_distill_wait_limit(ns))
+
+
+def z2z_xent_scratch_bytes(cfg: Config, N: int, grad_dtype: Optional[torch.dtype] = None):
+    """(least, most) bytes of scratch for the cross entropy of N rows: of its losses alone, or with gradients of the tables
+    in fp32 or bf16."""
+    _need(grad_dtype in (None, torch.float32, torch.bfloat16), "grad_dtype must be fp32, bf16 or None")
+    least, most = C.c_size_t(0), C.c_size_t(0)
+    gd = -1 if grad_dtype is None else DTYPE_FP32 if grad_dtype == torch.float32 else DTYPE_BF16
+    _check(lib().z2z_xent_scratch_bytes(C.byref(cfg), N, gd, C.byref(least), C.byref(most)))
+    return least.value, most.value
+
+
+def _xent_rows(cb: Codebook, hidden: torch.Tensor, row_seq, row_nvis, W_U, U_h, targets):
+    c, dt, N = cb.cfg, _table_dtype(cb), hidden.shape[0]
+    return N, (cb.handle, _dev(hidden, dt, N * c.d, "hidden"), N, _dev(row_seq, torch.int32, N, "row_seq"),
+               _dev(row_nvis, torch.int32, N, "row_nvis"), _dev(W_U, dt, c.V * c.d, "W_U"), _cache(cb, U_h, dt, "U_h"),
+               _dev(targets, torch.int32, N, "targets"))
+
+
+def _xent_grads(cb: Codebook, N: int, accumulate: bool, grad_hidden, grad_WU, grad_Uh, scratch: torch.Tensor):
+    c = cb.cfg
+    some = grad_WU if grad_WU is not None else grad_Uh
+    gt = torch.float32 if some is None else some.dtype
+    _need(gt in (torch.float32, torch.bfloat16), "grad_WU and grad_Uh must be fp32 or bf16")
+    # (without gradients of the tables their type is the session's: what its scratch is counted by)
+    code = c.dtype if some is None else DTYPE_FP32 if gt == torch.float32 else DTYPE_BF16
+    return (code, 1 if accumulate else 0, _dev(grad_hidden, _table_dtype(cb), N * c.d, "grad_hidden"), _dev(grad_WU, gt, c.V * c.d, "grad_WU"),
+            _cache(cb, grad_Uh, gt, "grad_Uh"), _dev(scratch, torch.uint8, scratch.numel(), "scratch"), scratch.numel())
+
+
+def z2z_xent_loss(cb: Codebook, hidden: torch.Tensor, row_seq: Optional[torch.Tensor], row_nvis: Optional[torch.Tensor], W_U: torch.Tensor,
+                  U_h: Optional[torch.Tensor], targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor, scratch: torch.Tensor):
+    """Cross entropy of hidden [N, d] over the joint vocabulary against targets [N] -> loss [N], lse [N] (see z2z.h);
+    scratch: uint8 tensor of z2z_xent_scratch_bytes."""
+    N, args = _xent_rows(cb, hidden, row_seq, row_nvis, W_U, U_h, targets)
+    _enqueue(lib().z2z_xent_loss, hidden, *args, _dev(loss, torch.float32, N, "loss"), _dev(lse, torch.float32, N, "lse"),
+             _dev(scratch, torch.uint8, scratch.numel(), "scratch"), scratch.numel())
+
+
+def z2z_xent_grad(cb: Codebook, hidden: torch.Tensor, row_seq: Optional[torch.Tensor], row_nvis: Optional[torch.Tensor], W_U: torch.Tensor,
+                  U_h: Optional[torch.Tensor], targets: torch.Tensor, lse: torch.Tensor, grad_loss: Optional[torch.Tensor], accumulate: bool,
+                  grad_hidden: Optional[torch.Tensor], grad_WU: Optional[torch.Tensor], grad_Uh: Optional[torch.Tensor], scratch: torch.Tensor):
+    """Backward pass of z2z_xent_loss: lse as it left it, grad_loss [N] (None: ones) -> the gradients that are given."""
+    N, args = _xent_rows(cb, hidden, row_seq, row_nvis, W_U, U_h, targets)
+    _enqueue(lib().z2z_xent_grad, hidden, *args, _dev(lse, torch.float32, N, "lse"), _dev(grad_loss, torch.float32, N, "grad_loss"),
+             *_xent_grads(cb, N, accumulate, grad_hidden, grad_WU, grad_Uh, scratch))
+
+
+def z2z_xent_step(cb: Codebook, hidden: torch.Tensor, row_seq: Optional[torch.Tensor], row_nvis: Optional[torch.Tensor], W_U: torch.Tensor,
+                  U_h: Optional[torch.Tensor], targets: torch.Tensor, row_weight: Optional[torch.Tensor], loss: torch.Tensor, lse: torch.Tensor,
+                  accumulate: bool, grad_hidden: Optional[torch.Tensor], grad_WU: Optional[torch.Tensor], grad_Uh: Optional[torch.Tensor],
+                  scratch: torch.Tensor):
+    """Losses and the gradients of sum(row_weight * loss) in one call."""
+    N, args = _xent_rows(cb, hidden, row_seq, row_nvis, W_U, U_h, targets)
+    _enqueue(lib().z2z_xent_step, hidden, *args, _dev(row_weight, torch.float32, N, "row_weight"), _dev(loss, torch.float32, N, "loss"),
+             _dev(lse, torch.float32, N, "lse"), *_xent_grads(cb, N, accumulate, grad_hidden, grad_WU, grad_Uh, scratch))
+
+
+class GradTensors:
+    """Records of gradient tensors for z2z_grad_clip, made once for tensors that stay where they are."""
+
+    def __init__(self, records, tensors, device):
+        self.records, self.device = records, device
+        self._keep = tensors
+
+
+def grad_tensors(grads: Sequence[torch.Tensor], outs: Optional[Sequence[Optional[torch.Tensor]]] = None) -> GradTensors:
+    """Gradients (fp32 or bf16, contiguous, on one device) and where they go: outs[i] of the same size, fp32 or bf16, the
+    gradient itself (in place), or None (counts for the norm alone); outs None: all in place."""
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    _need(len(grads) == len(outs), "as many outputs as gradients are needed")
+    codes = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+    rec = (GradTensor * len(grads))()
+    for r, g, o in zip(rec, grads, outs):
+        for t in (g, o) if o is not None else (g,):
+            _need(t.is_cuda and t.dtype in codes and t.is_contiguous() and t.numel() == g.numel() and t.device == grads[0].device,
+                  "gradients and outputs must be contiguous device tensors of the same size, fp32 or bf16, on one device")
+        r.d_grad, r.numel, r.grad_dtype = g.data_ptr(), g.numel(), codes[g.dtype]
+        r.d_out, r.out_dtype = (o.data_ptr(), codes[o.dtype]) if o is not None else (None, r.grad_dtype)
+    return GradTensors(rec, (grads, outs), grads[0].device if grads else None)
+
+
+def z2z_grad_clip_scratch_bytes(tensors: GradTensors) -> int:
+    out = C.c_size_t(0)
+    _check(lib().z2z_grad_clip_scratch_bytes(len(tensors.records), C.byref(out)))
+    return out.value
+
+
+def z2z_grad_clip(tensors: GradTensors, scale: float, max_norm: float, norm: Optional[torch.Tensor], scratch: torch.Tensor):
+    """norm [1] = |scale| * 2-norm of all gradients; outputs = scale * min(1, max_norm / (norm + 1e-6)) * gradient (see z2z.h);
+    scratch: uint8 tensor of z2z_grad_clip_scratch_bytes."""
+    _need(tensors.device is None or scratch.device == tensors.device, "scratch must be on the gradients' device")
+    _enqueue(lib().z2z_grad_clip, scratch, tensors.records, len(tensors.records), scale, max_norm, _dev(norm, torch.float32, 1, "norm"),
+             _dev(scratch, torch.uint8, scratch.numel(), "scratch"), scratch.numel())
 
 
 def z2z_beam_select(cb: Codebook, beams: int, logits: torch.Tensor, lse: torch.Tensor, scores: torch.Tensor,

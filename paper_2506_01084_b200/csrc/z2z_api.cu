@@ -7,8 +7,10 @@
 #include <vector>
 
 #include "z2z_common.cuh"
+#include "z2z_grad_clip.h"
 #include "z2z_internal.h"
 #include "z2z_stream.h"
+#include "z2z_xent.h"
 
 struct z2z_codebook {
   z2z_config cfg;
@@ -358,6 +360,118 @@ int32_t z2z_embed_grad(z2z_codebook* cb, const int32_t* d_codes, int32_t N, cons
   a.gWE = d_grad_WE; a.gEh = cb->cfg.cap > 0 ? d_grad_Eh : nullptr;
   a.scratch = reinterpret_cast<char*>(d_scratch);
   Z2Z_CUDA(z2z::launch_embed_grad(cb->view, a, reinterpret_cast<cudaStream_t>(stream)), "embed_grad");
+  return Z2Z_OK;
+}
+
+int32_t z2z_xent_scratch_bytes(const z2z_config* cfg, int32_t N, int32_t grad_dtype, size_t* out_least, size_t* out_most) {
+  int rc = check_config(cfg);
+  if (rc) return rc;
+  if (N < 0 || N > z2z::kXentMaxRows) return fail(Z2Z_ERR_INVALID_ARG, "need 0 <= N <= 2^20");
+  if (grad_dtype != -1 && grad_dtype != Z2Z_DTYPE_FP32 && grad_dtype != Z2Z_DTYPE_BF16) return fail(Z2Z_ERR_INVALID_ARG, "unknown grad_dtype");
+  if (!out_least || !out_most) return fail(Z2Z_ERR_INVALID_ARG, "out_least / out_most is NULL");
+  z2z::xent_scratch_bytes(*cfg, N, grad_dtype, out_least, out_most);
+  return Z2Z_OK;
+}
+
+static int32_t xent_call(z2z_codebook* cb, z2z::XentArgs& a, z2z_stream stream) {
+  if (!cb) return fail(Z2Z_ERR_INVALID_ARG, "cb is NULL");
+  if (a.N < 0 || a.N > z2z::kXentMaxRows) return fail(Z2Z_ERR_INVALID_ARG, "need 0 <= N <= 2^20");
+  if (a.want_grad) {
+    if (a.grad_dtype != Z2Z_DTYPE_FP32 && a.grad_dtype != Z2Z_DTYPE_BF16) return fail(Z2Z_ERR_INVALID_ARG, "unknown grad_dtype");
+    if (a.accumulate != 0 && a.accumulate != 1) return fail(Z2Z_ERR_INVALID_ARG, "accumulate must be 0 or 1");
+    if (cb->cfg.cap == 0) a.g_Uh = nullptr;
+    if (!a.g_hidden && !a.g_WU && !a.g_Uh) return fail(Z2Z_ERR_INVALID_ARG, "no gradient is wanted");
+    if (misaligned(a.g_hidden, 16) || misaligned(a.g_WU, 16) || misaligned(a.g_Uh, 16)) return fail(Z2Z_ERR_INVALID_ARG, "gradients must be 16-byte aligned");
+  }
+  if (a.N > 0) {
+    if (!a.hidden || !a.WU || !a.targets) return fail(Z2Z_ERR_INVALID_ARG, "d_hidden / d_WU / d_targets is NULL");
+    if (!a.Uh && cb->cfg.cap > 0) return fail(Z2Z_ERR_INVALID_ARG, "d_Uh is NULL");
+    if (misaligned(a.hidden, 16) || misaligned(a.WU, 16) || misaligned(a.Uh, 16)) return fail(Z2Z_ERR_INVALID_ARG, "tables and rows must be 16-byte aligned");
+    if (!a.lse || (a.want_loss && !a.loss)) return fail(Z2Z_ERR_INVALID_ARG, "d_loss / d_lse is NULL");
+    if (misaligned(a.row_seq, 4) || misaligned(a.row_nvis, 4) || misaligned(a.targets, 4) || misaligned(a.weight, 4) || misaligned(a.loss, 4) || misaligned(a.lse, 4))
+      return fail(Z2Z_ERR_INVALID_ARG, "arrays must be aligned to their elements");
+    if (!a.row_seq && a.N > cb->cfg.B) return fail(Z2Z_ERR_INVALID_ARG, "d_row_seq is required when N > B");
+    size_t least = 0, most = 0;
+    z2z::xent_scratch_bytes(cb->cfg, a.N, a.want_grad ? a.grad_dtype : -1, &least, &most);
+    if (!a.scratch || misaligned(a.scratch, 256)) return fail(Z2Z_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
+    if (a.scratch_bytes < least) return fail(Z2Z_ERR_WORKSPACE_TOO_SMALL, "scratch smaller than z2z_xent_scratch_bytes");
+  }
+  a.d = cb->cfg.d; a.dtype = cb->cfg.dtype;
+  a.err = reinterpret_cast<int*>(cb->ws + cb->plan.off_words);
+  Z2Z_CUDA(z2z::run_xent(cb->view, cb->cfg, a, reinterpret_cast<cudaStream_t>(stream)), "xent");
+  return Z2Z_OK;
+}
+
+int32_t z2z_xent_loss(z2z_codebook* cb, const void* d_hidden, int32_t N, const int32_t* d_row_seq,
+                      const int32_t* d_row_nvis, const void* d_WU, const void* d_Uh, const int32_t* d_targets,
+                      float* d_loss, float* d_lse, void* d_scratch, size_t scratch_bytes, z2z_stream stream) {
+  z2z::XentArgs a{};
+  a.N = N; a.hidden = d_hidden; a.row_seq = d_row_seq; a.row_nvis = d_row_nvis; a.WU = d_WU; a.Uh = d_Uh; a.targets = d_targets;
+  a.loss = d_loss; a.lse = d_lse; a.scratch = reinterpret_cast<char*>(d_scratch); a.scratch_bytes = scratch_bytes;
+  a.want_loss = true;
+  return xent_call(cb, a, stream);
+}
+
+int32_t z2z_xent_grad(z2z_codebook* cb, const void* d_hidden, int32_t N, const int32_t* d_row_seq,
+                      const int32_t* d_row_nvis, const void* d_WU, const void* d_Uh, const int32_t* d_targets,
+                      const float* d_lse, const float* d_grad_loss, int32_t grad_dtype, int32_t accumulate,
+                      void* d_grad_hidden, void* d_grad_WU, void* d_grad_Uh, void* d_scratch, size_t scratch_bytes,
+                      z2z_stream stream) {
+  z2z::XentArgs a{};
+  a.N = N; a.hidden = d_hidden; a.row_seq = d_row_seq; a.row_nvis = d_row_nvis; a.WU = d_WU; a.Uh = d_Uh; a.targets = d_targets;
+  a.lse = const_cast<float*>(d_lse); a.weight = d_grad_loss; a.grad_dtype = grad_dtype; a.accumulate = accumulate;
+  a.g_hidden = d_grad_hidden; a.g_WU = d_grad_WU; a.g_Uh = d_grad_Uh;
+  a.scratch = reinterpret_cast<char*>(d_scratch); a.scratch_bytes = scratch_bytes;
+  a.want_grad = true;
+  return xent_call(cb, a, stream);
+}
+
+int32_t z2z_xent_step(z2z_codebook* cb, const void* d_hidden, int32_t N, const int32_t* d_row_seq,
+                      const int32_t* d_row_nvis, const void* d_WU, const void* d_Uh, const int32_t* d_targets,
+                      const float* d_row_weight, float* d_loss, float* d_lse, int32_t grad_dtype, int32_t accumulate,
+                      void* d_grad_hidden, void* d_grad_WU, void* d_grad_Uh, void* d_scratch, size_t scratch_bytes,
+                      z2z_stream stream) {
+  z2z::XentArgs a{};
+  a.N = N; a.hidden = d_hidden; a.row_seq = d_row_seq; a.row_nvis = d_row_nvis; a.WU = d_WU; a.Uh = d_Uh; a.targets = d_targets;
+  a.loss = d_loss; a.lse = d_lse; a.weight = d_row_weight; a.grad_dtype = grad_dtype; a.accumulate = accumulate;
+  a.g_hidden = d_grad_hidden; a.g_WU = d_grad_WU; a.g_Uh = d_grad_Uh;
+  a.scratch = reinterpret_cast<char*>(d_scratch); a.scratch_bytes = scratch_bytes;
+  a.want_loss = a.want_grad = true;
+  return xent_call(cb, a, stream);
+}
+
+int32_t z2z_grad_clip_scratch_bytes(int32_t n, size_t* out_bytes) {
+  if (n < 0 || n > z2z::kGradClipMaxTensors) return fail(Z2Z_ERR_INVALID_ARG, "need 0 <= n <= 65536");
+  if (!out_bytes) return fail(Z2Z_ERR_INVALID_ARG, "out_bytes is NULL");
+  *out_bytes = z2z::grad_clip_scratch_bytes(n);
+  return Z2Z_OK;
+}
+
+int32_t z2z_grad_clip(const z2z_grad_tensor* h_tensors, int32_t n, float scale, float max_norm, float* d_norm,
+                      void* d_scratch, size_t scratch_bytes, z2z_stream stream) {
+  if (n < 0 || n > z2z::kGradClipMaxTensors) return fail(Z2Z_ERR_INVALID_ARG, "need 0 <= n <= 65536");
+  if (n > 0 && !h_tensors) return fail(Z2Z_ERR_INVALID_ARG, "h_tensors is NULL");
+  if (!std::isfinite(scale)) return fail(Z2Z_ERR_INVALID_ARG, "scale is not finite");
+  if (!(max_norm > 0.f)) return fail(Z2Z_ERR_INVALID_ARG, "need max_norm > 0");
+  if (misaligned(d_norm, 4)) return fail(Z2Z_ERR_INVALID_ARG, "arrays must be aligned to their elements");
+  long long total = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const z2z_grad_tensor& t = h_tensors[i];
+    if (t.numel < 0) return fail(Z2Z_ERR_INVALID_ARG, "numel of a tensor is negative");
+    if ((t.grad_dtype != Z2Z_DTYPE_FP32 && t.grad_dtype != Z2Z_DTYPE_BF16) || (t.d_out && t.out_dtype != Z2Z_DTYPE_FP32 && t.out_dtype != Z2Z_DTYPE_BF16))
+      return fail(Z2Z_ERR_INVALID_ARG, "unknown dtype of a tensor");
+    if (t.numel == 0) continue;
+    if (!t.d_grad) return fail(Z2Z_ERR_INVALID_ARG, "d_grad of a tensor is NULL");
+    if (misaligned(t.d_grad, t.grad_dtype == Z2Z_DTYPE_BF16 ? 2 : 4) || misaligned(t.d_out, t.out_dtype == Z2Z_DTYPE_BF16 ? 2 : 4))
+      return fail(Z2Z_ERR_INVALID_ARG, "a tensor must be aligned to its elements");
+    if (t.d_out == t.d_grad && t.out_dtype != t.grad_dtype) return fail(Z2Z_ERR_INVALID_ARG, "a tensor scaled in place keeps its type");
+    if (t.numel > z2z::grad_clip_max_elements() - total) return fail(Z2Z_ERR_INVALID_ARG, "need at most 2^43 elements");
+    total += t.numel;
+  }
+  if (n > 0 && (!d_scratch || misaligned(d_scratch, 8))) return fail(Z2Z_ERR_INVALID_ARG, "scratch must be 8-byte aligned");
+  if (scratch_bytes < z2z::grad_clip_scratch_bytes(n)) return fail(Z2Z_ERR_WORKSPACE_TOO_SMALL, "scratch smaller than z2z_grad_clip_scratch_bytes");
+  Z2Z_CUDA(z2z::launch_grad_clip(h_tensors, n, scale, max_norm, d_norm, reinterpret_cast<double*>(d_scratch), reinterpret_cast<cudaStream_t>(stream)),
+           "grad_clip");
   return Z2Z_OK;
 }
 

@@ -1,0 +1,293 @@
+// Global norm of many gradient tensors, and the tensors scaled to a largest norm.
+//
+//   norm = |scale| sqrt(sum over all tensors of g^2),   out = scale min(1, max_norm / (norm + 1e-6)) g
+//
+// Two launches: partial sums of squares, one per block; then every block adds the partial sums in the same order and
+// scales its share.  Both are bound by memory.  The tensors are cut into chunks of 32 KB, dealt to the blocks in turn;
+// the second launch takes them from the end, where the first one's are still in L2.  Where nothing would change (in
+// place, and a factor of 1) it writes nothing.
+//
+// Squares of 16 bytes are added in fp32 and those sums in fp64; 16 bytes whose sum of squares overflows, or is so small
+// that squares may have lost bits, are squared again in fp64, so that any finite gradient has a finite norm.
+#include <cmath>
+
+#include "z2z_common.cuh"
+#include "z2z_grad_clip.h"
+#include "z2z_internal.h"
+#include "z2z_sm100.cuh"
+
+namespace z2z {
+using namespace sm100;
+
+namespace {
+
+constexpr int kClipThreads = 256;
+constexpr int kVecs = 8;                         // 16-byte vectors per thread and chunk, loaded before any is used
+constexpr int kChunkVecs = kClipThreads * kVecs;
+constexpr int kBlocksPerSm = 4;
+constexpr int kRecords = 512;                    // tensors per launch (kernel parameters)
+
+struct Record {
+  const char* g;
+  char* out;
+  long long n;
+  int first;                                     // its first chunk
+  int type;                                      // bit 0: gradient is bf16, bit 1: output is
+};
+struct Records {
+  int count, chunks;
+  Record r[kRecords];
+};
+
+// The tensor that holds a chunk.
+__device__ __forceinline__ int record_of(const Records& t, int chunk) {
+  int lo = 0, hi = t.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (t.r[mid].first <= chunk) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// A chunk of a tensor: whole vectors [v0, v1) from the first 16-byte boundary on; the elements ahead of it go to the
+// first chunk and those behind the last vector to the last one.
+struct Span {
+  int head;                                      // elements before the boundary
+  long long v0, v1;
+  long long tail0, tail1;                        // elements of the tail
+};
+__device__ __forceinline__ Span span_of(const Record& r, int chunk) {
+  const int es = r.type & 1 ? 2 : 4, per = 16 / es;
+  Span s;
+  const int off = (int)(reinterpret_cast<uintptr_t>(r.g) & 15);
+  const long long head = off ? (16 - off) / es : 0;
+  s.head = (int)(head < r.n ? head : r.n);
+  const long long vecs = (r.n - s.head) / per;
+  s.v0 = (long long)(chunk - r.first) * kChunkVecs;
+  s.v1 = s.v0 + kChunkVecs < vecs ? s.v0 + kChunkVecs : vecs;
+  const bool last = s.v0 + kChunkVecs >= vecs && (s.v0 < vecs || chunk == r.first);
+  s.tail0 = last ? s.head + vecs * per : r.n;
+  s.tail1 = r.n;
+  if (chunk != r.first) s.head = -s.head;        // (not this chunk's)
+  return s;
+}
+
+__device__ __forceinline__ float load_one(const Record& r, long long i) {
+  return r.type & 1 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(r.g)[i]) : reinterpret_cast<const float*>(r.g)[i];
+}
+__device__ __forceinline__ void store_one(const Record& r, long long i, float x) {
+  if (r.type & 2) reinterpret_cast<__nv_bfloat16*>(r.out)[i] = __float2bfloat16_rn(x);
+  else reinterpret_cast<float*>(r.out)[i] = x;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void unpack(const uint4& v, float* x) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (BF16) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    else x[i] = __uint_as_float(w[i]);
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ double squares(const uint4& v) {
+  constexpr int kPer = BF16 ? 8 : 4;
+  float x[kPer];
+  unpack<BF16>(v, x);
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) s = fmaf(x[i], x[i], s);
+  if (s > 1e-30f && s < 1e38f) return (double)s;
+  double t = 0.0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) t += (double)x[i] * (double)x[i];
+  return t;
+}
+
+__device__ __forceinline__ const uint4* body(const Record& r, int head) {
+  return reinterpret_cast<const uint4*>(r.g + (size_t)head * (r.type & 1 ? 2 : 4));
+}
+
+template <bool BF16>
+__device__ __forceinline__ double chunk_squares(const uint4* from, const Span& s) {
+  uint4 v[kVecs];
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    const long long i = s.v0 + u * kClipThreads + threadIdx.x;
+    v[u] = i < s.v1 ? from[i] : make_uint4(0u, 0u, 0u, 0u);
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) sum += squares<BF16>(v[u]);
+  return sum;
+}
+
+// Sum over the block in an order of its own; thread 0 has it.
+__device__ __forceinline__ double block_sum(double x) {
+  __shared__ double s[kClipThreads / 32];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_down_sync(0xffffffffu, x, o);
+  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    x = threadIdx.x < kClipThreads / 32 ? s[threadIdx.x] : 0.0;
+#pragma unroll
+    for (int o = 4; o; o >>= 1) x += __shfl_down_sync(0xffffffffu, x, o);
+  }
+  return x;
+}
+
+__global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_norm(const __grid_constant__ Records t, double* part) {
+  pdl_wait();
+  pdl_trigger();
+  double sum = 0.0;
+  for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const Record& r = t.r[record_of(t, c)];
+    const Span s = span_of(r, c);
+    const uint4* from = body(r, abs(s.head));
+    sum += r.type & 1 ? chunk_squares<true>(from, s) : chunk_squares<false>(from, s);
+    if (s.head > (int)threadIdx.x) { const double x = load_one(r, threadIdx.x); sum += x * x; }
+    if (s.tail0 + threadIdx.x < s.tail1) { const double x = load_one(r, s.tail0 + threadIdx.x); sum += x * x; }
+  }
+  sum = block_sum(sum);
+  if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+template <bool FROM, bool TO>
+__device__ __forceinline__ void chunk_scale(const Record& r, const Span& s, float factor) {
+  constexpr int kPer = FROM ? 8 : 4, kOut = kPer * (TO ? 2 : 4);
+  const int head = abs(s.head);
+  const uint4* from = body(r, head);
+  char* to = r.out + (size_t)head * (TO ? 2 : 4);
+  const bool whole = (reinterpret_cast<uintptr_t>(to) & (kOut < 16 ? kOut - 1 : 15)) == 0;
+  uint4 v[kVecs];
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    const long long i = s.v0 + u * kClipThreads + threadIdx.x;
+    if (i < s.v1) v[u] = from[i];
+  }
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    const long long i = s.v0 + u * kClipThreads + threadIdx.x;
+    if (i >= s.v1) continue;
+    float x[kPer];
+    unpack<FROM>(v[u], x);
+    uint32_t o[kOut / 4];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) x[k] *= factor;
+    if (TO) {
+#pragma unroll
+      for (int k = 0; k < kPer / 2; ++k) { const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]); o[k] = *reinterpret_cast<const uint32_t*>(&p); }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) o[k] = __float_as_uint(x[k]);
+    }
+    char* at = to + i * kOut;
+    if (whole) {
+      if constexpr (kOut == 8) *reinterpret_cast<uint2*>(at) = make_uint2(o[0], o[1]);
+      else {
+#pragma unroll
+        for (int k = 0; k < kOut / 16; ++k) reinterpret_cast<uint4*>(at)[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) store_one(r, head + i * kPer + k, x[k]);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_scale(const __grid_constant__ Records t, const double* part, int parts, float scale, float max_norm,
+                                                             float* norm_out) {
+  __shared__ float s_factor;
+  __shared__ int s_write;
+  pdl_wait();
+  pdl_trigger();
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < parts; i += kClipThreads) sum += part[i];
+  sum = block_sum(sum);
+  if (threadIdx.x == 0) {
+    const float norm = (float)(fabs((double)scale) * sqrt(sum));
+    if (norm_out && blockIdx.x == 0) *norm_out = norm;
+    s_factor = scale * fminf(1.f, max_norm / (norm + 1e-6f));
+    s_write = norm < INFINITY;                   // (nor a NaN)
+  }
+  __syncthreads();
+  if (!s_write) return;
+  const float factor = s_factor;
+  for (int c = t.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
+    const Record& r = t.r[record_of(t, c)];
+    if (!r.out || (r.out == r.g && factor == 1.f)) continue;
+    const Span s = span_of(r, c);
+    switch (r.type) {
+      case 0: chunk_scale<false, false>(r, s, factor); break;
+      case 1: chunk_scale<true, false>(r, s, factor); break;
+      case 2: chunk_scale<false, true>(r, s, factor); break;
+      default: chunk_scale<true, true>(r, s, factor); break;
+    }
+    if (s.head > (int)threadIdx.x) store_one(r, threadIdx.x, load_one(r, threadIdx.x) * factor);
+    if (s.tail0 + threadIdx.x < s.tail1) store_one(r, s.tail0 + threadIdx.x, load_one(r, s.tail0 + threadIdx.x) * factor);
+  }
+}
+
+int clip_blocks() {
+  static const int n = [] {
+    int dev = 0, v = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v <= 0) {
+      cudaGetLastError();                        // (no GPU: sizes are still asked for)
+      v = 148;
+    }
+    return kBlocksPerSm * v;
+  }();
+  return n;
+}
+
+int chunks_of(const z2z_grad_tensor& t) {
+  const long long bytes = t.numel * (t.grad_dtype == Z2Z_DTYPE_BF16 ? 2 : 4);
+  const long long c = (bytes + (long long)kChunkVecs * 16 - 1) / ((long long)kChunkVecs * 16);
+  return (int)c;
+}
+
+}  // namespace
+
+size_t grad_clip_scratch_bytes(int n) { return (size_t)((n + kRecords - 1) / kRecords) * clip_blocks() * sizeof(double); }
+long long grad_clip_max_elements() { return (long long)kChunkVecs * 4 << 30; }
+
+cudaError_t launch_grad_clip(const z2z_grad_tensor* t, int n, float scale, float max_norm, float* norm, double* part, cudaStream_t s) {
+  const int blocks = clip_blocks();
+  // (16 KB of parameters: filled where they are handed over, launch by launch)
+  Records rec;
+  auto fill = [&](int from) {
+    rec.count = rec.chunks = 0;
+    bool writes = false;
+    for (int i = from; i < n && i < from + kRecords; ++i) {
+      if (t[i].numel == 0) continue;
+      Record& r = rec.r[rec.count++];
+      r.g = reinterpret_cast<const char*>(t[i].d_grad); r.out = reinterpret_cast<char*>(t[i].d_out); r.n = t[i].numel;
+      r.first = rec.chunks;
+      r.type = (t[i].grad_dtype == Z2Z_DTYPE_BF16 ? 1 : 0) | (t[i].out_dtype == Z2Z_DTYPE_BF16 ? 2 : 0);
+      rec.chunks += chunks_of(t[i]);
+      writes |= r.out != nullptr;
+    }
+    return writes;
+  };
+  int parts = 0;
+  for (int from = 0; from < n; from += kRecords) {
+    fill(from);
+    const int g = rec.chunks < blocks ? (rec.chunks > 0 ? rec.chunks : 1) : blocks;
+    const cudaError_t e = launch_pdl(k_clip_norm, dim3(g), dim3(kClipThreads), 0, s, rec, part + parts);
+    if (e != cudaSuccess) return e;
+    parts += g;
+  }
+  for (int from = 0; from < n || from == 0; from += kRecords) {
+    const bool writes = fill(from);
+    if (!writes && from > 0) continue;
+    const int g = writes ? (rec.chunks < blocks ? rec.chunks : blocks) : 1;
+    if (!writes) rec.chunks = 0;
+    const cudaError_t e = launch_pdl(k_clip_scale, dim3(g), dim3(kClipThreads), 0, s, rec, part, parts, scale, max_norm, from == 0 ? norm : nullptr);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace z2z
