@@ -7,13 +7,13 @@
 //   dh_r   = sum_v g_rv W_v       dW_v = sum_r g_rv h_r
 //
 // Three contractions of 2 N (V + n) d flop (the losses alone: one), all on tcgen05 with CTA pairs:
-//   logits   D[v, r] = W  H^T     M = 256 vocabulary rows, N = up to 256 hidden rows, K = d
-//   hidden   D[d, r] = W^T G^T    M = 256 columns,         N = up to 256 hidden rows, K = vocabulary rows
-//   tables   D[v, d] = G^T H      M = 256 vocabulary rows, N = up to 256 columns,     K = hidden rows
-// The vocabulary is taken in pieces: of each, G^T [v][r] is written by the epilogue of the logits, and both other
-// contractions read it, with operands whose contiguous axis is the contracted one (K-major) or the other (MN-major)
-// as they lie in memory: nothing is transposed.  Hidden rows are the MMA's N everywhere, so that few of them cost
-// little: what is left is one pass over the tables for the logits, one for dh and the write of dW.
+//   logits   D[r, v] = H  W^T     M = 256 hidden rows,     N = up to 256 vocabulary rows, K = d
+//   hidden   D[d, r] = W^T G^T    M = 256 columns,         N = up to 256 hidden rows,     K = vocabulary rows
+//   tables   D[v, d] = G^T H      M = 256 vocabulary rows, N = up to 256 columns,         K = hidden rows
+// The vocabulary is taken in pieces: of each, G [r][v] is written by the epilogue of the logits, whose threads have a
+// hidden row each, and both other contractions read it, with operands whose contiguous axis is the contracted one
+// (K-major) or the other (MN-major) as they lie in memory: nothing is transposed.  Few rows cost little beside the
+// tables: one pass over them for the logits, one for dh and the write of dW.
 //
 // Rows are sorted by their sequence first (stable), and rows without a target, which add nothing, are left out.
 // Hypertokens are a piece per sequence: its entries against its own rows, which start at a multiple of 32 there.
@@ -37,12 +37,15 @@ using namespace sm100;
 namespace {
 
 constexpr int kEpiWarps = 8;                     // two per tensor-memory lane quarter, which take every other 32 columns
-constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kThreads = 128 + 32 * kEpiWarps;   // a warpgroup of producer, issuer and two that leave; two of the epilogue
+// Registers: 384 threads are launched with 168 each; the epilogue, which holds a tile's sums, takes what the others leave
+// (128 x 56 + 256 x 224 = 384 x 168).
+constexpr int kRegsFew = 56, kRegsEpi = 224;
 constexpr int kStages = 6;
 constexpr int kTile = 256;                       // vocabulary rows or columns of a tile (128 per CTA)
 constexpr int kStageBytes = 32768;               // 128 x 64 of either operand
-constexpr int kMetaBytes = 2 * kTile * 16, kPartBytes = 4 * kTile * 8;
-constexpr int kFrontBytes = 1024 + kMetaBytes + kPartBytes;        // a multiple of 1024
+constexpr int kTurnBytes = 32 * 32 * 4;          // a warp's 32 x 32 values on their way from rows per thread to whole lines
+constexpr int kFrontBytes = 1024 + kEpiWarps * kTurnBytes;         // a multiple of 1024
 constexpr size_t kSmemBytes = 1024 + kFrontBytes + (size_t)kStages * kStageBytes;
 constexpr int kHyperPad = 32;                    // a sequence's rows start at a multiple of this beside its hypertokens
 constexpr int kLossRows = 8192;                  // rows whose partial sums are held at a time
@@ -60,7 +63,7 @@ static_assert(sizeof(Ctrl) <= 1024 && kFrontBytes % 1024 == 0, "control block");
 // What the plan leaves in the scratch.
 struct Plan {
   int32_t* head;             // [0] rows that take part, [1..3] jobs of hypertokens: logits, hidden, tables; [4] largest weight
-  int32_t *cnt; float* wmax; // [B]
+  int32_t* cnt;              // [B] rows of a sequence that take part
   int32_t *s0, *h0;          // [B + 1] first position of a sequence's rows, and the one beside its hypertokens
   int32_t *j1, *j2, *j3;     // [B + 1] jobs of the sequences before
   int32_t *perm, *inv;       // position -> row, row -> position or -1
@@ -82,7 +85,8 @@ struct Params {
   int d, dt;
   int v0, vn;                // piece: vocabulary rows v0 .. v0 + vn
   int w_row0;                // its first row in the tensor map of W
-  int tr, th;                // rows per tile, and per tile of a sequence's rows
+  int cta_rows, nv;          // logits: hidden rows per CTA, vocabulary rows per tile
+  int tr, th;                // rows per tile of dh, and per tile of a sequence's rows
   int r_lo, r_hi;            // positions of this launch (losses: a share of the rows)
   int sb;                    // row tiles that are taken through all vocabulary tiles before the next ones
   int np1, np2, np3;         // products of parts
@@ -92,7 +96,7 @@ struct Params {
   int first;                 // first piece: dh's partial sums are set, not added to
   // logits
   __nv_bfloat16 *g, *gh; long long g_plane, gh_plane; int g_pitch, gh_pitch, g_parts;
-  bool exact_exp;
+  bool exact_exp; int exact_sums;                // bit 0: of dh, bit 1: of the tables
   float2 *part, *part_h; int part_rows, part_rows_h, part0;
   float* tl;
   // gradients
@@ -103,120 +107,125 @@ struct Params {
 };
 
 struct Maps {
-  CUtensorMap w_k, u_k, hs_k, hh_k;              // K-major: 64 columns x 128 rows (hidden: half a tile)
-  CUtensorMap w_m, u_m, ut_m, hs_m, hh_m;        // MN-major: 64 columns x 64 rows (ut: 16)
-  CUtensorMap g_k, gh_k, g_m, gh_m;
+  // K-major: 64 columns x 128 rows of a table, or a CTA's rows of a tile of hidden rows or of G
+  CUtensorMap w_k, u_k, hs_k, hh_k, g_k, gh_k;
+  // MN-major: 64 columns x 64 rows (ut: 16)
+  CUtensorMap w_m, u_m, ut_m, hs_m, hh_m, g_m, gh_m;
 };
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // ---- plan ------------------------------------------------------------------------------------------
-struct RowState { bool mine, live, bad; int target, nvis; float w; };
-__device__ __forceinline__ RowState row_state(const CbView& cb, const RowArgs& a, int r, int b) {
-  RowState s{false, false, false, -1, 0, 1.f};
-  if (r >= a.N) return s;
-  const int seq = a.row_seq ? a.row_seq[r] : r;
-  s.mine = b < cb.B ? seq == b : (seq < 0 || seq >= cb.B);
-  if (!s.mine || b >= cb.B) return s;
-  s.nvis = cb.n[b];
-  if (a.row_nvis) { const int x = a.row_nvis[r]; s.nvis = x < s.nvis ? (x < 0 ? 0 : x) : s.nvis; }
-  s.target = a.targets[r];
-  s.bad = s.target != Z2Z_CODE_NONE && (s.target < 0 || s.target >= cb.V + s.nvis);
-  s.live = s.target != Z2Z_CODE_NONE && !s.bad;
-  if (a.weight) { s.w = a.weight[r]; if (s.w == 0.f) s.live = false; }
-  return s;
-}
+// One block: a histogram of the rows that take part over their sequences, its prefix sums, and a stable place for
+// every row.  (A warp per sequence that looked through all rows took 60 us at 4096 rows of 16 sequences.)
+struct PlanShared {
+  int warp_sums[32];
+  float wmax;
+};
+constexpr int kPlanThreads = 1024;
+__host__ __device__ constexpr size_t plan_shared_bytes(int B) { return sizeof(PlanShared) + (size_t)B * 8 + (size_t)32 * B * 2; }
 
-constexpr int kScan = 8;                         // rows per lane and step: so many loads are under way
-
-// A warp per sequence (and one for rows without): how many of its rows take part, and their largest weight.
-__global__ void __launch_bounds__(128) k_xent_count(CbView cb, RowArgs a, Plan pl) {
+__global__ void __launch_bounds__(kPlanThreads) k_xent_plan(CbView cb, RowArgs a, Plan pl) {
+  extern __shared__ unsigned char smem[];
+  PlanShared& sh = *reinterpret_cast<PlanShared*>(smem);
+  int* s_cnt = reinterpret_cast<int*>(smem + sizeof(PlanShared));       // rows of a sequence, then where its next ones go
+  int* s_n = s_cnt + cb.B;
+  unsigned short* s_warp = reinterpret_cast<unsigned short*>(s_n + cb.B);      // [B][32] rows of a warp
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_trigger();
-  const int b = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (b >= cb.B) return;
-  int count = 0; float wmax = 0.f; bool bad = false;
-  const int lo = a.row_seq ? 0 : b, hi = a.row_seq ? a.N : min(a.N, b + 1);
-  for (int r0 = lo; r0 < hi; r0 += 32 * kScan) {
-    RowState s[kScan];
-#pragma unroll
-    for (int u = 0; u < kScan; ++u) { const int r = r0 + 32 * u + lane; s[u] = row_state(cb, a, r < hi ? r : a.N, b); }
-#pragma unroll
-    for (int u = 0; u < kScan; ++u) {
-      count += s[u].live;
-      bad |= s[u].bad;
-      if (s[u].live) { const float w = fabsf(s[u].w); wmax = w > wmax || w != w ? w : wmax; }
-    }
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    count += __shfl_xor_sync(0xffffffffu, count, o);
-    const float w = __shfl_xor_sync(0xffffffffu, wmax, o);
-    wmax = w > wmax || w != w ? w : wmax;
-  }
-  if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(&cb.status[b], Z2Z_ST_BAD_TOKEN);
-  if (lane == 0) { pl.cnt[b] = count; pl.wmax[b] = wmax; }
-}
+  for (int b = tid; b < cb.B; b += kPlanThreads) { s_cnt[b] = 0; s_n[b] = cb.n[b]; }
+  for (int i = tid; i < 32 * cb.B; i += kPlanThreads) s_warp[i] = 0;
+  if (tid == 0) sh.wmax = 0.f;
+  __syncthreads();
 
-// The same warps place their rows, in order, behind those of the sequences before.
-__global__ void __launch_bounds__(128) k_xent_place(CbView cb, RowArgs a, Plan pl) {
-  pdl_wait();
-  pdl_trigger();
-  const int b = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (b > cb.B) return;
-  int s0 = 0, h0 = 0, j1 = 0, j2 = 0, j3 = 0;
-  float wmax = 0.f;
-  for (int i = lane; i < cb.B; i += 32) {
-    const float w = pl.wmax[i];
-    wmax = w > wmax || w != w ? w : wmax;
-    if (i >= b) continue;
-    const int c = pl.cnt[i], n = cb.n[i];
-    s0 += c;
-    h0 += ceil_div(c, kHyperPad) * kHyperPad;
-    const int rt = ceil_div(c, a.th), kt = ceil_div(n, kTile);
-    j1 += rt * kt;
-    if (a.hidden && n) j2 += rt * a.dt;
-    if (a.tables) j3 += kt * a.dt;
-  }
+  constexpr int kAhead = 4;                      // rows of a thread whose loads are under way together
+  int wbits = 0; bool wnan = false;
+  for (int r0 = tid; r0 < a.N; r0 += kAhead * kPlanThreads) {
+    int seq[kAhead], tgt[kAhead], nv[kAhead]; float w[kAhead];
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    s0 += __shfl_xor_sync(0xffffffffu, s0, o); h0 += __shfl_xor_sync(0xffffffffu, h0, o);
-    j1 += __shfl_xor_sync(0xffffffffu, j1, o); j2 += __shfl_xor_sync(0xffffffffu, j2, o);
-    j3 += __shfl_xor_sync(0xffffffffu, j3, o);
-    const float w = __shfl_xor_sync(0xffffffffu, wmax, o);
-    wmax = w > wmax || w != w ? w : wmax;
-  }
-  if (lane == 0) {
-    pl.s0[b] = s0; pl.h0[b] = h0; pl.j1[b] = j1; pl.j2[b] = j2; pl.j3[b] = j3;
-    if (b == cb.B) { pl.head[0] = s0; pl.head[1] = j1; pl.head[2] = j2; pl.head[3] = j3; pl.head[4] = __float_as_int(wmax); }
-  }
-  int at = s0;
-  const int lo = a.row_seq || b == cb.B ? 0 : b, hi = a.row_seq ? a.N : (b == cb.B ? 0 : min(a.N, b + 1));
-  for (int r0 = lo; r0 < hi; r0 += 32 * kScan) {
-    RowState s[kScan];
-    float lse[kScan];
-#pragma unroll
-    for (int u = 0; u < kScan; ++u) {
-      const int r = r0 + 32 * u + lane;
-      s[u] = row_state(cb, a, r < hi ? r : a.N, b);
-      lse[u] = s[u].live && a.lse ? a.lse[r] : 0.f;
+    for (int u = 0; u < kAhead; ++u) {
+      const int r = r0 + u * kPlanThreads;
+      const bool in = r < a.N;
+      seq[u] = in ? (a.row_seq ? a.row_seq[r] : r) : -1;
+      tgt[u] = in ? a.targets[r] : Z2Z_CODE_NONE;
+      nv[u] = in && a.row_nvis ? a.row_nvis[r] : 0x7fffffff;
+      w[u] = in && a.weight ? a.weight[r] : 1.f;
     }
 #pragma unroll
-    for (int u = 0; u < kScan; ++u) {
-      const int r = r0 + 32 * u + lane;
-      const unsigned live = __ballot_sync(0xffffffffu, s[u].live);
-      if (s[u].live) {
-        const int p = at + __popc(live & ((1u << lane) - 1u));
-        pl.perm[p] = r;
-        pl.inv[r] = p;
-        pl.meta[p] = make_float4(lse[u], s[u].w / wmax, __int_as_float(s[u].target), __int_as_float(s[u].nvis));
-      } else if (s[u].mine) {
-        pl.inv[r] = -1;
+    for (int u = 0; u < kAhead; ++u) {
+      const int r = r0 + u * kPlanThreads;
+      if (r >= a.N) continue;
+      int b = -1;
+      if (seq[u] >= 0 && seq[u] < cb.B && tgt[u] != Z2Z_CODE_NONE) {
+        const int n = min(max(nv[u], 0), s_n[seq[u]]);
+        if (tgt[u] < 0 || tgt[u] >= cb.V + n) atomicOr(&cb.status[seq[u]], Z2Z_ST_BAD_TOKEN);
+        else if (w[u] != 0.f) b = seq[u];
+      }
+      pl.inv[r] = b;                             // (read again below by the same thread)
+      if (b >= 0) {
+        atomicAdd(&s_cnt[b], 1);
+        const float x = fabsf(w[u]);
+        if (x != x) wnan = true;
+        wbits = max(wbits, __float_as_int(x));
+      } else {
         if (a.loss_out) a.loss_out[r] = 0.f;
         if (a.lse_out) a.lse_out[r] = 0.f;
       }
-      at += __popc(live);
     }
+  }
+  // (magnitudes compare as whole numbers)
+  if (wnan) wbits = 0x7fc00000;
+  wbits = __reduce_max_sync(0xffffffffu, wbits);
+  if (lane == 0) atomicMax(reinterpret_cast<int*>(&sh.wmax), wbits);
+  __syncthreads();
+  const float wmax = sh.wmax;
+
+  // prefix sums over the sequences (B <= 1024: one each)
+  const int b = tid, c = b < cb.B ? s_cnt[b] : 0, n = b < cb.B ? s_n[b] : 0;
+  const int rt = ceil_div(c, a.th), kt = ceil_div(n, kTile);
+  const int v[5] = {c, ceil_div(c, kHyperPad) * kHyperPad, rt * kt, a.hidden && n ? rt * a.dt : 0, a.tables ? kt * a.dt : 0};
+  int32_t* const out[5] = {pl.s0, pl.h0, pl.j1, pl.j2, pl.j3};
+  int first = 0;
+#pragma unroll
+  for (int i = 0; i < 5; ++i) {
+    int total;
+    const int x = block_scan_1024(v[i], sh.warp_sums, total);
+    if (b < cb.B) out[i][b] = x;
+    if (tid == 0) {
+      out[i][cb.B] = total;
+      if (i == 0) pl.head[0] = total;
+      if (i >= 2) pl.head[i - 1] = total;
+    }
+    if (i == 0) first = x;
+  }
+  if (b < cb.B) { pl.cnt[b] = c; s_cnt[b] = first; }
+  if (tid == 0) pl.head[4] = __float_as_int(wmax);
+  __syncthreads();
+
+  // Places, 1024 rows at a time: rows of the same sequence in a warp by votes, the warps of a sequence one after another.
+  for (int r0 = 0; r0 < a.N; r0 += kPlanThreads) {
+    const int r = r0 + tid, q = r < a.N ? pl.inv[r] : -1;
+    float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (q >= 0) {
+      int nv = s_n[q];
+      if (a.row_nvis) nv = min(max(a.row_nvis[r], 0), nv);
+      m = make_float4(a.lse ? a.lse[r] : 0.f, (a.weight ? a.weight[r] : 1.f) / wmax, __int_as_float(a.targets[r]), __int_as_float(nv));
+    }
+    const unsigned same = __match_any_sync(0xffffffffu, q);
+    const int rank = __popc(same & ((1u << lane) - 1u));
+    if (q >= 0 && rank == 0) s_warp[q * 32 + warp] = (unsigned short)__popc(same);
+    __syncthreads();
+    int at = -1;
+    if (q >= 0) {
+      at = s_cnt[q] + rank;
+      for (int i = 0; i < warp; ++i) at += s_warp[q * 32 + i];
+    }
+    __syncthreads();
+    if (q >= 0 && rank == 0) { atomicAdd(&s_cnt[q], (int)s_warp[q * 32 + warp]); s_warp[q * 32 + warp] = 0; }
+    if (r < a.N) pl.inv[r] = at;
+    if (at >= 0) { pl.perm[at] = r; pl.meta[at] = m; }
+    __syncthreads();
   }
 }
 
@@ -319,14 +328,17 @@ __global__ void __launch_bounds__(128) k_xent_split(const float* __restrict__ sr
 enum JobType { kLogits, kLogitsHyper, kHidden, kHiddenHyper, kTables, kTablesHyper };
 struct Job {
   int type, b;
-  int m0;                    // first row of the result: vocabulary row, hypertoken or column
-  int r0, n;                 // first column of the result (position, or column of the table), and how many
+  int m0;                    // first row of the result: position (within the sequence), column, or vocabulary row
+  int r0, n;                 // its first column: vocabulary row, position, or column of the table; and how many
   int k0, k16;               // first contracted row, steps of 16
   bool tail;                 // one more step, from the copy of the last hypertokens
-  int limit;                 // rows of a sequence's tile that exist (hypertokens)
+  int limit;                 // positions of the tile that exist
   int part;                  // slot of the result
 };
-__device__ __forceinline__ int pad32(int n) { return (n + 31) & ~31; }
+__host__ __device__ __forceinline__ int pad32(int n) { return (n + 31) & ~31; }
+// Vocabulary tiles of a piece: up to the next multiple of 64, since G's columns are contracted in blocks of 64.
+__host__ __device__ __forceinline__ int pad64(int n) { return (n + 63) & ~63; }
+__host__ __device__ __forceinline__ int vocabulary_tiles(int vn, int nv) { return (pad64(vn) + nv - 1) / nv; }
 
 // Logits of a launch, dealt in turn: all row tiles of a share of the rows for one vocabulary tile, then the next, so
 // that the clusters at work share both operands.
@@ -336,7 +348,7 @@ struct LogitsWalk {
   __device__ LogitsWalk(const Params& pp, int c_, int C_) : p(pp), c(c_), C(C_) {
     const int rows = min(p.pl.head[0], p.r_hi) - p.r_lo;
     live = rows > 0 ? rows : 0;
-    RT = ceil_div(live, p.tr); VT = ceil_div(p.vn, kTile);
+    RT = ceil_div(live, 2 * p.cta_rows); VT = vocabulary_tiles(p.vn, p.nv);
     base = RT * VT;
     hyper = p.hyper ? p.pl.head[1] : 0;
     idx = c;
@@ -348,20 +360,20 @@ struct LogitsWalk {
     if (at < base) {
       const int s = at / (p.sb * VT), rem = at - s * p.sb * VT, in = min(p.sb, RT - s * p.sb), vt = rem / in;
       const int rt = s * p.sb + rem - vt * in;
-      j.type = kLogits; j.b = -1; j.m0 = vt * kTile;
-      j.r0 = p.r_lo + rt * p.tr;
-      j.limit = min(p.tr, live - rt * p.tr);
-      j.n = pad32(j.limit);
+      j.type = kLogits; j.b = -1; j.m0 = p.r_lo + rt * 2 * p.cta_rows;
+      j.limit = min(2 * p.cta_rows, live - rt * 2 * p.cta_rows);
+      j.r0 = vt * p.nv;
+      j.n = min(p.nv, pad64(p.vn) - j.r0);
       j.part = p.part0 + 2 * vt;
       return true;
     }
     if (at - base >= hyper) return false;
     const int b = find_seq(p.pl.j1, p.cb.B, at - base), i = at - base - p.pl.j1[b];
     const int rows = p.pl.cnt[b], rt = ceil_div(rows, p.th), kt = i / rt, q = i - kt * rt;
-    j.type = kLogitsHyper; j.b = b; j.m0 = kt * kTile;
-    j.r0 = q * p.th;                             // (within the sequence)
-    j.limit = min(p.th, rows - j.r0);
-    j.n = pad32(j.limit);
+    j.type = kLogitsHyper; j.b = b; j.m0 = q * p.th;
+    j.limit = min(p.th, rows - j.m0);
+    j.r0 = kt * kTile;
+    j.n = min(kTile, pad32(p.cb.n[b] - j.r0));
     j.part = 2 * kt;
     return true;
   }
@@ -440,6 +452,13 @@ __device__ __forceinline__ int job_products(const Params& p, int type) {
   return type <= kLogitsHyper ? p.np1 : (type <= kHiddenHyper ? p.np2 : p.np3);
 }
 __device__ __forceinline__ int job_blocks(const Job& j) { return (j.k16 + 3) / 4 + (j.tail ? 1 : 0); }
+// The tensor cores' additions into an accumulator truncate: a chain of n of them is off by about n / 2 steps of 2^-24 to
+// one side (losses at d = 4096 were 3e-6 off).  Where that counts an accumulator takes kChain blocks of 64, and the epilogue
+// adds those sums in registers, rounded to nearest, while the MMAs go on in the other accumulator.
+constexpr int kChain = 16;
+__device__ __forceinline__ int job_chain(const Params& p, const Job& j) {
+  return j.type <= kLogitsHyper || (p.exact_sums & (j.type <= kHiddenHyper ? 1 : 2)) ? kChain : 1 << 30;
+}
 
 // MN-major operand of 64-column boxes of 64 rows with the 128-byte swizzle: the next 8 contracted rows are 1024 bytes
 // on (stride byte offset), the next 64 columns 8192 (leading byte offset).
@@ -453,39 +472,10 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
   return d;
 }
 
-// Barrier of the epilogue warps; true if `ok` was true in all their threads.
-__device__ __forceinline__ bool epilogue_all(bool ok) {
-  uint32_t all;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %1, 0;\n\t"
-      "bar.red.and.pred q, 1, %2, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(all)
-      : "r"(ok ? 1u : 0u), "n"(32 * kEpiWarps)
-      : "memory");
-  return all != 0;
-}
-
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
-}
-
-// Sums over the lanes of 32 values each: lane i gets that of value i.
-template <typename Op>
-__device__ __forceinline__ float lanes_to_one(float (&x)[32], int lane, Op op) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const bool up = lane & o;
-#pragma unroll
-    for (int i = 0; i < o; ++i) {
-      const float keep = up ? x[i + o] : x[i], send = up ? x[i] : x[i + o];
-      x[i] = op(keep, __shfl_xor_sync(0xffffffffu, send, o));
-    }
-  }
-  return x[0];
 }
 
 __device__ __forceinline__ void merge_ms(float& m, float& s, float om, float os) {
@@ -498,15 +488,64 @@ __device__ __forceinline__ void merge_ms(float& m, float& s, float om, float os)
 
 enum Kind { kLoss, kGrad, kProducts };
 
-template <int KIND, typename TO>
+// A warp's block of 32 x 32 values, lane = row, to `rows` rows of memory `pitch` elements apart: turned in shared memory (16-byte
+// groups of a row exchanged with its row's low bits), so that a store writes whole sectors of a few rows.  (Stored from the
+// lanes' own rows, 32 lines per instruction, a tile of dW took 15000 clocks.)  cols: columns that exist, a multiple of 8.
+// ADD: to what is there, rounded once.
+template <typename T, bool ADD>
+__device__ __forceinline__ void store_block(float (&v)[32], float4* turn, T* out, long long pitch, int rows, int cols, int lane) {
+  constexpr int kPer = 16 / sizeof(T);           // elements per lane and store
+  constexpr int kLanes = 32 / kPer, kSteps = 32 / (32 / kLanes);       // lanes per row, stores
+  const int row0 = lane / kLanes, col = (lane % kLanes) * kPer;
+  uint4 old[kSteps];
+  if (ADD) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int r = row0 + i * (32 / kLanes);
+      old[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (r < rows && col < cols) old[i] = *reinterpret_cast<const uint4*>(out + r * pitch + col);
+    }
+  }
+  __syncwarp();                                  // (the block before has been read)
+#pragma unroll
+  for (int g = 0; g < 8; ++g) turn[lane * 8 + (g ^ (lane & 7))] = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int r = row0 + i * (32 / kLanes);
+    uint4 o;
+    if constexpr (sizeof(T) == 4) {
+      float4 x = turn[r * 8 + ((col / 4) ^ (r & 7))];
+      if (ADD) {
+        x.x += __uint_as_float(old[i].x); x.y += __uint_as_float(old[i].y); x.z += __uint_as_float(old[i].z); x.w += __uint_as_float(old[i].w);
+      }
+      o = make_uint4(__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(x.z), __float_as_uint(x.w));
+    } else {
+      const float4 x = turn[r * 8 + ((col / 4) ^ (r & 7))], y = turn[r * 8 + ((col / 4 + 1) ^ (r & 7))];
+      const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+      const uint32_t w[4] = {old[i].x, old[i].y, old[i].z, old[i].w};
+      uint32_t t[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float lo = f[2 * k], hi = f[2 * k + 1];
+        if (ADD) { lo += __uint_as_float(w[k] << 16); hi += __uint_as_float(w[k] & 0xffff0000u); }
+        const __nv_bfloat162 pair = __floats2bfloat162_rn(lo, hi);
+        t[k] = *reinterpret_cast<const uint32_t*>(&pair);
+      }
+      o = make_uint4(t[0], t[1], t[2], t[3]);
+    }
+    if (r < rows && col < cols) *reinterpret_cast<uint4*>(out + r * pitch + col) = o;
+  }
+}
+
+// CHAINED: accumulators of kChain blocks, added in registers.
+template <int KIND, bool CHAINED, typename TO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   using Walk = typename std::conditional<KIND == kProducts, GradWalk, LogitsWalk>::type;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Ctrl* ctrl = reinterpret_cast<Ctrl*>(sm);
-  float4* s_meta = reinterpret_cast<float4*>(sm + 1024);
-  float2* s_part = reinterpret_cast<float2*>(sm + 1024 + kMetaBytes);
   const uint32_t stage_base = smem_u32(sm + kFrontBytes);
   const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();       // 0: leader (issues the MMAs), 1: peer
@@ -528,8 +567,9 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   pdl_wait();
   pdl_trigger();
 
-  if (warp == 0) {
-    if (lane == 0) {
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+    if (warp == 0 && lane == 0) {
       // ---------------- TMA producer (both CTAs): own 128 rows of A, own half of B's ----------------------
       const uint64_t pol = policy_evict_last();
       uint32_t full_leader[kStages];
@@ -548,29 +588,26 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             auto expect = [&](uint32_t bytes) { if (rank == 0) mbar_expect_tx(smem_u32(&ctrl->full[stage]), 2u * bytes); };
             if (KIND != kProducts) {
               const bool hy = j.type == kLogitsHyper;
-              expect(16384u + 64u * (uint32_t)(hy ? p.th : p.tr));               // (half a tile of hidden rows, 128 bytes each)
+              expect(16384u + 128u * (uint32_t)(hy ? p.th >> 1 : p.cta_rows));
               if (hy) {
-                tma_load_3d_pair(A, &tm.u_k, kb * 64, j.b * p.cb.cap + j.m0 + rank * 128, p.a1[pr], bar, pol);
-                tma_load_3d_pair(B, &tm.hh_k, kb * 64, h0 + j.r0 + rank * half, p.b1[pr], bar, pol);
+                tma_load_3d_pair(A, &tm.hh_k, kb * 64, h0 + j.m0 + rank * (p.th >> 1), p.a1[pr], bar, pol);
+                tma_load_3d_pair(B, &tm.u_k, kb * 64, j.b * p.cb.cap + j.r0 + rank * half, p.b1[pr], bar, pol);
               } else {
-                tma_load_3d_pair(A, &tm.w_k, kb * 64, p.w_row0 + j.m0 + rank * 128, p.a1[pr], bar, pol);
-                tma_load_3d_pair(B, &tm.hs_k, kb * 64, j.r0 + rank * half, p.b1[pr], bar, pol);
+                tma_load_3d_pair(A, &tm.hs_k, kb * 64, j.m0 + rank * p.cta_rows, p.a1[pr], bar, pol);
+                tma_load_3d_pair(B, &tm.w_k, kb * 64, p.w_row0 + j.r0 + rank * half, p.b1[pr], bar, pol);
               }
             } else if (j.type == kHidden || j.type == kHiddenHyper) {
               const bool hy = j.type == kHiddenHyper, last = kb >= whole;
-              const int nb = half > 64 ? 2 : 1;
-              expect((last ? 4096u : 16384u) + 8192u * nb);
+              expect((last ? 4096u : 16384u) + 64u * (uint32_t)(hy ? p.th : p.tr));            // (G: half a tile's rows)
               const CUtensorMap* am = hy ? (last ? &tm.ut_m : &tm.u_m) : &tm.w_m;
               const int ay = hy ? (last ? j.b * 16 : j.b * p.cb.cap + kb * 64) : p.w_row0 + j.k0 + kb * 64;
-              const CUtensorMap* bm = hy ? &tm.gh_m : &tm.g_m;
-              const int by = last ? j.k16 * 16 : j.k0 + kb * 64, bx = h0 + j.r0 + rank * half;
               for (int i = 0; i < 2; ++i) tma_load_3d_pair(A + 8192u * i, am, j.m0 + rank * 128 + 64 * i, ay, p.a2[pr], bar, pol);
-              for (int i = 0; i < nb; ++i) tma_load_3d_pair(B + 8192u * i, bm, bx + 64 * i, by, p.b2[pr], bar, pol);
+              tma_load_3d_pair(B, hy ? &tm.gh_k : &tm.g_k, last ? j.k16 * 16 : j.k0 + kb * 64, h0 + j.r0 + rank * half, p.b2[pr], bar, pol);
             } else {
               const bool hy = j.type == kTablesHyper;
               const int nb = half > 64 ? 2 : 1;
               expect(16384u + 8192u * nb);
-              tma_load_3d_pair(A, hy ? &tm.gh_k : &tm.g_k, h0 + kb * 64, j.m0 + rank * 128, p.a3[pr], bar, pol);
+              for (int i = 0; i < 2; ++i) tma_load_3d_pair(A + 8192u * i, hy ? &tm.gh_m : &tm.g_m, j.m0 + rank * 128 + 64 * i, h0 + kb * 64, p.a3[pr], bar, pol);
               for (int i = 0; i < nb; ++i)
                 tma_load_3d_pair(B + 8192u * i, hy ? &tm.hh_m : &tm.hs_m, j.r0 + rank * half + 64 * i, h0 + kb * 64, p.b3[pr], bar, pol);
             }
@@ -578,9 +615,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
           }
         }
       }
-    }
-  } else if (warp == 1) {
-    if (rank == 0) {
+    } else if (warp == 1 && rank == 0) {
       // ---------------- MMA issuer (leader only, the whole warp: elect_one()) ------------------------------
       Walk w(p, c, C);
       Job j;
@@ -589,15 +624,22 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
       while (ok && w.next(j)) {
         const int blocks = job_blocks(j), products = job_products(p, j.type), whole = (j.k16 + 3) / 4;
         if (blocks == 0) continue;               // (nothing to contract: the epilogue writes zeros)
-        const uint32_t buf = job_i & 1u, aph = (job_i >> 1) & 1u;
-        if (!mbar_wait_warp(smem_u32(&ctrl->acc_empty[buf]), aph ^ 1u, &ctrl->abort)) { ok = false; break; }
-        tc_fence_after();
-        const bool a_mn = j.type == kHidden || j.type == kHiddenHyper, b_mn = KIND == kProducts;
+        const int chain = CHAINED ? job_chain(p, j) : 1 << 30;
+        int left = 0;                            // blocks until the accumulator changes
+        const bool a_mn = KIND == kProducts, b_mn = j.type >= kTables;
         const uint32_t idesc = idesc_bf16_f32(kTile, j.n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
-        const uint32_t D = tmem_base + buf * kTile;
-        uint32_t acc = 0;
+        uint32_t acc = 0, D = 0;
         for (int pr = 0; pr < products && ok; ++pr) {
           for (int kb = 0; kb < blocks; ++kb) {
+            if (left == 0) {
+              if (acc) { if (elect_one()) umma_commit_pair(smem_u32(&ctrl->acc_full[job_i & 1u])); __syncwarp(); ++job_i; }
+              if (!mbar_wait_warp(smem_u32(&ctrl->acc_empty[job_i & 1u]), ((job_i >> 1) & 1u) ^ 1u, &ctrl->abort)) { ok = false; break; }
+              tc_fence_after();
+              D = tmem_base + (job_i & 1u) * kTile;
+              acc = 0;
+              left = chain;
+            }
+            --left;
             if (!mbar_wait_warp(smem_u32(&ctrl->full[stage]), phase, &ctrl->abort)) { ok = false; break; }
             tc_fence_after();
             const uint32_t A = stage_base + (uint32_t)stage * kStageBytes, B = A + 16384u;
@@ -606,7 +648,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 if (k < steps)
-                  umma_bf16_pair(D, KIND == kProducts && a_mn ? smem_desc_mn(A + k * 2048) : smem_desc_sw128(A + k * 32),
+                  umma_bf16_pair(D, a_mn ? smem_desc_mn(A + k * 2048) : smem_desc_sw128(A + k * 32),
                                  b_mn ? smem_desc_mn(B + k * 2048) : smem_desc_sw128(B + k * 32), idesc, k ? 1u : acc);
               }
               umma_commit_pair(smem_u32(&ctrl->empty[stage]));
@@ -617,15 +659,17 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
           }
         }
         if (!ok) break;
-        if (elect_one()) umma_commit_pair(smem_u32(&ctrl->acc_full[buf]));
+        if (elect_one()) umma_commit_pair(smem_u32(&ctrl->acc_full[job_i & 1u]));
         __syncwarp();
         ++job_i;
       }
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));
     // ---------------- epilogue (both CTAs): thread = row of the result (x every other 32 columns) -----------
-    const int q = warp & 3, half = (warp - 2) >> 2, et = threadIdx.x - 64;
-    const int in_tile = rank * 128 + q * 32 + lane;
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    const int in_cta = q * 32 + lane, in_tile = rank * 128 + in_cta;
+    float4* turn = reinterpret_cast<float4*>(sm + 1024 + (warp - 4) * kTurnBytes);
     uint32_t acc_empty_leader[2];
     acc_empty_leader[0] = map_to_cta(smem_u32(&ctrl->acc_empty[0]), 0);
     acc_empty_leader[1] = map_to_cta(smem_u32(&ctrl->acc_empty[1]), 0);
@@ -635,177 +679,171 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
     uint32_t job_i = 0;
     bool ok = true;
     while (ok && w.next(j)) {
-      const bool some = job_blocks(j) > 0;
-      const uint32_t buf = job_i & 1u, aph = (job_i >> 1) & 1u;
-      const uint32_t tbase = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile;
-      if constexpr (KIND != kProducts) {
-        // what the tile's hidden rows are; the buffer of the job before last is free once all are at this job
-        float4* meta = s_meta + (job_i & 1u) * kTile;
-        const int pos0 = j.b >= 0 ? p.pl.s0[j.b] + j.r0 : j.r0;
-        if (et < j.n) meta[et] = et < j.limit ? p.pl.meta[pos0 + et] : make_float4(0.f, 0.f, __int_as_float(-1), __int_as_float(-1));
-        ok = mbar_wait(smem_u32(&ctrl->acc_full[buf]), aph, &ctrl->abort);
-        ok = epilogue_all(ok);
-        if (!ok) break;
+      const int blocks = job_blocks(j) * job_products(p, j.type), chain = CHAINED ? job_chain(p, j) : 1 << 30;
+      const bool some = blocks > 0;
+      auto wait_full = [&]() {
+        const bool good = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctrl->acc_full[job_i & 1u]), (job_i >> 1) & 1u, &ctrl->abort));
         tc_fence_after();
-        const int m = j.m0 + in_tile, limit = j.b >= 0 ? p.cb.n[j.b] : p.vn;       // row of the piece, or hypertoken
-        const int id = j.b >= 0 ? p.cb.V + m : p.v0 + m;
-        const bool there = m < limit;
-        for (int c0 = 32 * half; c0 < j.n; c0 += 64) {
-          uint32_t v[32];
-          tmem_ld32(tbase + c0, v);
-          tmem_ld_wait();
-          if constexpr (KIND == kGrad) {
-            const long long row = j.b >= 0 ? (long long)m * p.gh_pitch + p.pl.h0[j.b] + j.r0 + c0 : (long long)m * p.g_pitch + j.r0 + c0;
-            __nv_bfloat16* out = (j.b >= 0 ? p.gh : p.g) + row;
-            const long long plane = j.b >= 0 ? p.gh_plane : p.g_plane;
-#pragma unroll
-            for (int x = 0; x < 32; ++x) {
-              const float4 r = meta[c0 + x];
-              const float l = __uint_as_float(v[x]);
-              const float e = p.exact_exp ? expf(l - r.x) : ex2((l - r.x) * kLog2e);
-              const bool sees = there && r.y != 0.f && (j.b < 0 || m < __float_as_int(r.w));
-              v[x] = __float_as_uint(sees ? r.y * (e - (__float_as_int(r.z) == id ? 1.f : 0.f)) : 0.f);
-            }
-            for (int part = 0; part < p.g_parts; ++part) {
-              uint32_t o[16];
-#pragma unroll
-              for (int x = 0; x < 16; ++x) {
-                const __nv_bfloat162 t = __floats2bfloat162_rn(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1]));
-                o[x] = *reinterpret_cast<const uint32_t*>(&t);
-                if (part + 1 < p.g_parts) {
-                  v[2 * x] = __float_as_uint(__uint_as_float(v[2 * x]) - __low2float(t));
-                  v[2 * x + 1] = __float_as_uint(__uint_as_float(v[2 * x + 1]) - __high2float(t));
-                }
-              }
-#pragma unroll
-              for (int x = 0; x < 4; ++x)
-                *reinterpret_cast<uint4*>(out + (size_t)part * plane + 8 * x) = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
-            }
-          } else {
-            // Sum of exponentials of 32 vocabulary rows for each of 32 hidden rows.  One reference for all of them
-            // while their logits are within 40 of another: the lanes' values are then reduced once, otherwise
-            // the maxima of the hidden rows are found first.
-            float x[32], top = -INFINITY, low = INFINITY;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float4 r = meta[c0 + i];
-              const float l = __uint_as_float(v[i]);
-              if (there && __float_as_int(r.z) == id) p.tl[pos0 + c0 + i] = l;
-              const bool sees = there && (j.b < 0 ? c0 + i < j.limit : m < __float_as_int(r.w));
-              x[i] = sees ? l : -INFINITY;
-              top = sees ? fmaxf(top, l) : top;
-              low = sees ? fminf(low, l) : low;
-            }
-            bool odd = false;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) odd |= x[i] != x[i] || x[i] == INFINITY;
-#pragma unroll
-            for (int o = 16; o; o >>= 1) {
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-              low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
-            }
-            odd = __any_sync(0xffffffffu, odd);
-            float ref;                                                           // of hidden row c0 + lane
-            if (!odd && (top == -INFINITY || top - low < 40.f)) {
-              ref = top;
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = top == -INFINITY ? 0.f : ex2((x[i] - top) * kLog2e);
-            } else {
-              float y[32];
-#pragma unroll
-              for (int i = 0; i < 32; ++i) y[i] = x[i] != x[i] ? INFINITY : x[i];
-              ref = lanes_to_one(y, lane, [](float a, float b) { return fmaxf(a, b); });
-#pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const float r = __shfl_sync(0xffffffffu, ref, i);
-                x[i] = r == -INFINITY ? 0.f : ex2((x[i] - r) * kLog2e);                     // (+inf: inf - inf, a NaN in the sum)
-              }
-            }
-            const float s = lanes_to_one(x, lane, [](float a, float b) { return a + b; });
-            s_part[q * kTile + c0 + lane] = make_float2(ref, s);
-          }
-        }
+        return good;
+      };
+      auto release = [&]() {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(acc_empty_leader[buf]);
-        if constexpr (KIND == kLoss) {
-          epilogue_all(true);
-          if (et < j.limit) {
-            float m_ = -INFINITY, s_ = 0.f;
-            for (int i = 0; i < 4; ++i) { const float2 v = s_part[i * kTile + et]; merge_ms(m_, s_, v.x, v.y); }
-            float2* out = j.b >= 0 ? p.part_h + (size_t)(j.part + rank) * p.part_rows_h + pos0 + et
-                                   : p.part + (size_t)(j.part + rank) * p.part_rows + pos0 - p.r_lo + et;
-            *out = make_float2(m_, s_);
-          }
-        }
+        if (lane == 0) mbar_arrive_cluster(acc_empty_leader[job_i & 1u]);
         ++job_i;
-      } else {
-        if (some) {
-          if (!mbar_wait(smem_u32(&ctrl->acc_full[buf]), aph, &ctrl->abort)) { ok = false; break; }
-          __syncwarp();
-          tc_fence_after();
-        }
-        const int m = j.m0 + in_tile;
-        if (j.type == kHidden || j.type == kHiddenHyper) {
-          const bool set = p.first || j.type == kHiddenHyper;
-          const int pos0 = j.b >= 0 ? p.pl.s0[j.b] + j.r0 : j.r0;
-          float* out = p.dh + (size_t)j.part * p.dh_slot + (size_t)pos0 * p.d + m;
-          for (int c0 = 32 * half; c0 < j.n && (some || set); c0 += 64) {
-            uint32_t v[32];
-            if (some) { tmem_ld32(tbase + c0, v); tmem_ld_wait(); }
-            if (m >= p.d) continue;
-            float old[32];
+      };
+      auto load = [&](int c0, float (&v)[32]) {
+        uint32_t x[32];
+        tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (job_i & 1u) * kTile + c0, x);
+        tmem_ld_wait();
 #pragma unroll
-            for (int x = 0; x < 32; ++x) {
-              if (!some) v[x] = 0u;
-              old[x] = !set && c0 + x < j.limit ? out[(size_t)(c0 + x) * p.d] : 0.f;
+        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(x[i]);
+      };
+      float acc[CHAINED ? 4 : 1][32];            // columns 32 (half + 2 g) + x
+      if constexpr (CHAINED) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int x = 0; x < 32; ++x) acc[g][x] = 0.f;
+        for (int at = 0; at < blocks; at += min(chain, blocks)) {
+          if (!wait_full()) { ok = false; break; }
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int c0 = 32 * half + 64 * g;
+            if (c0 < j.n) {
+              float v[32];
+              load(c0, v);
+#pragma unroll
+              for (int x = 0; x < 32; ++x) acc[g][x] += v[x];
             }
-#pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (c0 + x < j.limit) out[(size_t)(c0 + x) * p.d] = old[x] + __uint_as_float(v[x]);
           }
-        } else if (some || !p.acc) {
-          const int rows = j.b >= 0 ? p.cb.n[j.b] : p.vn;
-          TO* out = j.b >= 0 ? reinterpret_cast<TO*>(p.gUh) + ((size_t)j.b * p.cb.cap + m) * p.d + j.r0
-                             : reinterpret_cast<TO*>(p.gWU) + (size_t)(p.v0 + m) * p.d + j.r0;
-          const int cols = min(j.n, p.d - j.r0);
-          for (int c0 = 32 * half; c0 < cols; c0 += 64) {
-            uint32_t v[32];
-            if (some) { tmem_ld32(tbase + c0, v); tmem_ld_wait(); }
-            if (m >= rows) continue;
+          release();
+        }
+        if (!ok) break;
+      } else if (some && !wait_full()) { ok = false; break; }
+      // `use` gets the sums of every group of 32 columns of this warp
+      auto groups = [&](auto&& use) {
 #pragma unroll
-            for (int x = 0; x < 32; x += 8) {
-              if (c0 + x >= cols) break;         // (columns come in eights)
-              float r[8];
+        for (int g = 0; g < 4; ++g) {
+          const int c0 = 32 * half + 64 * g;
+          if (c0 >= j.n) continue;
+          if constexpr (CHAINED) use(c0, acc[g]);
+          else {
+            if (some) load(c0, acc[0]);
+            use(c0, acc[0]);
+          }
+        }
+        if constexpr (!CHAINED) { if (some) release(); }
+      };
+      if constexpr (KIND != kProducts) {
+        const bool hy = j.b >= 0;
+        const int cta_rows = hy ? p.th >> 1 : p.cta_rows, row = rank * cta_rows + in_cta;       // of the tile
+        const bool there = in_cta < cta_rows && row < j.limit;
+        const int pos = (hy ? p.pl.s0[j.b] : 0) + j.m0 + row;
+        float4 r = make_float4(0.f, 0.f, __int_as_float(-1), __int_as_float(0));
+        if (there) r = p.pl.meta[pos];
+        const int target = __float_as_int(r.z) - (hy ? p.cb.V : p.v0) - j.r0;                   // its column of the tile, if it has it
+        const int limit = !there ? 0 : (hy ? min(__float_as_int(r.w), p.cb.n[j.b]) : p.vn) - j.r0;       // columns that the row sees
+        if constexpr (KIND == kGrad) {
+          // rows up to the next multiple of 32 get zeros: they are contracted in steps of 16
+          const int first = rank * cta_rows + q * 32;
+          const int rows = min(min(32, cta_rows - q * 32), pad32(j.limit) - first);
+          __nv_bfloat16* out = hy ? p.gh + (size_t)(p.pl.h0[j.b] + j.m0 + first) * p.gh_pitch + j.r0 : p.g + (size_t)(j.m0 + first) * p.g_pitch + j.r0;
+          const long long plane = hy ? p.gh_plane : p.g_plane, pitch = hy ? p.gh_pitch : p.g_pitch;
+          const float lse = r.x, weight = r.y;
+          groups([&](int c0, float (&v)[32]) {
+            const int see = weight != 0.f ? limit - c0 : 0;
+            if (p.exact_exp) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) r[i] = some ? scale * __uint_as_float(v[x + i]) : 0.f;
-              TO* to = out + c0 + x;
-              if constexpr (sizeof(TO) == 4) {
-                float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-                if (p.acc) { a = *reinterpret_cast<const float4*>(to); b = *reinterpret_cast<const float4*>(to + 4); }
-                *reinterpret_cast<float4*>(to) = make_float4(a.x + r[0], a.y + r[1], a.z + r[2], a.w + r[3]);
-                *reinterpret_cast<float4*>(to + 4) = make_float4(b.x + r[4], b.y + r[5], b.z + r[6], b.w + r[7]);
-              } else {
-                uint4 o = make_uint4(0u, 0u, 0u, 0u);
-                if (p.acc) o = *reinterpret_cast<const uint4*>(to);
-                uint32_t* ow = reinterpret_cast<uint32_t*>(&o);
+              for (int x = 0; x < 32; ++x) v[x] = weight * (expf(v[x] - lse) - (x == target - c0 ? 1.f : 0.f));
+            } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const __nv_bfloat162 before = *reinterpret_cast<const __nv_bfloat162*>(&ow[i]);
-                  const __nv_bfloat162 t = __floats2bfloat162_rn(__low2float(before) + r[2 * i], __high2float(before) + r[2 * i + 1]);
-                  ow[i] = *reinterpret_cast<const uint32_t*>(&t);
-                }
-                *reinterpret_cast<uint4*>(to) = o;
+              for (int x = 0; x < 32; ++x) v[x] = weight * (ex2((v[x] - lse) * kLog2e) - (x == target - c0 ? 1.f : 0.f));
+            }
+            if (__any_sync(0xffffffffu, see < 32)) {
+#pragma unroll
+              for (int x = 0; x < 32; ++x) v[x] = x < see ? v[x] : 0.f;
+            }
+            if (rows <= 0) return;
+            for (int part = 0; part < p.g_parts; ++part) {
+              store_block<__nv_bfloat16, false>(v, turn, out + (size_t)part * plane + c0, pitch, rows, 32, lane);
+              if (part + 1 < p.g_parts) {
+#pragma unroll
+                for (int x = 0; x < 32; ++x) v[x] -= __bfloat162float(__float2bfloat16_rn(v[x]));
               }
             }
+          });
+        } else {
+          float m = -INFINITY, s = 0.f;
+          groups([&](int c0, float (&v)[32]) {
+            const int see = limit - c0;
+            if (!__any_sync(0xffffffffu, see > 0)) return;
+            if (__any_sync(0xffffffffu, see < 32)) {
+#pragma unroll
+              for (int x = 0; x < 32; ++x) v[x] = x < see ? v[x] : -INFINITY;
+            }
+            const int at = target - c0;
+            if (at >= 0 && at < 32 && at < see) {
+              float l = v[0];
+#pragma unroll
+              for (int x = 1; x < 32; ++x) l = x == at ? v[x] : l;
+              p.tl[pos] = l;
+            }
+            float top = v[0];
+#pragma unroll
+            for (int x = 1; x < 32; ++x) top = fmaxf(top, v[x]);
+            bool nan = false;
+            if (top == -INFINITY) {              // nothing here, or NaN
+#pragma unroll
+              for (int x = 0; x < 32; ++x) nan |= v[x] != v[x];
+            } else {
+              top = fmaxf(top, m);
+              s *= m == top ? 1.f : ex2((m - top) * kLog2e);
+              m = top;
+              float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
+#pragma unroll
+              for (int x = 0; x < 32; x += 4) {
+                a0 += ex2((v[x] - m) * kLog2e); a1 += ex2((v[x + 1] - m) * kLog2e);
+                a2 += ex2((v[x + 2] - m) * kLog2e); a3 += ex2((v[x + 3] - m) * kLog2e);
+              }
+              s += (a0 + a1) + (a2 + a3);
+              nan = s != s;                      // (+inf: inf - inf)
+            }
+            if (nan) { m = INFINITY; s = __int_as_float(0x7fc00000); }
+          });
+          if (there) {
+            float2* out = hy ? p.part_h + (size_t)(j.part + half) * p.part_rows_h + pos : p.part + (size_t)(j.part + half) * p.part_rows + pos - p.r_lo;
+            *out = make_float2(m, s);
           }
         }
-        if (some) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(acc_empty_leader[buf]);
-          ++job_i;
-        }
+      } else if (j.type == kHidden || j.type == kHiddenHyper) {
+        const int m = j.m0 + in_tile, pos0 = (j.b >= 0 ? p.pl.s0[j.b] : 0) + j.r0;
+        const bool set = p.first || j.type == kHiddenHyper;
+        float* out = p.dh + (size_t)j.part * p.dh_slot + (size_t)pos0 * p.d + m;
+        groups([&](int c0, float (&v)[32]) {
+          if (m >= p.d || !(some || set)) return;
+#pragma unroll
+          for (int x0 = 0; x0 < 32; x0 += 8) {
+            float old[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) old[x] = !set && c0 + x0 + x < j.limit ? out[(size_t)(c0 + x0 + x) * p.d] : 0.f;
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              if (c0 + x0 + x < j.limit) out[(size_t)(c0 + x0 + x) * p.d] = some ? old[x] + v[x0 + x] : old[x];
+          }
+        });
+      } else {
+        const int first = j.m0 + rank * 128 + q * 32, rows = (j.b >= 0 ? p.cb.n[j.b] : p.vn) - first;
+        const int cols = min(j.n, p.d - j.r0);
+        TO* out = (j.b >= 0 ? reinterpret_cast<TO*>(p.gUh) + ((size_t)j.b * p.cb.cap + first) * p.d
+                            : reinterpret_cast<TO*>(p.gWU) + (size_t)(p.v0 + first) * p.d) + j.r0;
+        groups([&](int c0, float (&v)[32]) {
+          if (rows <= 0 || c0 >= cols || !(some || !p.acc)) return;
+#pragma unroll
+          for (int x = 0; x < 32; ++x) v[x] = some ? scale * v[x] : 0.f;
+          if (p.acc) store_block<TO, true>(v, turn, out + c0, p.d, rows, cols - c0, lane);
+          else store_block<TO, false>(v, turn, out + c0, p.d, rows, cols - c0, lane);
+        });
       }
     }
   }
@@ -816,30 +854,50 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   if (warp == 2) tmem_dealloc_pair(tmem_base, 512);
 }
 
-// Eight threads per row: the partial sums of its vocabulary and hypertoken tiles, its loss and lse.
-__global__ void __launch_bounds__(256) k_xent_merge(CbView cb, RowArgs a, Plan pl, const float2* part, int part_rows, int parts,
-                                                    const float2* part_h, int part_rows_h, const float* tl, int r_lo, int r_hi) {
+// 32 threads per row, a warp for 32 rows each: the partial sums of its vocabulary and hypertoken tiles, its loss and lse.
+__global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan pl, const float2* part, int part_rows, int parts,
+                                                     const float2* part_h, int part_rows_h, const float* tl, int r_lo, int r_hi) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float2 s_ms[8][32];
+  __shared__ float2 s_ms[32][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5, pos = r_lo + blockIdx.x * 32 + x;
   const bool live = pos < min(pl.head[0], r_hi);
   float m = -INFINITY, s = 0.f;
-  int row = 0;
   if (live) {
-    row = pl.perm[pos];
-    const int b = a.row_seq ? a.row_seq[row] : row;
-    for (int i = y; i < parts; i += 8) { const float2 v = part[(size_t)i * part_rows + pos - r_lo]; merge_ms(m, s, v.x, v.y); }
-    const int hyper = 2 * ceil_div(cb.n[b], kTile);
-    for (int i = y; i < hyper; i += 8) { const float2 v = part_h[(size_t)i * part_rows_h + pos]; merge_ms(m, s, v.x, v.y); }
+    auto all = [&](const float2* from, size_t stride, int count) {
+      constexpr int kAhead = 8;
+      for (int i = y; i < count; i += 32 * kAhead) {
+        float2 v[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) v[u] = i + 32 * u < count ? from[(size_t)(i + 32 * u) * stride] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) merge_ms(m, s, v[u].x, v[u].y);
+      }
+    };
+    all(part + pos - r_lo, part_rows, parts);
+    if (cb.cap > 0) {
+      const int row = pl.perm[pos], b = a.row_seq ? a.row_seq[row] : row;
+      all(part_h + pos, part_rows_h, 2 * ceil_div(cb.n[b], kTile));
+    }
   }
-  s_ms[y][x] = make_float2(m, s);
+  s_ms[x][y] = make_float2(m, s);
   __syncthreads();
-  if (y != 0 || !live) return;
-  for (int i = 1; i < 8; ++i) merge_ms(m, s, s_ms[i][x].x, s_ms[i][x].y);
+  // a warp per row from here on
+  const int p2 = r_lo + blockIdx.x * 32 + y;
+  const float2 v = s_ms[y][x];
+  m = v.x; s = v.y;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o);
+    // (both lanes of a pair add in the same order)
+    if (x & o) { float lm = om, ls = os; merge_ms(lm, ls, m, s); m = lm; s = ls; }
+    else merge_ms(m, s, om, os);
+  }
+  if (x != 0 || p2 >= min(pl.head[0], r_hi)) return;
+  const int row = pl.perm[p2];
   const float ls = logf(s);
   a.lse_out[row] = m + ls;
-  a.loss_out[row] = ls + (m - tl[pos]);
+  a.loss_out[row] = ls + (m - tl[p2]);
 }
 
 // dh of a row: its partial sums, those of the vocabulary's parts first, times the largest weight.
@@ -911,6 +969,7 @@ struct Shape {
   int N, d, V, B, cap, dtype, parts;             // parts: bf16 parts of an operand
   int grad_dtype, g_parts;                       // < 0: losses alone
   int np, nh;                                    // rows of the sorted copy, and beside hypertokens
+  int cta_rows, nv;
   int tr, th, dt, split;
   int pieces, vc;                                // vocabulary rows per piece, a multiple of 256
 };
@@ -922,6 +981,7 @@ Shape shape_of(const z2z_config& c, int N, int grad_dtype, long long vc) {
   s.g_parts = grad_dtype < 0 ? 0 : (s.parts > 1 || grad_dtype == Z2Z_DTYPE_FP32 ? kMaxParts : 1);
   s.np = (int)up_to(N, kTile);
   s.nh = (int)up_to((long long)N + (long long)(kHyperPad - 1) * (N < c.B ? N : c.B), kTile);
+  s.cta_rows = N > 192 ? 128 : (int)up_to((N + 1) / 2, 16);
   // row tiles of equal height
   const int rt = (N + kTile - 1) / kTile;
   s.tr = (int)up_to((N + rt - 1) / rt, 32);
@@ -937,6 +997,12 @@ Shape shape_of(const z2z_config& c, int N, int grad_dtype, long long vc) {
   s.pieces = (int)((c.V + vc - 1) / vc);
   s.vc = (int)up_to((c.V + s.pieces - 1) / s.pieces, kTile);
   s.pieces = (c.V + s.vc - 1) / s.vc;
+  // One row tile: as many vocabulary rows per tile as make its rounds of all clusters even.
+  s.nv = kTile;
+  if (rt == 1) {
+    const int rounds = (s.vc + kClusters * kTile - 1) / (kClusters * kTile), each = (s.vc + rounds * kClusters - 1) / (rounds * kClusters);
+    s.nv = (int)up_to(each, 32);
+  }
   return s;
 }
 
@@ -956,7 +1022,7 @@ Layout layout_of(const Shape& s, char* base) {
   auto take = [&](size_t bytes) { char* r = base + o; o = (size_t)up_to((long long)(o + bytes), 256); return r; };
   const size_t row = (size_t)s.d * 2 * s.parts;
   l.pl.head = (int32_t*)take(32);
-  l.pl.cnt = (int32_t*)take((size_t)s.B * 4); l.pl.wmax = (float*)take((size_t)s.B * 4);
+  l.pl.cnt = (int32_t*)take((size_t)s.B * 4);
   int32_t** tables[] = {&l.pl.s0, &l.pl.h0, &l.pl.j1, &l.pl.j2, &l.pl.j3};
   for (int32_t** t : tables) *t = (int32_t*)take((size_t)(s.B + 1) * 4);
   l.pl.perm = (int32_t*)take((size_t)s.np * 4); l.pl.inv = (int32_t*)take((size_t)s.np * 4);
@@ -968,7 +1034,7 @@ Layout layout_of(const Shape& s, char* base) {
   }
   if (s.parts > 1) l.wp = (__nv_bfloat16*)take(row * s.vc);
   if (s.grad_dtype < 0) {
-    const int vt = (s.V + kTile - 1) / kTile, rows = s.np < kLossRows ? s.np : kLossRows;
+    const int vt = s.pieces * vocabulary_tiles(s.vc, s.nv), rows = s.np < kLossRows ? s.np : kLossRows;
     l.part = (float2*)take((size_t)2 * vt * rows * 8);
     if (s.cap > 0) l.part_h = (float2*)take((size_t)2 * (hyper_rows(s) / kTile) * s.np * 8);
     l.tl = (float*)take((size_t)s.np * 4);
@@ -1041,9 +1107,9 @@ void products(int parts_a, int parts_b, int* n, int8_t* a, int8_t* b) {
     }
 }
 
-template <int KIND, typename TO>
+template <int KIND, bool CHAINED, typename TO>
 cudaError_t launch_main(const Params& p, const Maps& tm, int clusters, cudaStream_t s) {
-  auto kern = k_xent<KIND, TO>;
+  auto kern = k_xent<KIND, CHAINED, TO>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   if (e != cudaSuccess) return e;
   return launch_pdl(kern, dim3(2 * clusters), dim3(kThreads), kSmemBytes, s, p, tm);
@@ -1062,9 +1128,9 @@ cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x,
   a.th = sh.th; a.dt = sh.dt;
   if (grad) { a.weight = x.weight; a.lse = x.lse; a.hidden = x.g_hidden != nullptr; a.tables = x.g_Uh != nullptr; }
   else { a.loss_out = x.loss; a.lse_out = x.lse; }
-  cudaError_t e = launch_pdl(k_xent_count, dim3((sh.B + 3) / 4), dim3(128), 0, s, cb, a, l.pl);
+  cudaError_t e = cudaFuncSetAttribute(k_xent_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan_shared_bytes(1024));
   if (e != cudaSuccess) return e;
-  if ((e = launch_pdl(k_xent_place, dim3((sh.B + 4) / 4), dim3(128), 0, s, cb, a, l.pl)) != cudaSuccess) return e;
+  if ((e = launch_pdl(k_xent_plan, dim3(1), dim3(kPlanThreads), plan_shared_bytes(sh.B), s, cb, a, l.pl)) != cudaSuccess) return e;
   GatherArgs g{};
   g.hidden = x.hidden; g.Uh = x.Uh; g.d = d; g.positions = sh.np;
   g.hs = l.hs; g.hs_plane = (long long)sh.np * d;
@@ -1077,7 +1143,7 @@ cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x,
   if (e != cudaSuccess) return e;
 
   Params p{};
-  p.cb = cb; p.pl = l.pl; p.d = d; p.dt = sh.dt; p.tr = sh.tr; p.th = sh.th;
+  p.cb = cb; p.pl = l.pl; p.d = d; p.dt = sh.dt; p.cta_rows = sh.cta_rows; p.nv = sh.nv; p.tr = sh.tr; p.th = sh.th;
   products(sh.parts, sh.parts, &p.np1, p.a1, p.b1);
   // dh has the session's type: of three parts of g for fp32 tables' gradients it takes the first
   if (grad) {
@@ -1085,32 +1151,33 @@ cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x,
     products(sh.g_parts, sh.parts, &p.np3, p.a3, p.b3);
   }
   p.g_parts = sh.g_parts; p.exact_exp = sh.g_parts > 1;
-  p.g = l.g; p.g_pitch = sh.np; p.g_plane = (long long)sh.vc * sh.np;
-  p.gh = l.gh; p.gh_pitch = sh.nh; p.gh_plane = (long long)hyper_rows(sh) * sh.nh;
+  p.exact_sums = (sh.parts > 1 ? 1 : 0) | (sh.g_parts > 1 ? 2 : 0);
+  p.g = l.g; p.g_pitch = sh.vc; p.g_plane = (long long)sh.vc * sh.np;
+  p.gh = l.gh; p.gh_pitch = hyper_rows(sh); p.gh_plane = (long long)hyper_rows(sh) * sh.nh;
   p.part = l.part; p.part_h = l.part_h; p.part_rows_h = sh.np; p.tl = l.tl;
   p.split = sh.split; p.dh = grad && x.g_hidden ? l.dh : nullptr; p.dh_slot = (long long)sh.np * d;
   p.gWU = x.g_WU; p.gUh = sh.cap > 0 ? x.g_Uh : nullptr; p.acc = x.accumulate ? 1 : 0;
   p.mem_cycles = kTile * kTile * (x.grad_dtype == Z2Z_DTYPE_FP32 ? 4 : 2) * (x.accumulate ? 2 : 1) / 46;
   p.err = x.err;
   // hidden rows of the row tiles that are taken through all vocabulary tiles together: a quarter of L2
-  const long long tile_bytes = (long long)sh.tr * d * 2 * sh.parts;
+  const long long tile_bytes = (long long)2 * sh.cta_rows * d * 2 * sh.parts;
   p.sb = (int)((32ll << 20) / tile_bytes); if (p.sb < 1) p.sb = 1;
 
   Maps tm{};
   const long long ur = (long long)sh.B * sh.cap;
-  bool ok = make_map(&tm.hs_k, l.hs, sh.np, d, d, sh.parts, g.hs_plane, sh.tr / 2);
+  bool ok = make_map(&tm.hs_k, l.hs, sh.np, d, d, sh.parts, g.hs_plane, sh.cta_rows);
   if (sh.cap > 0) {
     const void* U = sh.parts > 1 ? l.up : x.Uh;
     ok = ok && make_map(&tm.u_k, U, ur, d, d, sh.parts, g.up_plane, 128) && make_map(&tm.hh_k, l.hh, sh.nh, d, d, sh.parts, g.hh_plane, sh.th / 2);
     if (grad)
       ok = ok && make_map(&tm.u_m, U, ur, d, d, sh.parts, g.up_plane, 64) && make_map(&tm.ut_m, l.ut, sh.B * 16, d, d, sh.parts, g.ut_plane, 16) &&
            make_map(&tm.hh_m, l.hh, sh.nh, d, d, sh.parts, g.hh_plane, 64) &&
-           make_map(&tm.gh_k, l.gh, hyper_rows(sh), sh.nh, sh.nh, sh.g_parts, p.gh_plane, 128) &&
-           make_map(&tm.gh_m, l.gh, hyper_rows(sh), sh.nh, sh.nh, sh.g_parts, p.gh_plane, 64);
+           make_map(&tm.gh_k, l.gh, sh.nh, hyper_rows(sh), hyper_rows(sh), sh.g_parts, p.gh_plane, sh.th / 2) &&
+           make_map(&tm.gh_m, l.gh, sh.nh, hyper_rows(sh), hyper_rows(sh), sh.g_parts, p.gh_plane, 64);
   }
   if (grad)
     ok = ok && make_map(&tm.hs_m, l.hs, sh.np, d, d, sh.parts, g.hs_plane, 64) &&
-         make_map(&tm.g_k, l.g, sh.vc, sh.np, sh.np, sh.g_parts, p.g_plane, 128) && make_map(&tm.g_m, l.g, sh.vc, sh.np, sh.np, sh.g_parts, p.g_plane, 64);
+         make_map(&tm.g_k, l.g, sh.np, sh.vc, sh.vc, sh.g_parts, p.g_plane, sh.tr / 2) && make_map(&tm.g_m, l.g, sh.np, sh.vc, sh.vc, sh.g_parts, p.g_plane, 64);
   const void* W = sh.parts > 1 ? l.wp : x.WU;
   const long long w_rows = sh.parts > 1 ? sh.vc : sh.V, w_plane = (long long)sh.vc * d;
   ok = ok && make_map(&tm.w_k, W, w_rows, d, d, sh.parts, w_plane, 128) && make_map(&tm.w_m, W, w_rows, d, d, sh.parts, w_plane, 64);
@@ -1123,23 +1190,24 @@ cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x,
     for (int i = 0; i < sh.pieces; ++i) {
       p.v0 = i * sh.vc; p.vn = sh.V - p.v0 < sh.vc ? sh.V - p.v0 : sh.vc;
       p.w_row0 = sh.parts > 1 ? 0 : p.v0;
-      p.part0 = 2 * i * (sh.vc / kTile);
+      p.part0 = 2 * i * vocabulary_tiles(sh.vc, sh.nv);
       p.first = i == 0;
       p.hyper = i == 0 && r0 == 0 && sh.cap > 0;
       p.hyper_hidden = p.hyper && p.dh;
       if (sh.parts > 1)
         if ((e = launch_pdl(k_xent_split, dim3(p.vn < 4096 ? p.vn : 4096), dim3(128), 0, s, reinterpret_cast<const float*>(x.WU) + (size_t)p.v0 * d, l.wp, w_plane, p.vn, d)) != cudaSuccess) return e;
-      if (!grad) {
-        if ((e = launch_main<kLoss, float>(p, tm, clusters, s)) != cudaSuccess) return e;
-        continue;
-      }
-      if ((e = launch_main<kGrad, float>(p, tm, clusters, s)) != cudaSuccess) return e;
-      e = x.grad_dtype == Z2Z_DTYPE_FP32 ? launch_main<kProducts, float>(p, tm, clusters, s) : launch_main<kProducts, __nv_bfloat16>(p, tm, clusters, s);
+      const bool chained = p.np1 * ((d + 63) / 64) > kChain;                // (logits)
+      if (!grad) e = chained ? launch_main<kLoss, true, float>(p, tm, clusters, s) : launch_main<kLoss, false, float>(p, tm, clusters, s);
+      else e = chained ? launch_main<kGrad, true, float>(p, tm, clusters, s) : launch_main<kGrad, false, float>(p, tm, clusters, s);
+      if (e == cudaSuccess && grad)
+        e = x.grad_dtype == Z2Z_DTYPE_FP32 ? launch_main<kProducts, true, float>(p, tm, clusters, s)
+            : p.exact_sums                 ? launch_main<kProducts, true, __nv_bfloat16>(p, tm, clusters, s)
+                                           : launch_main<kProducts, false, __nv_bfloat16>(p, tm, clusters, s);
       if (e != cudaSuccess) return e;
     }
     if (!grad) {
-      const int rows = p.r_hi - p.r_lo, vt = (sh.V + kTile - 1) / kTile;
-      if ((e = launch_pdl(k_xent_merge, dim3((rows + 31) / 32), dim3(256), 0, s, cb, a, l.pl, l.part, p.part_rows, 2 * vt, l.part_h, sh.np, l.tl, p.r_lo, p.r_hi)) != cudaSuccess)
+      const int rows = p.r_hi - p.r_lo, vt = p.part0 / 2 + vocabulary_tiles(p.vn, sh.nv);
+      if ((e = launch_pdl(k_xent_merge, dim3((rows + 31) / 32), dim3(1024), 0, s, cb, a, l.pl, l.part, p.part_rows, 2 * vt, l.part_h, sh.np, l.tl, p.r_lo, p.r_hi)) != cudaSuccess)
         return e;
     }
   }
@@ -1155,13 +1223,16 @@ cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x,
 }  // namespace
 
 void xent_scratch_bytes(const z2z_config& c, int N, int grad_dtype, size_t* least, size_t* most) {
-  if (N <= 0) { *least = *most = 0; return; }
-  // (a step needs what either pass does)
-  const size_t l0 = bytes_with(c, N, -1, kLeastPiece), m0 = bytes_with(c, N, -1, wanted_piece(c, N, -1));
-  const size_t l1 = grad_dtype < 0 ? 0 : bytes_with(c, N, grad_dtype, kLeastPiece);
-  const size_t m1 = grad_dtype < 0 ? 0 : bytes_with(c, N, grad_dtype, wanted_piece(c, N, grad_dtype));
-  *least = l0 > l1 ? l0 : l1;
-  *most = m0 > m1 ? m0 : m1;
+  *least = *most = 0;
+  if (N <= 0) return;
+  // A step needs what either pass does.  (Smaller pieces may need more room for the losses' partial sums.)
+  auto add = [&](int gd) {
+    const size_t m = bytes_with(c, N, gd, wanted_piece(c, N, gd)), l = bytes_with(c, N, gd, kLeastPiece);
+    if (m > *most) *most = m;
+    if ((l < m ? l : m) > *least) *least = l < m ? l : m;
+  };
+  add(-1);
+  if (grad_dtype >= 0) add(grad_dtype);
 }
 
 cudaError_t run_xent(const CbView& cb, const z2z_config& cfg, const XentArgs& a, cudaStream_t s) {
