@@ -49,12 +49,13 @@ __device__ __forceinline__ int record_of(const Records& t, int chunk) {
   return lo;
 }
 
-// A chunk of a tensor: whole vectors [v0, v1) from the first 16-byte boundary on; the elements ahead of it go to the
+// A chunk of a tensor: whole vectors v0 .. v0 + count from the first 16-byte boundary on; the elements ahead of it go to the
 // first chunk and those behind the last vector to the last one.
 struct Span {
   int head;                                      // elements before the boundary
-  long long v0, v1;
-  long long tail0, tail1;                        // elements of the tail
+  long long v0;
+  int count;                                     // vectors
+  long long tail0;                               // first element of the tail, which ends with the tensor
 };
 __device__ __forceinline__ Span span_of(const Record& r, int chunk) {
   const int es = r.type & 1 ? 2 : 4, per = 16 / es;
@@ -64,10 +65,10 @@ __device__ __forceinline__ Span span_of(const Record& r, int chunk) {
   s.head = (int)(head < r.n ? head : r.n);
   const long long vecs = (r.n - s.head) / per;
   s.v0 = (long long)(chunk - r.first) * kChunkVecs;
-  s.v1 = s.v0 + kChunkVecs < vecs ? s.v0 + kChunkVecs : vecs;
-  const bool last = s.v0 + kChunkVecs >= vecs && (s.v0 < vecs || chunk == r.first);
+  const long long left = vecs - s.v0;
+  s.count = left <= 0 ? 0 : (left < kChunkVecs ? (int)left : kChunkVecs);
+  const bool last = left <= kChunkVecs && (left > 0 || chunk == r.first);
   s.tail0 = last ? s.head + vecs * per : r.n;
-  s.tail1 = r.n;
   if (chunk != r.first) s.head = -s.head;        // (not this chunk's)
   return s;
 }
@@ -110,12 +111,12 @@ __device__ __forceinline__ const uint4* body(const Record& r, int head) {
 }
 
 template <bool BF16>
-__device__ __forceinline__ double chunk_squares(const uint4* from, const Span& s) {
+__device__ __forceinline__ double chunk_squares(const uint4* from, int count) {
   uint4 v[kVecs];
 #pragma unroll
   for (int u = 0; u < kVecs; ++u) {
-    const long long i = s.v0 + u * kClipThreads + threadIdx.x;
-    v[u] = i < s.v1 ? from[i] : make_uint4(0u, 0u, 0u, 0u);
+    const int i = u * kClipThreads + threadIdx.x;
+    v[u] = i < count ? from[i] : make_uint4(0u, 0u, 0u, 0u);
   }
   double sum = 0.0;
 #pragma unroll
@@ -145,10 +146,10 @@ __global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_norm(const 
   for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
     const Record& r = t.r[record_of(t, c)];
     const Span s = span_of(r, c);
-    const uint4* from = body(r, abs(s.head));
-    sum += r.type & 1 ? chunk_squares<true>(from, s) : chunk_squares<false>(from, s);
+    const uint4* from = body(r, abs(s.head)) + s.v0;
+    sum += r.type & 1 ? chunk_squares<true>(from, s.count) : chunk_squares<false>(from, s.count);
     if (s.head > (int)threadIdx.x) { const double x = load_one(r, threadIdx.x); sum += x * x; }
-    if (s.tail0 + threadIdx.x < s.tail1) { const double x = load_one(r, s.tail0 + threadIdx.x); sum += x * x; }
+    if (s.tail0 + threadIdx.x < r.n) { const double x = load_one(r, s.tail0 + threadIdx.x); sum += x * x; }
   }
   sum = block_sum(sum);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -156,43 +157,48 @@ __global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_norm(const 
 
 template <bool FROM, bool TO>
 __device__ __forceinline__ void chunk_scale(const Record& r, const Span& s, float factor) {
-  constexpr int kPer = FROM ? 8 : 4, kOut = kPer * (TO ? 2 : 4);
+  constexpr int kPer = FROM ? 8 : 4, kOut = kPer * (TO ? 2 : 4), kAlign = kOut < 16 ? kOut : 16;
+  constexpr int kBatch = 4;                      // vectors loaded before any is used
   const int head = abs(s.head);
-  const uint4* from = body(r, head);
-  char* to = r.out + (size_t)head * (TO ? 2 : 4);
-  const bool whole = (reinterpret_cast<uintptr_t>(to) & (kOut < 16 ? kOut - 1 : 15)) == 0;
-  uint4 v[kVecs];
+  const uint4* from = body(r, head) + s.v0;
+  char* to = r.out + (size_t)head * (TO ? 2 : 4) + s.v0 * kOut;
+  const bool whole = (reinterpret_cast<uintptr_t>(to) & (kAlign - 1)) == 0;
+#pragma unroll 1
+  for (int i0 = threadIdx.x; i0 < s.count; i0 += kBatch * kClipThreads) {
+    uint4 v[kBatch];
 #pragma unroll
-  for (int u = 0; u < kVecs; ++u) {
-    const long long i = s.v0 + u * kClipThreads + threadIdx.x;
-    if (i < s.v1) v[u] = from[i];
-  }
+    for (int u = 0; u < kBatch; ++u)
+      if (i0 + u * kClipThreads < s.count) v[u] = from[i0 + u * kClipThreads];
 #pragma unroll
-  for (int u = 0; u < kVecs; ++u) {
-    const long long i = s.v0 + u * kClipThreads + threadIdx.x;
-    if (i >= s.v1) continue;
-    float x[kPer];
-    unpack<FROM>(v[u], x);
-    uint32_t o[kOut / 4];
+    for (int u = 0; u < kBatch; ++u) {
+      const int i = i0 + u * kClipThreads;
+      if (i >= s.count) break;
+      float x[kPer];
+      unpack<FROM>(v[u], x);
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) x[k] *= factor;
-    if (TO) {
+      for (int k = 0; k < kPer; ++k) x[k] *= factor;
+      char* at = to + (size_t)i * kOut;
+      if (!whole) {
 #pragma unroll
-      for (int k = 0; k < kPer / 2; ++k) { const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]); o[k] = *reinterpret_cast<const uint32_t*>(&p); }
-    } else {
+        for (int k = 0; k < kPer; ++k) {
+          if (TO) reinterpret_cast<__nv_bfloat16*>(at)[k] = __float2bfloat16_rn(x[k]);
+          else reinterpret_cast<float*>(at)[k] = x[k];
+        }
+        continue;
+      }
+      uint32_t o[kOut / 4];
+      if constexpr (TO) {
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) o[k] = __float_as_uint(x[k]);
-    }
-    char* at = to + i * kOut;
-    if (whole) {
+        for (int k = 0; k < kPer / 2; ++k) { const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]); o[k] = *reinterpret_cast<const uint32_t*>(&p); }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) o[k] = __float_as_uint(x[k]);
+      }
       if constexpr (kOut == 8) *reinterpret_cast<uint2*>(at) = make_uint2(o[0], o[1]);
       else {
 #pragma unroll
         for (int k = 0; k < kOut / 16; ++k) reinterpret_cast<uint4*>(at)[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
       }
-    } else {
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) store_one(r, head + i * kPer + k, x[k]);
     }
   }
 }
@@ -226,7 +232,7 @@ __global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_scale(const
       default: chunk_scale<true, true>(r, s, factor); break;
     }
     if (s.head > (int)threadIdx.x) store_one(r, threadIdx.x, load_one(r, threadIdx.x) * factor);
-    if (s.tail0 + threadIdx.x < s.tail1) store_one(r, s.tail0 + threadIdx.x, load_one(r, s.tail0 + threadIdx.x) * factor);
+    if (s.tail0 + threadIdx.x < r.n) store_one(r, s.tail0 + threadIdx.x, load_one(r, s.tail0 + threadIdx.x) * factor);
   }
 }
 
