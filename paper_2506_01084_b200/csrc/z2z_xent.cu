@@ -44,7 +44,7 @@ constexpr int kRegsFew = 56, kRegsEpi = 224;
 constexpr int kStages = 6;
 constexpr int kTile = 256;                       // vocabulary rows or columns of a tile (128 per CTA)
 constexpr int kStageBytes = 32768;               // 128 x 64 of either operand
-constexpr int kTurnBytes = 32 * 32 * 4;          // a warp's 32 x 32 values on their way from rows per thread to whole lines
+constexpr int kTurnBytes = 32 * 128;             // a warp's 32 rows of 128 bytes on their way from rows per thread to whole lines
 constexpr int kFrontBytes = 1024 + kEpiWarps * kTurnBytes;         // a multiple of 1024
 constexpr size_t kSmemBytes = 1024 + kFrontBytes + (size_t)kStages * kStageBytes;
 constexpr int kHyperPad = 32;                    // a sequence's rows start at a multiple of this beside its hypertokens
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_xent_plan(CbView cb, RowArgs a
       if (seq[u] >= 0 && seq[u] < cb.B && tgt[u] != Z2Z_CODE_NONE) {
         const int n = min(max(nv[u], 0), s_n[seq[u]]);
         if (tgt[u] < 0 || tgt[u] >= cb.V + n) atomicOr(&cb.status[seq[u]], Z2Z_ST_BAD_TOKEN);
-        else if (w[u] != 0.f) b = seq[u];
+        else if (w[u] != 0.f || a.loss_out) b = seq[u];
       }
       pl.inv[r] = b;                             // (read again below by the same thread)
       if (b >= 0) {
@@ -210,7 +210,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_xent_plan(CbView cb, RowArgs a
     if (q >= 0) {
       int nv = s_n[q];
       if (a.row_nvis) nv = min(max(a.row_nvis[r], 0), nv);
-      m = make_float4(a.lse ? a.lse[r] : 0.f, (a.weight ? a.weight[r] : 1.f) / wmax, __int_as_float(a.targets[r]), __int_as_float(nv));
+      const float x = a.weight ? a.weight[r] : 1.f;
+      m = make_float4(a.lse ? a.lse[r] : 0.f, x == 0.f ? 0.f : x / wmax, __int_as_float(a.targets[r]), __int_as_float(nv));
     }
     const unsigned same = __match_any_sync(0xffffffffu, q);
     const int rank = __popc(same & ((1u << lane) - 1u));
@@ -486,55 +487,96 @@ __device__ __forceinline__ void merge_ms(float& m, float& s, float om, float os)
   m = top;
 }
 
-enum Kind { kLoss, kGrad, kProducts };
+// kKeep: the losses' sums, and every logit in 16 bits as its distance from the largest of its row and half tile, in
+// steps of 2^-11 (half of one: p off by 2^-12, where g's rounding to bf16 is 2^-8); from 32 on, p < 1e-14, it is none.
+enum Kind { kLoss, kGrad, kProducts, kKeep };
+constexpr float kKeepSteps = 2048.f;
+constexpr uint32_t kKeepNone = 65535u;
 
-// A warp's block of 32 x 32 values, lane = row, to `rows` rows of memory `pitch` elements apart: turned in shared memory (16-byte
-// groups of a row exchanged with its row's low bits), so that a store writes whole sectors of a few rows.  (Stored from the
-// lanes' own rows, 32 lines per instruction, a tile of dW took 15000 clocks.)  cols: columns that exist, a multiple of 8.
-// ADD: to what is there, rounded once.
-template <typename T, bool ADD>
-__device__ __forceinline__ void store_block(float (&v)[32], float4* turn, T* out, long long pitch, int rows, int cols, int lane) {
-  constexpr int kPer = 16 / sizeof(T);           // elements per lane and store
-  constexpr int kLanes = 32 / kPer, kSteps = 32 / (32 / kLanes);       // lanes per row, stores
-  const int row0 = lane / kLanes, col = (lane % kLanes) * kPer;
-  uint4 old[kSteps];
-  if (ADD) {
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int r = row0 + i * (32 / kLanes);
-      old[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (r < rows && col < cols) old[i] = *reinterpret_cast<const uint4*>(out + r * pitch + col);
-    }
-  }
+// Rows of 128 bytes, one per lane, to `rows` rows of memory `pitch` bytes apart: turned in shared memory (16-byte groups of a
+// row exchanged by its row's low bits), so that a store writes whole lines of four rows.  (Stored from the lanes' own
+// rows, 32 lines per instruction, a tile of dW took 15000 clocks.)  bytes: of a row that exist, a multiple of 16.
+__device__ __forceinline__ void store_lines(const uint32_t (&w)[32], uint4* turn, char* out, long long pitch, int rows, int bytes, int lane) {
   __syncwarp();                                  // (the block before has been read)
 #pragma unroll
-  for (int g = 0; g < 8; ++g) turn[lane * 8 + (g ^ (lane & 7))] = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+  for (int g = 0; g < 8; ++g) turn[lane * 8 + (g ^ (lane & 7))] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
   __syncwarp();
+  const int r0 = lane >> 3, g = lane & 7;
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int r = row0 + i * (32 / kLanes);
-    uint4 o;
-    if constexpr (sizeof(T) == 4) {
-      float4 x = turn[r * 8 + ((col / 4) ^ (r & 7))];
-      if (ADD) {
-        x.x += __uint_as_float(old[i].x); x.y += __uint_as_float(old[i].y); x.z += __uint_as_float(old[i].z); x.w += __uint_as_float(old[i].w);
-      }
-      o = make_uint4(__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(x.z), __float_as_uint(x.w));
-    } else {
-      const float4 x = turn[r * 8 + ((col / 4) ^ (r & 7))], y = turn[r * 8 + ((col / 4 + 1) ^ (r & 7))];
-      const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-      const uint32_t w[4] = {old[i].x, old[i].y, old[i].z, old[i].w};
-      uint32_t t[4];
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + 4 * i;
+    const uint4 o = turn[r * 8 + (g ^ (r & 7))];
+    if (r < rows && 16 * g < bytes) *reinterpret_cast<uint4*>(out + r * pitch + 16 * g) = o;
+  }
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+// 64 columns of a table's gradient.  ADD: to what is there, rounded once; fp32 by reductions in L2 (every element has one
+// writer, so that their order does not matter), bf16 with a load ahead.
+template <typename T, bool ADD>
+__device__ __forceinline__ void store_columns(float (&v)[64], uint4* turn, T* out, long long pitch, int rows, int cols, int lane) {
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float lo = f[2 * k], hi = f[2 * k + 1];
-        if (ADD) { lo += __uint_as_float(w[k] << 16); hi += __uint_as_float(w[k] & 0xffff0000u); }
-        const __nv_bfloat162 pair = __floats2bfloat162_rn(lo, hi);
-        t[k] = *reinterpret_cast<const uint32_t*>(&pair);
+    for (int h = 0; h < 2; ++h) {
+      if (32 * h >= cols) break;
+      uint32_t w[32];
+#pragma unroll
+      for (int x = 0; x < 32; ++x) w[x] = __float_as_uint(v[32 * h + x]);
+      if (!ADD) {
+        store_lines(w, turn, reinterpret_cast<char*>(out + 32 * h), pitch * 4, rows, 4 * (cols - 32 * h), lane);
+      } else {
+        __syncwarp();
+#pragma unroll
+        for (int g = 0; g < 8; ++g) turn[lane * 8 + (g ^ (lane & 7))] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+        __syncwarp();
+        const int r0 = lane >> 3, g = lane & 7;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = r0 + 4 * i;
+          const uint4 o = turn[r * 8 + (g ^ (r & 7))];
+          if (r < rows && 4 * g < cols - 32 * h)
+            red_add_f32x4(out + r * pitch + 32 * h + 4 * g, __uint_as_float(o.x), __uint_as_float(o.y), __uint_as_float(o.z), __uint_as_float(o.w));
+        }
       }
-      o = make_uint4(t[0], t[1], t[2], t[3]);
     }
-    if (r < rows && col < cols) *reinterpret_cast<uint4*>(out + r * pitch + col) = o;
+  } else if constexpr (!ADD) {
+    uint32_t w[32];
+#pragma unroll
+    for (int x = 0; x < 32; ++x) w[x] = pack_bf16(v[2 * x], v[2 * x + 1]);
+    store_lines(w, turn, reinterpret_cast<char*>(out), pitch * 2, rows, 2 * cols, lane);
+  } else {
+    // four lanes per row and 32 columns; the old values are under way while the sums are turned
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (32 * h >= cols) break;
+      const int r0 = lane >> 2, col = 32 * h + (lane & 3) * 8;
+      uint4 old[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = r0 + 8 * i;
+        old[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows && col < cols) old[i] = *reinterpret_cast<const uint4*>(out + r * pitch + col);
+      }
+      __syncwarp();
+      float4* t4 = reinterpret_cast<float4*>(turn);
+#pragma unroll
+      for (int g = 0; g < 8; ++g)
+        t4[lane * 8 + (g ^ (lane & 7))] = make_float4(v[32 * h + 4 * g], v[32 * h + 4 * g + 1], v[32 * h + 4 * g + 2], v[32 * h + 4 * g + 3]);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = r0 + 8 * i, g = 2 * (lane & 3);
+        const float4 x = t4[r * 8 + (g ^ (r & 7))], y = t4[r * 8 + ((g + 1) ^ (r & 7))];
+        const uint32_t o[4] = {old[i].x, old[i].y, old[i].z, old[i].w};
+        const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        uint32_t t[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = pack_bf16(__uint_as_float(o[k] << 16) + f[2 * k], __uint_as_float(o[k] & 0xffff0000u) + f[2 * k + 1]);
+        if (r < rows && col < cols) *reinterpret_cast<uint4*>(out + r * pitch + col) = make_uint4(t[0], t[1], t[2], t[3]);
+      }
+    }
   }
 }
 
@@ -666,10 +708,10 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));
-    // ---------------- epilogue (both CTAs): thread = row of the result (x every other 32 columns) -----------
+    // ---------------- epilogue (both CTAs): thread = row of the result and 128 of its columns ------------------
     const int q = warp & 3, half = (warp - 4) >> 2;
     const int in_cta = q * 32 + lane, in_tile = rank * 128 + in_cta;
-    float4* turn = reinterpret_cast<float4*>(sm + 1024 + (warp - 4) * kTurnBytes);
+    uint4* turn = reinterpret_cast<uint4*>(sm + 1024 + (warp - 4) * kTurnBytes);
     uint32_t acc_empty_leader[2];
     acc_empty_leader[0] = map_to_cta(smem_u32(&ctrl->acc_empty[0]), 0);
     acc_empty_leader[1] = map_to_cta(smem_u32(&ctrl->acc_empty[1]), 0);
@@ -678,63 +720,50 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
     Job j;
     uint32_t job_i = 0;
     bool ok = true;
-    while (ok && w.next(j)) {
+    while (w.next(j)) {
       const int blocks = job_blocks(j) * job_products(p, j.type), chain = CHAINED ? job_chain(p, j) : 1 << 30;
       const bool some = blocks > 0;
-      auto wait_full = [&]() {
-        const bool good = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctrl->acc_full[job_i & 1u]), (job_i >> 1) & 1u, &ctrl->abort));
+      // the tile's sums, after which its accumulators are free
+      float acc[2][64];                          // columns 128 half + 64 u + x
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int x = 0; x < 64; ++x) acc[u][x] = 0.f;
+      for (int at = 0; at < blocks; at += min(chain, blocks)) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctrl->acc_full[job_i & 1u]), (job_i >> 1) & 1u, &ctrl->abort));
+        if (!ok) break;
         tc_fence_after();
-        return good;
-      };
-      auto release = [&]() {
+        const uint32_t from = tmem_base + ((uint32_t)(q * 32) << 16) + (job_i & 1u) * kTile + 128 * half;
+        if (CHAINED) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            if (128 * half + 32 * g < j.n) {
+              uint32_t v[32];
+              tmem_ld32(from + 32 * g, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int x = 0; x < 32; ++x) acc[g >> 1][32 * (g & 1) + x] += __uint_as_float(v[x]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            if (128 * half + 64 * u < j.n) {
+              uint32_t v[2][32];
+              tmem_ld32(from + 64 * u, v[0]);
+              if (128 * half + 64 * u + 32 < j.n) tmem_ld32(from + 64 * u + 32, v[1]);
+              tmem_ld_wait();
+#pragma unroll
+              for (int x = 0; x < 64; ++x) acc[u][x] = __uint_as_float(v[x >> 5][x & 31]);
+            }
+          }
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(acc_empty_leader[job_i & 1u]);
         ++job_i;
-      };
-      auto load = [&](int c0, float (&v)[32]) {
-        uint32_t x[32];
-        tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (job_i & 1u) * kTile + c0, x);
-        tmem_ld_wait();
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(x[i]);
-      };
-      float acc[CHAINED ? 4 : 1][32];            // columns 32 (half + 2 g) + x
-      if constexpr (CHAINED) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-#pragma unroll
-          for (int x = 0; x < 32; ++x) acc[g][x] = 0.f;
-        for (int at = 0; at < blocks; at += min(chain, blocks)) {
-          if (!wait_full()) { ok = false; break; }
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int c0 = 32 * half + 64 * g;
-            if (c0 < j.n) {
-              float v[32];
-              load(c0, v);
-#pragma unroll
-              for (int x = 0; x < 32; ++x) acc[g][x] += v[x];
-            }
-          }
-          release();
-        }
-        if (!ok) break;
-      } else if (some && !wait_full()) { ok = false; break; }
-      // `use` gets the sums of every group of 32 columns of this warp
-      auto groups = [&](auto&& use) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int c0 = 32 * half + 64 * g;
-          if (c0 >= j.n) continue;
-          if constexpr (CHAINED) use(c0, acc[g]);
-          else {
-            if (some) load(c0, acc[0]);
-            use(c0, acc[0]);
-          }
-        }
-        if constexpr (!CHAINED) { if (some) release(); }
-      };
+      }
+      if (!ok) break;
       if constexpr (KIND != kProducts) {
         const bool hy = j.b >= 0;
         const int cta_rows = hy ? p.th >> 1 : p.cta_rows, row = rank * cta_rows + in_cta;       // of the tile
@@ -742,108 +771,118 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         const int pos = (hy ? p.pl.s0[j.b] : 0) + j.m0 + row;
         float4 r = make_float4(0.f, 0.f, __int_as_float(-1), __int_as_float(0));
         if (there) r = p.pl.meta[pos];
-        const int target = __float_as_int(r.z) - (hy ? p.cb.V : p.v0) - j.r0;                   // its column of the tile, if it has it
-        const int limit = !there ? 0 : (hy ? min(__float_as_int(r.w), p.cb.n[j.b]) : p.vn) - j.r0;       // columns that the row sees
+        const int at = __float_as_int(r.z) - (hy ? p.cb.V : p.v0) - j.r0 - 128 * half;          // the target's column here, if it has it
+        const int see = !there ? 0 : min((hy ? min(__float_as_int(r.w), p.cb.n[j.b]) : p.vn) - j.r0, j.n) - 128 * half;     // columns that the row sees
+        // rows up to the next multiple of 32 get zeros (or none): they are contracted in steps of 16
+        const int first = rank * cta_rows + q * 32;
+        const int rows = min(min(32, cta_rows - q * 32), pad32(j.limit) - first);
+        __nv_bfloat16* out = (hy ? p.gh + (size_t)(p.pl.h0[j.b] + j.m0 + first) * p.gh_pitch : p.g + (size_t)(j.m0 + first) * p.g_pitch) + j.r0 + 128 * half;
+        const long long pitch = 2ll * (hy ? p.gh_pitch : p.g_pitch);
         if constexpr (KIND == kGrad) {
-          // rows up to the next multiple of 32 get zeros: they are contracted in steps of 16
-          const int first = rank * cta_rows + q * 32;
-          const int rows = min(min(32, cta_rows - q * 32), pad32(j.limit) - first);
-          __nv_bfloat16* out = hy ? p.gh + (size_t)(p.pl.h0[j.b] + j.m0 + first) * p.gh_pitch + j.r0 : p.g + (size_t)(j.m0 + first) * p.g_pitch + j.r0;
-          const long long plane = hy ? p.gh_plane : p.g_plane, pitch = hy ? p.gh_pitch : p.g_pitch;
+          const long long plane = hy ? p.gh_plane : p.g_plane;
           const float lse = r.x, weight = r.y;
-          groups([&](int c0, float (&v)[32]) {
-            const int see = weight != 0.f ? limit - c0 : 0;
+          const int show = weight != 0.f ? see : 0;
+          const bool all = __all_sync(0xffffffffu, show >= 128);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int cols = min(64, j.n - 128 * half - 64 * u);
+            if (cols <= 0 || rows <= 0) continue;
+            float (&v)[64] = acc[u];
             if (p.exact_exp) {
 #pragma unroll
-              for (int x = 0; x < 32; ++x) v[x] = weight * (expf(v[x] - lse) - (x == target - c0 ? 1.f : 0.f));
+              for (int x = 0; x < 64; ++x) v[x] = weight * (expf(v[x] - lse) - (x == at - 64 * u ? 1.f : 0.f));
             } else {
 #pragma unroll
-              for (int x = 0; x < 32; ++x) v[x] = weight * (ex2((v[x] - lse) * kLog2e) - (x == target - c0 ? 1.f : 0.f));
+              for (int x = 0; x < 64; ++x) v[x] = weight * (ex2((v[x] - lse) * kLog2e) - (x == at - 64 * u ? 1.f : 0.f));
             }
-            if (__any_sync(0xffffffffu, see < 32)) {
+            if (!all) {
 #pragma unroll
-              for (int x = 0; x < 32; ++x) v[x] = x < see ? v[x] : 0.f;
+              for (int x = 0; x < 64; ++x) v[x] = x < show - 64 * u ? v[x] : 0.f;
             }
-            if (rows <= 0) return;
             for (int part = 0; part < p.g_parts; ++part) {
-              store_block<__nv_bfloat16, false>(v, turn, out + (size_t)part * plane + c0, pitch, rows, 32, lane);
-              if (part + 1 < p.g_parts) {
+              uint32_t o[32];
 #pragma unroll
-                for (int x = 0; x < 32; ++x) v[x] -= __bfloat162float(__float2bfloat16_rn(v[x]));
+              for (int x = 0; x < 32; ++x) {
+                o[x] = pack_bf16(v[2 * x], v[2 * x + 1]);
+                v[2 * x] -= __uint_as_float(o[x] << 16);
+                v[2 * x + 1] -= __uint_as_float(o[x] & 0xffff0000u);
               }
+              store_lines(o, turn, reinterpret_cast<char*>(out + (size_t)part * plane + 64 * u), pitch, rows, 2 * cols, lane);
             }
-          });
+          }
         } else {
-          float m = -INFINITY, s = 0.f;
-          groups([&](int c0, float (&v)[32]) {
-            const int see = limit - c0;
-            if (!__any_sync(0xffffffffu, see > 0)) return;
-            if (__any_sync(0xffffffffu, see < 32)) {
+          if (!__all_sync(0xffffffffu, see >= 128)) {
 #pragma unroll
-              for (int x = 0; x < 32; ++x) v[x] = x < see ? v[x] : -INFINITY;
-            }
-            const int at = target - c0;
-            if (at >= 0 && at < 32 && at < see) {
-              float l = v[0];
+            for (int x = 0; x < 128; ++x) acc[x >> 6][x & 63] = x < see ? acc[x >> 6][x & 63] : -INFINITY;
+          }
+          if (__any_sync(0xffffffffu, at >= 0 && at < 128)) {
+            float l = acc[0][0];
 #pragma unroll
-              for (int x = 1; x < 32; ++x) l = x == at ? v[x] : l;
-              p.tl[pos] = l;
-            }
-            float top = v[0];
+            for (int x = 1; x < 128; ++x) l = x == at ? acc[x >> 6][x & 63] : l;
+            if (at >= 0 && at < 128 && at < see) p.tl[pos] = l;
+          }
+          float m = acc[0][0], s = 0.f;
 #pragma unroll
-            for (int x = 1; x < 32; ++x) top = fmaxf(top, v[x]);
-            bool nan = false;
-            if (top == -INFINITY) {              // nothing here, or NaN
+          for (int x = 1; x < 128; ++x) m = fmaxf(m, acc[x >> 6][x & 63]);
+          bool nan = false;
+          if (m == -INFINITY) {                  // nothing here, or NaN
 #pragma unroll
-              for (int x = 0; x < 32; ++x) nan |= v[x] != v[x];
-            } else {
-              top = fmaxf(top, m);
-              s *= m == top ? 1.f : ex2((m - top) * kLog2e);
-              m = top;
-              float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
+            for (int x = 0; x < 128; ++x) nan |= acc[x >> 6][x & 63] != acc[x >> 6][x & 63];
+          } else {
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int x = 0; x < 32; x += 4) {
-                a0 += ex2((v[x] - m) * kLog2e); a1 += ex2((v[x + 1] - m) * kLog2e);
-                a2 += ex2((v[x + 2] - m) * kLog2e); a3 += ex2((v[x + 3] - m) * kLog2e);
-              }
-              s += (a0 + a1) + (a2 + a3);
-              nan = s != s;                      // (+inf: inf - inf)
-            }
-            if (nan) { m = INFINITY; s = __int_as_float(0x7fc00000); }
-          });
+            for (int x = 0; x < 128; ++x) part[x & 3] += ex2((acc[x >> 6][x & 63] - m) * kLog2e);
+            s = (part[0] + part[1]) + (part[2] + part[3]);
+            nan = s != s;                        // (+inf: inf - inf)
+          }
           if (there) {
-            float2* out = hy ? p.part_h + (size_t)(j.part + half) * p.part_rows_h + pos : p.part + (size_t)(j.part + half) * p.part_rows + pos - p.r_lo;
-            *out = make_float2(m, s);
+            float2* ms = hy ? p.part_h + (size_t)(j.part + half) * p.part_rows_h + pos : p.part + (size_t)(j.part + half) * p.part_rows + pos - p.r_lo;
+            *ms = nan ? make_float2(INFINITY, __int_as_float(0x7fc00000)) : make_float2(m, s);
+          }
+          if constexpr (KIND == kKeep) {
+            // (a row of NaN has a NaN lse, whatever is kept of it)
+            auto steps = [&](float l) { return m == -INFINITY ? kKeepNone : min(__float2uint_rn((m - l) * kKeepSteps), kKeepNone); };
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int cols = min(64, j.n - 128 * half - 64 * u);
+              if (cols <= 0 || rows <= 0) continue;
+              uint32_t o[32];
+#pragma unroll
+              for (int x = 0; x < 32; ++x) o[x] = steps(acc[u][2 * x]) | steps(acc[u][2 * x + 1]) << 16;
+              store_lines(o, turn, reinterpret_cast<char*>(out + 64 * u), pitch, rows, 2 * cols, lane);
+            }
           }
         }
       } else if (j.type == kHidden || j.type == kHiddenHyper) {
         const int m = j.m0 + in_tile, pos0 = (j.b >= 0 ? p.pl.s0[j.b] : 0) + j.r0;
         const bool set = p.first || j.type == kHiddenHyper;
-        float* out = p.dh + (size_t)j.part * p.dh_slot + (size_t)pos0 * p.d + m;
-        groups([&](int c0, float (&v)[32]) {
-          if (m >= p.d || !(some || set)) return;
+        float* out = p.dh + (size_t)j.part * p.dh_slot + (size_t)(pos0 + 128 * half) * p.d + m;
+        const int limit = j.limit - 128 * half;
+        if (m < p.d && (some || set)) {
 #pragma unroll
-          for (int x0 = 0; x0 < 32; x0 += 8) {
+          for (int x0 = 0; x0 < 128; x0 += 8) {
+            if (x0 >= limit) break;
             float old[8];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) old[x] = !set && c0 + x0 + x < j.limit ? out[(size_t)(c0 + x0 + x) * p.d] : 0.f;
+            for (int x = 0; x < 8; ++x) old[x] = !set && x0 + x < limit ? out[(size_t)(x0 + x) * p.d] : 0.f;
 #pragma unroll
             for (int x = 0; x < 8; ++x)
-              if (c0 + x0 + x < j.limit) out[(size_t)(c0 + x0 + x) * p.d] = some ? old[x] + v[x0 + x] : old[x];
+              if (x0 + x < limit) out[(size_t)(x0 + x) * p.d] = old[x] + acc[(x0 + x) >> 6][(x0 + x) & 63];
           }
-        });
-      } else {
+        }
+      } else if (some || !p.acc) {
         const int first = j.m0 + rank * 128 + q * 32, rows = (j.b >= 0 ? p.cb.n[j.b] : p.vn) - first;
-        const int cols = min(j.n, p.d - j.r0);
         TO* out = (j.b >= 0 ? reinterpret_cast<TO*>(p.gUh) + ((size_t)j.b * p.cb.cap + first) * p.d
-                            : reinterpret_cast<TO*>(p.gWU) + (size_t)(p.v0 + first) * p.d) + j.r0;
-        groups([&](int c0, float (&v)[32]) {
-          if (rows <= 0 || c0 >= cols || !(some || !p.acc)) return;
+                            : reinterpret_cast<TO*>(p.gWU) + (size_t)(p.v0 + first) * p.d) + j.r0 + 128 * half;
 #pragma unroll
-          for (int x = 0; x < 32; ++x) v[x] = some ? scale * v[x] : 0.f;
-          if (p.acc) store_block<TO, true>(v, turn, out + c0, p.d, rows, cols - c0, lane);
-          else store_block<TO, false>(v, turn, out + c0, p.d, rows, cols - c0, lane);
-        });
+        for (int u = 0; u < 2; ++u) {
+          const int cols = min(min(j.n, p.d - j.r0) - 128 * half - 64 * u, 64);
+          if (rows <= 0 || cols <= 0) continue;
+#pragma unroll
+          for (int x = 0; x < 64; ++x) acc[u][x] = some ? scale * acc[u][x] : 0.f;
+          if (p.acc) store_columns<TO, true>(acc[u], turn, out + 64 * u, p.d, rows, cols, lane);
+          else store_columns<TO, false>(acc[u], turn, out + 64 * u, p.d, rows, cols, lane);
+        }
       }
     }
   }
@@ -855,8 +894,11 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
 }
 
 // 32 threads per row, a warp for 32 rows each: the partial sums of its vocabulary and hypertoken tiles, its loss and lse.
+// With gradients to follow (parts_of_rows > 0) lse also goes to the plan, and the copies of a hidden row without weight are
+// zeroed: they are contracted with g = 0, whatever they hold.
 __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan pl, const float2* part, int part_rows, int parts,
-                                                     const float2* part_h, int part_rows_h, const float* tl, int r_lo, int r_hi) {
+                                                     const float2* part_h, int part_rows_h, const float* tl, int r_lo, int r_hi,
+                                                     GatherArgs g, int parts_of_rows) {
   pdl_wait();
   pdl_trigger();
   __shared__ float2 s_ms[32][33];
@@ -893,11 +935,72 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
     if (x & o) { float lm = om, ls = os; merge_ms(lm, ls, m, s); m = lm; s = ls; }
     else merge_ms(m, s, om, os);
   }
-  if (x != 0 || p2 >= min(pl.head[0], r_hi)) return;
+  if (p2 >= min(pl.head[0], r_hi)) return;
   const int row = pl.perm[p2];
-  const float ls = logf(s);
-  a.lse_out[row] = m + ls;
-  a.loss_out[row] = ls + (m - tl[p2]);
+  if (x == 0) {
+    const float ls = logf(s);
+    a.lse_out[row] = m + ls;
+    a.loss_out[row] = ls + (m - tl[p2]);
+    if (parts_of_rows) pl.meta[p2].x = m + ls;
+  }
+  if (parts_of_rows && pl.meta[p2].y == 0.f) {
+    const int b = a.row_seq ? a.row_seq[row] : row, h = pl.h0[b] + p2 - pl.s0[b];
+    for (int i = 0; i < parts_of_rows; ++i) {
+      put_row<__nv_bfloat16>(nullptr, g.hs + (size_t)i * g.hs_plane + (size_t)p2 * g.d, 0, g.d, x, 32);
+      if (g.hh) put_row<__nv_bfloat16>(nullptr, g.hh + (size_t)i * g.hh_plane + (size_t)h * g.d, 0, g.d, x, 32);
+    }
+  }
+}
+
+// g from what kKeep has left, in its place: p = exp(m - steps / 2048 - lse), the target's from its own logit.  A block takes 2048
+// columns of a row; rows up to the next multiple of 32 are zeros.  `base`: the target code of the first column.
+struct KeptArgs { __nv_bfloat16* g; int pitch; const float2* part; int part_rows, nv; };
+__device__ __forceinline__ void kept_columns(uint16_t* g, int cols, int lo, const float2* part, int part_rows, int nv, const float4& r, int target, float tl) {
+  const float lse = r.x, weight = r.y;
+  for (int v = lo + threadIdx.x * 8; v < min(cols, lo + 2048); v += blockDim.x * 8) {
+    const uint4 w = *reinterpret_cast<const uint4*>(g + v);
+    const int vt = v / nv, half = (v - vt * nv) >> 7;
+    const float from = part[(size_t)(2 * vt + half) * part_rows].x - lse;
+    const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+    uint32_t o[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float x[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t q = i ? in[k] >> 16 : in[k] & 0xffffu;
+        float e = ex2(fmaf((float)q, -kLog2e / kKeepSteps, from * kLog2e));
+        if (q == kKeepNone) e = 0.f;
+        if (v + 2 * k + i == target) e = expf(tl - lse) - 1.f;
+        x[i] = weight == 0.f ? 0.f : (lse != lse ? lse : weight * e);
+      }
+      o[k] = pack_bf16(x[0], x[1]);
+    }
+    *reinterpret_cast<uint4*>(g + v) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
+__global__ void __launch_bounds__(256) k_xent_kept(CbView cb, RowArgs a, Plan pl, KeptArgs w, KeptArgs u, const float* tl, int chunks) {
+  pdl_wait();
+  pdl_trigger();
+  const int pos = blockIdx.x, live = pl.head[0];
+  if (pos >= pad32(live)) return;
+  const float4 r = pos < live ? pl.meta[pos] : make_float4(0.f, 0.f, __int_as_float(-1), 0.f);
+  const float t = pos < live ? tl[pos] : 0.f;
+  const int chunk = blockIdx.y, target = __float_as_int(r.z);
+  if (chunk < chunks) {
+    kept_columns(reinterpret_cast<uint16_t*>(w.g) + (size_t)pos * w.pitch, pad64(cb.V), chunk * 2048, w.part + pos, w.part_rows, w.nv, r,
+                 target < cb.V ? target : -1, t);
+    return;
+  }
+  if (pos >= live) return;
+  // hypertokens, and the zeros up to the sequence's next multiple of 32
+  const int row = pl.perm[pos], b = a.row_seq ? a.row_seq[row] : row, n = pad32(cb.n[b]), lo = (chunk - chunks) * 2048;
+  if (lo >= n) return;
+  const int h = pl.h0[b] + pos - pl.s0[b];
+  kept_columns(reinterpret_cast<uint16_t*>(u.g) + (size_t)h * u.pitch, n, lo, u.part + pos, u.part_rows, u.nv, r, target - cb.V, t);
+  if (pos + 1 == pl.s0[b + 1])
+    for (int i = h + 1; i < pl.h0[b + 1]; ++i)
+      for (int v = lo + threadIdx.x * 8; v < min(n, lo + 2048); v += blockDim.x * 8) *reinterpret_cast<uint4*>(u.g + (size_t)i * u.pitch + v) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // dh of a row: its partial sums, those of the vocabulary's parts first, times the largest weight.
@@ -968,15 +1071,16 @@ constexpr int kClusters = 74;                    // B200's pairs of SMs; what si
 struct Shape {
   int N, d, V, B, cap, dtype, parts;             // parts: bf16 parts of an operand
   int grad_dtype, g_parts;                       // < 0: losses alone
+  bool keep;                                     // a step whose logits are kept from the losses to the gradients
   int np, nh;                                    // rows of the sorted copy, and beside hypertokens
   int cta_rows, nv;
   int tr, th, dt, split;
   int pieces, vc;                                // vocabulary rows per piece, a multiple of 256
 };
 
-Shape shape_of(const z2z_config& c, int N, int grad_dtype, long long vc) {
+Shape shape_of(const z2z_config& c, int N, int grad_dtype, long long vc, bool keep) {
   Shape s{};
-  s.N = N; s.d = c.d; s.V = c.V; s.B = c.B; s.cap = c.cap; s.dtype = c.dtype; s.grad_dtype = grad_dtype;
+  s.N = N; s.d = c.d; s.V = c.V; s.B = c.B; s.cap = c.cap; s.dtype = c.dtype; s.grad_dtype = grad_dtype; s.keep = keep;
   s.parts = c.dtype == Z2Z_DTYPE_FP32 ? kMaxParts : 1;
   s.g_parts = grad_dtype < 0 ? 0 : (s.parts > 1 || grad_dtype == Z2Z_DTYPE_FP32 ? kMaxParts : 1);
   s.np = (int)up_to(N, kTile);
@@ -993,7 +1097,7 @@ Shape shape_of(const z2z_config& c, int N, int grad_dtype, long long vc) {
   s.split = tiles >= kClusters ? 1 : kClusters / tiles;
   if (s.split > kMaxSplit) s.split = kMaxSplit;
   const long long whole = up_to(c.V, kTile);
-  if (vc > whole) vc = whole;
+  if (vc > whole || keep) vc = whole;
   s.pieces = (int)((c.V + vc - 1) / vc);
   s.vc = (int)up_to((c.V + s.pieces - 1) / s.pieces, kTile);
   s.pieces = (c.V + s.vc - 1) / s.vc;
@@ -1015,7 +1119,10 @@ struct Layout {
 };
 
 int hyper_rows(const Shape& s) { return (int)up_to(s.cap, kTile); }
+// Rows whose partial sums are held at a time.
+int loss_rows(const Shape& s) { return s.keep || s.np < kLossRows ? s.np : kLossRows; }
 
+// (A step's; what the gradients alone do not use is small beside the rest.)
 Layout layout_of(const Shape& s, char* base) {
   Layout l{};
   size_t o = 0;
@@ -1033,12 +1140,10 @@ Layout layout_of(const Shape& s, char* base) {
     if (s.parts > 1) l.up = (__nv_bfloat16*)take(row * s.B * s.cap);
   }
   if (s.parts > 1) l.wp = (__nv_bfloat16*)take(row * s.vc);
-  if (s.grad_dtype < 0) {
-    const int vt = s.pieces * vocabulary_tiles(s.vc, s.nv), rows = s.np < kLossRows ? s.np : kLossRows;
-    l.part = (float2*)take((size_t)2 * vt * rows * 8);
-    if (s.cap > 0) l.part_h = (float2*)take((size_t)2 * (hyper_rows(s) / kTile) * s.np * 8);
-    l.tl = (float*)take((size_t)s.np * 4);
-  } else {
+  l.part = (float2*)take((size_t)2 * s.pieces * vocabulary_tiles(s.vc, s.nv) * loss_rows(s) * 8);
+  if (s.cap > 0) l.part_h = (float2*)take((size_t)2 * (hyper_rows(s) / kTile) * s.np * 8);
+  l.tl = (float*)take((size_t)s.np * 4);
+  if (s.grad_dtype >= 0) {
     if (s.cap > 0) {
       l.ut = (__nv_bfloat16*)take(row * s.B * 16);
       l.gh = (__nv_bfloat16*)take((size_t)s.g_parts * hyper_rows(s) * s.nh * 2);
@@ -1050,7 +1155,7 @@ Layout layout_of(const Shape& s, char* base) {
   return l;
 }
 
-// Vocabulary rows of a piece: G^T of 256 MB (8192 rows at least).  fp32 tables are also held in parts.
+// Vocabulary rows of a piece: G of 256 MB (8192 rows at least).  fp32 tables are also held in parts.
 long long wanted_piece(const z2z_config& c, int N, int grad_dtype) {
   const bool f32 = c.dtype == Z2Z_DTYPE_FP32;
   if (grad_dtype < 0) return f32 ? 16384 : up_to(c.V, kTile);
@@ -1062,13 +1167,21 @@ long long wanted_piece(const z2z_config& c, int N, int grad_dtype) {
 }
 constexpr long long kLeastPiece = 2048;
 
-size_t bytes_with(const z2z_config& c, int N, int grad_dtype, long long vc) { return layout_of(shape_of(c, N, grad_dtype, vc), nullptr).bytes; }
+// A step may keep its logits (16 bits each) instead of computing them again for the gradients, which are a quarter of its
+// products: where g is a single part and the scratch has room, of which at most 4 GB are asked for.
+bool may_keep(const z2z_config& c, int N, int grad_dtype) {
+  return grad_dtype == Z2Z_DTYPE_BF16 && c.dtype == Z2Z_DTYPE_BF16 && up_to(N, kTile) * up_to(c.V, kTile) * 2 <= 4ll << 30;
+}
+
+size_t bytes_with(const z2z_config& c, int N, int grad_dtype, long long vc, bool keep) {
+  return layout_of(shape_of(c, N, grad_dtype, vc, keep), nullptr).bytes;
+}
 
 // The largest pieces up to the wanted ones for which the scratch suffices; 0 if none.
 long long piece_for(const z2z_config& c, int N, int grad_dtype, size_t bytes) {
   long long vc = wanted_piece(c, N, grad_dtype);
   for (;;) {
-    if (bytes_with(c, N, grad_dtype, vc) <= bytes) return vc;
+    if (bytes_with(c, N, grad_dtype, vc, false) <= bytes) return vc;
     if (vc <= kLeastPiece) return 0;
     vc = vc / 2 < kLeastPiece ? kLeastPiece : vc / 2;
   }
@@ -1115,19 +1228,27 @@ cudaError_t launch_main(const Params& p, const Maps& tm, int clusters, cudaStrea
   return launch_pdl(kern, dim3(2 * clusters), dim3(kThreads), kSmemBytes, s, p, tm);
 }
 
-// One of the two passes: losses, or gradients from lse.
-cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x, bool grad, cudaStream_t s) {
+template <int KIND, typename TO>
+cudaError_t launch_main(const Params& p, const Maps& tm, int clusters, bool chained, cudaStream_t s) {
+  return chained ? launch_main<KIND, true, TO>(p, tm, clusters, s) : launch_main<KIND, false, TO>(p, tm, clusters, s);
+}
+
+// Losses, gradients from lse, or both.
+cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& x, cudaStream_t s) {
+  const bool loss = x.want_loss, grad = x.want_grad;
   const int gd = grad ? x.grad_dtype : -1;
-  const long long vc = piece_for(cfg, x.N, gd, x.scratch_bytes);
+  const bool keep = loss && grad && may_keep(cfg, x.N, gd) && bytes_with(cfg, x.N, gd, 0, true) <= x.scratch_bytes;
+  const long long vc = keep ? cfg.V : piece_for(cfg, x.N, gd, x.scratch_bytes);
   if (vc == 0) return cudaErrorMemoryAllocation;
-  const Shape sh = shape_of(cfg, x.N, gd, vc);
+  const Shape sh = shape_of(cfg, x.N, gd, vc, keep);
   const Layout l = layout_of(sh, x.scratch);
   const int d = sh.d, clusters = sm_count_xent() / 2;
   RowArgs a{};
   a.N = x.N; a.row_seq = x.row_seq; a.row_nvis = x.row_nvis; a.targets = x.targets;
   a.th = sh.th; a.dt = sh.dt;
-  if (grad) { a.weight = x.weight; a.lse = x.lse; a.hidden = x.g_hidden != nullptr; a.tables = x.g_Uh != nullptr; }
-  else { a.loss_out = x.loss; a.lse_out = x.lse; }
+  if (grad) { a.weight = x.weight; a.hidden = x.g_hidden != nullptr; a.tables = x.g_Uh != nullptr; }
+  if (loss) { a.loss_out = x.loss; a.lse_out = x.lse; }
+  else a.lse = x.lse;
   cudaError_t e = cudaFuncSetAttribute(k_xent_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan_shared_bytes(1024));
   if (e != cudaSuccess) return e;
   if ((e = launch_pdl(k_xent_plan, dim3(1), dim3(kPlanThreads), plan_shared_bytes(sh.B), s, cb, a, l.pl)) != cudaSuccess) return e;
@@ -1145,8 +1266,8 @@ cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x,
   Params p{};
   p.cb = cb; p.pl = l.pl; p.d = d; p.dt = sh.dt; p.cta_rows = sh.cta_rows; p.nv = sh.nv; p.tr = sh.tr; p.th = sh.th;
   products(sh.parts, sh.parts, &p.np1, p.a1, p.b1);
-  // dh has the session's type: of three parts of g for fp32 tables' gradients it takes the first
   if (grad) {
+    // (dh of a bf16 session takes the first of g's parts: it is stored in bf16)
     products(sh.parts, sh.parts, &p.np2, p.a2, p.b2);
     products(sh.g_parts, sh.parts, &p.np3, p.a3, p.b3);
   }
@@ -1154,7 +1275,7 @@ cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x,
   p.exact_sums = (sh.parts > 1 ? 1 : 0) | (sh.g_parts > 1 ? 2 : 0);
   p.g = l.g; p.g_pitch = sh.vc; p.g_plane = (long long)sh.vc * sh.np;
   p.gh = l.gh; p.gh_pitch = hyper_rows(sh); p.gh_plane = (long long)hyper_rows(sh) * sh.nh;
-  p.part = l.part; p.part_h = l.part_h; p.part_rows_h = sh.np; p.tl = l.tl;
+  p.part = l.part; p.part_h = l.part_h; p.part_rows = loss_rows(sh); p.part_rows_h = sh.np; p.tl = l.tl;
   p.split = sh.split; p.dh = grad && x.g_hidden ? l.dh : nullptr; p.dh_slot = (long long)sh.np * d;
   p.gWU = x.g_WU; p.gUh = sh.cap > 0 ? x.g_Uh : nullptr; p.acc = x.accumulate ? 1 : 0;
   p.mem_cycles = kTile * kTile * (x.grad_dtype == Z2Z_DTYPE_FP32 ? 4 : 2) * (x.accumulate ? 2 : 1) / 46;
@@ -1183,41 +1304,52 @@ cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x,
   ok = ok && make_map(&tm.w_k, W, w_rows, d, d, sh.parts, w_plane, 128) && make_map(&tm.w_m, W, w_rows, d, d, sh.parts, w_plane, 64);
   if (!ok) return cudaErrorInvalidValue;
 
-  const int share = grad ? x.N : (x.N < kLossRows ? x.N : kLossRows);
-  for (int r0 = 0; r0 < x.N; r0 += share) {
-    p.r_lo = r0; p.r_hi = r0 + share < x.N ? r0 + share : x.N;
-    p.part_rows = (int)(sh.np < kLossRows ? sh.np : kLossRows);
-    for (int i = 0; i < sh.pieces; ++i) {
-      p.v0 = i * sh.vc; p.vn = sh.V - p.v0 < sh.vc ? sh.V - p.v0 : sh.vc;
-      p.w_row0 = sh.parts > 1 ? 0 : p.v0;
-      p.part0 = 2 * i * vocabulary_tiles(sh.vc, sh.nv);
-      p.first = i == 0;
-      p.hyper = i == 0 && r0 == 0 && sh.cap > 0;
-      p.hyper_hidden = p.hyper && p.dh;
-      if (sh.parts > 1)
-        if ((e = launch_pdl(k_xent_split, dim3(p.vn < 4096 ? p.vn : 4096), dim3(128), 0, s, reinterpret_cast<const float*>(x.WU) + (size_t)p.v0 * d, l.wp, w_plane, p.vn, d)) != cudaSuccess) return e;
-      const bool chained = p.np1 * ((d + 63) / 64) > kChain;                // (logits)
-      if (!grad) e = chained ? launch_main<kLoss, true, float>(p, tm, clusters, s) : launch_main<kLoss, false, float>(p, tm, clusters, s);
-      else e = chained ? launch_main<kGrad, true, float>(p, tm, clusters, s) : launch_main<kGrad, false, float>(p, tm, clusters, s);
-      if (e == cudaSuccess && grad)
-        e = x.grad_dtype == Z2Z_DTYPE_FP32 ? launch_main<kProducts, true, float>(p, tm, clusters, s)
-            : p.exact_sums                 ? launch_main<kProducts, true, __nv_bfloat16>(p, tm, clusters, s)
-                                           : launch_main<kProducts, false, __nv_bfloat16>(p, tm, clusters, s);
+  const int tiles = vocabulary_tiles(sh.vc, sh.nv);
+  auto piece = [&](int i, bool again) {
+    p.v0 = i * sh.vc; p.vn = sh.V - p.v0 < sh.vc ? sh.V - p.v0 : sh.vc;
+    p.w_row0 = sh.parts > 1 ? 0 : p.v0;
+    p.part0 = 2 * i * tiles;
+    p.first = i == 0;
+    if (sh.parts == 1 || (again && sh.pieces == 1)) return cudaSuccess;
+    return launch_pdl(k_xent_split, dim3(p.vn < 4096 ? p.vn : 4096), dim3(128), 0, s, reinterpret_cast<const float*>(x.WU) + (size_t)p.v0 * d, l.wp, w_plane, p.vn, d);
+  };
+  const bool chained = p.np1 * ((d + 63) / 64) > kChain;                     // (logits)
+  if (loss) {
+    const int share = loss_rows(sh) < x.N ? loss_rows(sh) : x.N;
+    for (int r0 = 0; r0 < x.N; r0 += share) {
+      p.r_lo = r0; p.r_hi = r0 + share < x.N ? r0 + share : x.N;
+      for (int i = 0; i < sh.pieces; ++i) {
+        p.hyper = i == 0 && r0 == 0 && sh.cap > 0;
+        if ((e = piece(i, r0 > 0)) != cudaSuccess) return e;
+        e = keep ? launch_main<kKeep, float>(p, tm, clusters, chained, s) : launch_main<kLoss, float>(p, tm, clusters, chained, s);
+        if (e != cudaSuccess) return e;
+      }
+      const int parts = p.part0 + 2 * vocabulary_tiles(p.vn, sh.nv);
+      e = launch_pdl(k_xent_merge, dim3((p.r_hi - p.r_lo + 31) / 32), dim3(1024), 0, s, cb, a, l.pl, l.part, p.part_rows, parts, l.part_h, sh.np, l.tl,
+                     p.r_lo, p.r_hi, g, grad ? sh.parts : 0);
       if (e != cudaSuccess) return e;
     }
-    if (!grad) {
-      const int rows = p.r_hi - p.r_lo, vt = p.part0 / 2 + vocabulary_tiles(p.vn, sh.nv);
-      if ((e = launch_pdl(k_xent_merge, dim3((rows + 31) / 32), dim3(1024), 0, s, cb, a, l.pl, l.part, p.part_rows, 2 * vt, l.part_h, sh.np, l.tl, p.r_lo, p.r_hi)) != cudaSuccess)
-        return e;
-    }
   }
-  if (grad && x.g_hidden) {
-    e = sh.dtype == Z2Z_DTYPE_FP32
-            ? launch_pdl(k_xent_hidden<float>, dim3(x.N), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<float*>(x.g_hidden), d)
-            : launch_pdl(k_xent_hidden<__nv_bfloat16>, dim3(x.N), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<__nv_bfloat16*>(x.g_hidden), d);
+  if (!grad) return cudaSuccess;
+  if (keep) {
+    const KeptArgs w{l.g, p.g_pitch, l.part, p.part_rows, sh.nv}, u{l.gh, p.gh_pitch, l.part_h, p.part_rows_h, kTile};
+    const int chunks = (pad64(sh.V) + 2047) / 2048, hyper = (sh.cap + 2047) / 2048;
+    if ((e = launch_pdl(k_xent_kept, dim3(sh.np, chunks + hyper), dim3(256), 0, s, cb, a, l.pl, w, u, l.tl, chunks)) != cudaSuccess) return e;
+  }
+  p.r_lo = 0; p.r_hi = x.N;
+  for (int i = 0; i < sh.pieces; ++i) {
+    p.hyper = i == 0 && sh.cap > 0;
+    p.hyper_hidden = p.hyper && p.dh;
+    if ((e = piece(i, loss)) != cudaSuccess) return e;
+    if (!keep && (e = launch_main<kGrad, float>(p, tm, clusters, chained, s)) != cudaSuccess) return e;
+    e = x.grad_dtype == Z2Z_DTYPE_FP32 ? launch_main<kProducts, true, float>(p, tm, clusters, s)
+                                       : launch_main<kProducts, __nv_bfloat16>(p, tm, clusters, p.exact_sums != 0, s);
     if (e != cudaSuccess) return e;
   }
-  return cudaSuccess;
+  if (!x.g_hidden) return cudaSuccess;
+  return sh.dtype == Z2Z_DTYPE_FP32
+             ? launch_pdl(k_xent_hidden<float>, dim3(x.N), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<float*>(x.g_hidden), d)
+             : launch_pdl(k_xent_hidden<__nv_bfloat16>, dim3(x.N), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<__nv_bfloat16*>(x.g_hidden), d);
 }
 
 }  // namespace
@@ -1225,14 +1357,14 @@ cudaError_t run_pass(const CbView& cb, const z2z_config& cfg, const XentArgs& x,
 void xent_scratch_bytes(const z2z_config& c, int N, int grad_dtype, size_t* least, size_t* most) {
   *least = *most = 0;
   if (N <= 0) return;
-  // A step needs what either pass does.  (Smaller pieces may need more room for the losses' partial sums.)
-  auto add = [&](int gd) {
-    const size_t m = bytes_with(c, N, gd, wanted_piece(c, N, gd)), l = bytes_with(c, N, gd, kLeastPiece);
-    if (m > *most) *most = m;
-    if ((l < m ? l : m) > *least) *least = l < m ? l : m;
-  };
-  add(-1);
-  if (grad_dtype >= 0) add(grad_dtype);
+  *most = bytes_with(c, N, grad_dtype, wanted_piece(c, N, grad_dtype), false);
+  // (smaller pieces may need more room for the losses' partial sums)
+  *least = bytes_with(c, N, grad_dtype, kLeastPiece, false);
+  if (*least > *most) *least = *most;
+  if (may_keep(c, N, grad_dtype)) {
+    const size_t kept = bytes_with(c, N, grad_dtype, 0, true);
+    if (kept > *most) *most = kept;
+  }
 }
 
 cudaError_t run_xent(const CbView& cb, const z2z_config& cfg, const XentArgs& a, cudaStream_t s) {
@@ -1241,11 +1373,7 @@ cudaError_t run_xent(const CbView& cb, const z2z_config& cfg, const XentArgs& a,
     return launch_pdl(k_xent_zero, dim3(148 * 8), dim3(128), 0, s, cb, reinterpret_cast<char*>(a.g_WU), reinterpret_cast<char*>(a.g_Uh),
                       a.d * (a.grad_dtype == Z2Z_DTYPE_FP32 ? 4 : 2));
   }
-  if (a.want_loss) {
-    const cudaError_t e = run_pass(cb, cfg, a, false, s);
-    if (e != cudaSuccess) return e;
-  }
-  return a.want_grad ? run_pass(cb, cfg, a, true, s) : cudaSuccess;
+  return run_passes(cb, cfg, a, s);
 }
 
 }  // namespace z2z
