@@ -41,11 +41,11 @@ constexpr int kThreads = 128 + 32 * kEpiWarps;   // a warpgroup of producer, iss
 // Registers: 384 threads are launched with 168 each; the epilogue, which holds a tile's sums, takes what the others leave
 // (128 x 56 + 256 x 224 = 384 x 168).
 constexpr int kRegsFew = 56, kRegsEpi = 224;
-constexpr int kStages = 6;
+constexpr int kStages = 5;
 constexpr int kTile = 256;                       // vocabulary rows or columns of a tile (128 per CTA)
 constexpr int kStageBytes = 32768;               // 128 x 64 of either operand
-constexpr int kTurnBytes = 32 * 128;             // a warp's 32 rows of 128 bytes on their way from rows per thread to whole lines
-constexpr int kFrontBytes = 1024 + kEpiWarps * kTurnBytes;         // a multiple of 1024
+constexpr int kTurnBytes = 32 * 128;             // a warp's 32 rows of 128 bytes on their way to memory; two of them
+constexpr int kFrontBytes = 1024 + kEpiWarps * 2 * kTurnBytes;     // a multiple of 1024
 constexpr size_t kSmemBytes = 1024 + kFrontBytes + (size_t)kStages * kStageBytes;
 constexpr int kHyperPad = 32;                    // a sequence's rows start at a multiple of this beside its hypertokens
 constexpr int kLossRows = 8192;                  // rows whose partial sums are held at a time
@@ -111,6 +111,8 @@ struct Maps {
   CUtensorMap w_k, u_k, hs_k, hh_k, g_k, gh_k;
   // MN-major: 64 columns x 64 rows (ut: 16)
   CUtensorMap w_m, u_m, ut_m, hs_m, hh_m, g_m, gh_m;
+  // stores: 32 rows x 128 bytes of G and of W_U's gradient
+  CUtensorMap g_s, gh_s, o_w;
 };
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -473,6 +475,12 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
   return d;
 }
 
+// Arrival at a barrier of this cluster that orders nothing: the accumulator has been read into registers when it is made
+// (tcgen05.wait::ld), and a release would wait for the stores of the tile before (a tile of dW 6900 -> 4100 clocks).
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -493,30 +501,74 @@ enum Kind { kLoss, kGrad, kProducts, kKeep };
 constexpr float kKeepSteps = 2048.f;
 constexpr uint32_t kKeepNone = 65535u;
 
-// Rows of 128 bytes, one per lane, to `rows` rows of memory `pitch` bytes apart: turned in shared memory (16-byte groups of a
-// row exchanged by its row's low bits), so that a store writes whole lines of four rows.  (Stored from the lanes' own
-// rows, 32 lines per instruction, a tile of dW took 15000 clocks.)  bytes: of a row that exist, a multiple of 16.
-__device__ __forceinline__ void store_lines(const uint32_t (&w)[32], uint4* turn, char* out, long long pitch, int rows, int bytes, int lane) {
-  __syncwarp();                                  // (the block before has been read)
-#pragma unroll
-  for (int g = 0; g < 8; ++g) turn[lane * 8 + (g ^ (lane & 7))] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
-  __syncwarp();
-  const int r0 = lane >> 3, g = lane & 7;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + 4 * i;
-    const uint4 o = turn[r * 8 + (g ^ (r & 7))];
-    if (r < rows && 16 * g < bytes) *reinterpret_cast<uint4*>(out + r * pitch + 16 * g) = o;
-  }
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* m, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(m), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
 }
+__device__ __forceinline__ void tma_add_3d(const CUtensorMap* m, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(m), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// A warp's way to memory for blocks of 32 rows (one per lane) of 128 bytes: two buffers in shared memory, in which 16-byte
+// groups of a row are exchanged by its row's low bits (the 128-byte swizzle), and then either one TMA store of the
+// block or stores of whole lines of four rows.  (Stored from the lanes' own rows, 32 lines per instruction, a tile of dW
+// took 15000 clocks.)
+struct Turn {
+  uint4* buf;                                    // [2][32 * 8]
+  int at, lane;
+  __device__ __forceinline__ uint4* put(const uint32_t (&w)[32]) {
+    uint4* to = buf + at * 256;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) to[lane * 8 + (g ^ (lane & 7))] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+    return to;
+  }
+  // Whole blocks; what lies outside the map is left out.
+  template <bool ADD>
+  __device__ __forceinline__ void tma(const uint32_t (&w)[32], const CUtensorMap* m, int x, int y, int z) {
+    if (lane == 0) bulk_wait_read<1>();          // the buffer's block before has left
+    __syncwarp();
+    uint4* from = put(w);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+      if (ADD) tma_add_3d(m, smem_u32(from), x, y, z);
+      else tma_store_3d(m, smem_u32(from), x, y, z);
+      bulk_commit();
+    }
+    at ^= 1;
+  }
+  // `rows` rows of `bytes` bytes (a multiple of 16), `pitch` bytes apart.
+  template <bool ADD>
+  __device__ __forceinline__ void lines(const uint32_t (&w)[32], char* out, long long pitch, int rows, int bytes) {
+    if (lane == 0) bulk_wait_read<0>();
+    __syncwarp();
+    const uint4* from = put(w);
+    __syncwarp();
+    const int r0 = lane >> 3, g = lane & 7;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + 4 * i;
+      const uint4 o = from[r * 8 + (g ^ (r & 7))];
+      if (r < rows && 16 * g < bytes) {
+        char* to = out + r * pitch + 16 * g;
+        if (ADD) red_add_f32x4(reinterpret_cast<float*>(to), __uint_as_float(o.x), __uint_as_float(o.y), __uint_as_float(o.z), __uint_as_float(o.w));
+        else *reinterpret_cast<uint4*>(to) = o;
+      }
+    }
+    __syncwarp();
+  }
+};
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&t);
 }
-// 64 columns of a table's gradient.  ADD: to what is there, rounded once; fp32 by reductions in L2 (every element has one
-// writer, so that their order does not matter), bf16 with a load ahead.
+// 64 columns of a table's gradient; m: its map, for blocks that end with it or not at all, or NULL.  ADD: to what is there,
+// rounded once; fp32 by reductions in L2 (every element has one writer, so that their order does not matter), bf16
+// with a load ahead.
 template <typename T, bool ADD>
-__device__ __forceinline__ void store_columns(float (&v)[64], uint4* turn, T* out, long long pitch, int rows, int cols, int lane) {
+__device__ __forceinline__ void store_columns(float (&v)[64], Turn& turn, const CUtensorMap* m, int x0, int y0, T* out, long long pitch, int rows, int cols) {
   if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -524,30 +576,18 @@ __device__ __forceinline__ void store_columns(float (&v)[64], uint4* turn, T* ou
       uint32_t w[32];
 #pragma unroll
       for (int x = 0; x < 32; ++x) w[x] = __float_as_uint(v[32 * h + x]);
-      if (!ADD) {
-        store_lines(w, turn, reinterpret_cast<char*>(out + 32 * h), pitch * 4, rows, 4 * (cols - 32 * h), lane);
-      } else {
-        __syncwarp();
-#pragma unroll
-        for (int g = 0; g < 8; ++g) turn[lane * 8 + (g ^ (lane & 7))] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
-        __syncwarp();
-        const int r0 = lane >> 3, g = lane & 7;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = r0 + 4 * i;
-          const uint4 o = turn[r * 8 + (g ^ (r & 7))];
-          if (r < rows && 4 * g < cols - 32 * h)
-            red_add_f32x4(out + r * pitch + 32 * h + 4 * g, __uint_as_float(o.x), __uint_as_float(o.y), __uint_as_float(o.z), __uint_as_float(o.w));
-        }
-      }
+      if (m) turn.tma<ADD>(w, m, x0 + 32 * h, y0, 0);
+      else turn.lines<ADD>(w, reinterpret_cast<char*>(out + 32 * h), pitch * 4, rows, 4 * (cols - 32 * h));
     }
   } else if constexpr (!ADD) {
     uint32_t w[32];
 #pragma unroll
     for (int x = 0; x < 32; ++x) w[x] = pack_bf16(v[2 * x], v[2 * x + 1]);
-    store_lines(w, turn, reinterpret_cast<char*>(out), pitch * 2, rows, 2 * cols, lane);
+    if (m) turn.tma<false>(w, m, x0, y0, 0);
+    else turn.lines<false>(w, reinterpret_cast<char*>(out), pitch * 2, rows, 2 * cols);
   } else {
     // four lanes per row and 32 columns; the old values are under way while the sums are turned
+    const int lane = turn.lane;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if (32 * h >= cols) break;
@@ -559,11 +599,11 @@ __device__ __forceinline__ void store_columns(float (&v)[64], uint4* turn, T* ou
         old[i] = make_uint4(0u, 0u, 0u, 0u);
         if (r < rows && col < cols) old[i] = *reinterpret_cast<const uint4*>(out + r * pitch + col);
       }
-      __syncwarp();
-      float4* t4 = reinterpret_cast<float4*>(turn);
+      uint32_t w[32];
 #pragma unroll
-      for (int g = 0; g < 8; ++g)
-        t4[lane * 8 + (g ^ (lane & 7))] = make_float4(v[32 * h + 4 * g], v[32 * h + 4 * g + 1], v[32 * h + 4 * g + 2], v[32 * h + 4 * g + 3]);
+      for (int x = 0; x < 32; ++x) w[x] = __float_as_uint(v[32 * h + x]);
+      __syncwarp();
+      const float4* t4 = reinterpret_cast<const float4*>(turn.put(w));
       __syncwarp();
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -711,7 +751,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
     // ---------------- epilogue (both CTAs): thread = row of the result and 128 of its columns ------------------
     const int q = warp & 3, half = (warp - 4) >> 2;
     const int in_cta = q * 32 + lane, in_tile = rank * 128 + in_cta;
-    uint4* turn = reinterpret_cast<uint4*>(sm + 1024 + (warp - 4) * kTurnBytes);
+    Turn turn{reinterpret_cast<uint4*>(sm + 1024 + (warp - 4) * 2 * kTurnBytes), 0, lane};
     uint32_t acc_empty_leader[2];
     acc_empty_leader[0] = map_to_cta(smem_u32(&ctrl->acc_empty[0]), 0);
     acc_empty_leader[1] = map_to_cta(smem_u32(&ctrl->acc_empty[1]), 0);
@@ -725,10 +765,12 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
       const bool some = blocks > 0;
       // the tile's sums, after which its accumulators are free
       float acc[2][64];                          // columns 128 half + 64 u + x
+      if (CHAINED || !some) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int x = 0; x < 64; ++x) acc[u][x] = 0.f;
+          for (int x = 0; x < 64; ++x) acc[u][x] = 0.f;
+      }
       for (int at = 0; at < blocks; at += min(chain, blocks)) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctrl->acc_full[job_i & 1u]), (job_i >> 1) & 1u, &ctrl->abort));
         if (!ok) break;
@@ -760,7 +802,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(acc_empty_leader[job_i & 1u]);
+        if (lane == 0) mbar_arrive_relaxed(acc_empty_leader[job_i & 1u]);
         ++job_i;
       }
       if (!ok) break;
@@ -776,7 +818,8 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         // rows up to the next multiple of 32 get zeros (or none): they are contracted in steps of 16
         const int first = rank * cta_rows + q * 32;
         const int rows = min(min(32, cta_rows - q * 32), pad32(j.limit) - first);
-        __nv_bfloat16* out = (hy ? p.gh + (size_t)(p.pl.h0[j.b] + j.m0 + first) * p.gh_pitch : p.g + (size_t)(j.m0 + first) * p.g_pitch) + j.r0 + 128 * half;
+        const int row0 = (hy ? p.pl.h0[j.b] : 0) + j.m0 + first;
+        __nv_bfloat16* out = (hy ? p.gh + (size_t)row0 * p.gh_pitch : p.g + (size_t)row0 * p.g_pitch) + j.r0 + 128 * half;
         const long long pitch = 2ll * (hy ? p.gh_pitch : p.g_pitch);
         if constexpr (KIND == kGrad) {
           const long long plane = hy ? p.gh_plane : p.g_plane;
@@ -807,7 +850,8 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
                 v[2 * x] -= __uint_as_float(o[x] << 16);
                 v[2 * x + 1] -= __uint_as_float(o[x] & 0xffff0000u);
               }
-              store_lines(o, turn, reinterpret_cast<char*>(out + (size_t)part * plane + 64 * u), pitch, rows, 2 * cols, lane);
+              if (rows == 32) turn.tma<false>(o, hy ? &tm.gh_s : &tm.g_s, j.r0 + 128 * half + 64 * u, row0, part);
+              else turn.lines<false>(o, reinterpret_cast<char*>(out + (size_t)part * plane + 64 * u), pitch, rows, 2 * cols);
             }
           }
         } else {
@@ -849,7 +893,8 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
               uint32_t o[32];
 #pragma unroll
               for (int x = 0; x < 32; ++x) o[x] = steps(acc[u][2 * x]) | steps(acc[u][2 * x + 1]) << 16;
-              store_lines(o, turn, reinterpret_cast<char*>(out + 64 * u), pitch, rows, 2 * cols, lane);
+              if (rows == 32) turn.tma<false>(o, hy ? &tm.gh_s : &tm.g_s, j.r0 + 128 * half + 64 * u, row0, 0);
+              else turn.lines<false>(o, reinterpret_cast<char*>(out + 64 * u), pitch, rows, 2 * cols);
             }
           }
         }
@@ -872,6 +917,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         }
       } else if (some || !p.acc) {
         const int first = j.m0 + rank * 128 + q * 32, rows = (j.b >= 0 ? p.cb.n[j.b] : p.vn) - first;
+        const float mul = some ? scale : 0.f;
         TO* out = (j.b >= 0 ? reinterpret_cast<TO*>(p.gUh) + ((size_t)j.b * p.cb.cap + first) * p.d
                             : reinterpret_cast<TO*>(p.gWU) + (size_t)(p.v0 + first) * p.d) + j.r0 + 128 * half;
 #pragma unroll
@@ -879,12 +925,14 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
           const int cols = min(min(j.n, p.d - j.r0) - 128 * half - 64 * u, 64);
           if (rows <= 0 || cols <= 0) continue;
 #pragma unroll
-          for (int x = 0; x < 64; ++x) acc[u][x] = some ? scale * acc[u][x] : 0.f;
-          if (p.acc) store_columns<TO, true>(acc[u], turn, out + 64 * u, p.d, rows, cols, lane);
-          else store_columns<TO, false>(acc[u], turn, out + 64 * u, p.d, rows, cols, lane);
+          for (int x = 0; x < 64; ++x) acc[u][x] *= mul;
+          const CUtensorMap* m = j.b < 0 ? &tm.o_w : nullptr;
+          if (p.acc) store_columns<TO, true>(acc[u], turn, m, j.r0 + 128 * half + 64 * u, p.v0 + first, out + 64 * u, p.d, rows, cols);
+          else store_columns<TO, false>(acc[u], turn, m, j.r0 + 128 * half + 64 * u, p.v0 + first, out + 64 * u, p.d, rows, cols);
         }
       }
     }
+    if (lane == 0) bulk_wait_all();
   }
   tc_fence_before();
   __syncthreads();
@@ -952,55 +1000,74 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
   }
 }
 
-// g from what kKeep has left, in its place: p = exp(m - steps / 2048 - lse), the target's from its own logit.  A block takes 2048
-// columns of a row; rows up to the next multiple of 32 are zeros.  `base`: the target code of the first column.
+// g from what kKeep has left, in its place: p = exp(m - steps / 2048 - lse), the target's from its own logit.  Blocks take
+// 8192 columns of a row at a time; rows up to the next multiple of 32 become zeros.
 struct KeptArgs { __nv_bfloat16* g; int pitch; const float2* part; int part_rows, nv; };
-__device__ __forceinline__ void kept_columns(uint16_t* g, int cols, int lo, const float2* part, int part_rows, int nv, const float4& r, int target, float tl) {
-  const float lse = r.x, weight = r.y;
-  for (int v = lo + threadIdx.x * 8; v < min(cols, lo + 2048); v += blockDim.x * 8) {
-    const uint4 w = *reinterpret_cast<const uint4*>(g + v);
+constexpr int kKeptThreads = 256, kKeptVecs = 4, kKeptColumns = 8 * kKeptThreads * kKeptVecs;
+// see: columns that the row sees; those behind them up to `cols` become zeros.
+__device__ __forceinline__ void kept_columns(uint16_t* g, int lo, int cols, int see, const float2* part, int part_rows, int nv, const float4& r, int target, float tl) {
+  const float lse = r.x, weight = r.y, none = lse - lse;                     // (0, or NaN for a row of NaN)
+  uint4 w[kKeptVecs];
+  float from[kKeptVecs];
+#pragma unroll
+  for (int u = 0; u < kKeptVecs; ++u) {
+    const int v = lo + 8 * (u * kKeptThreads + (int)threadIdx.x);
+    if (v >= cols) break;
+    w[u] = *reinterpret_cast<const uint4*>(g + v);
     const int vt = v / nv, half = (v - vt * nv) >> 7;
-    const float from = part[(size_t)(2 * vt + half) * part_rows].x - lse;
-    const uint32_t in[4] = {w.x, w.y, w.z, w.w};
-    uint32_t o[4];
+    from[u] = (part[(size_t)(2 * vt + half) * part_rows].x - lse) * kLog2e;
+  }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float x[2];
+  for (int u = 0; u < kKeptVecs; ++u) {
+    const int v = lo + 8 * (u * kKeptThreads + (int)threadIdx.x);
+    if (v >= cols) break;
+    const uint32_t in[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+    float x[8];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t q = i ? in[k] >> 16 : in[k] & 0xffffu;
-        float e = ex2(fmaf((float)q, -kLog2e / kKeepSteps, from * kLog2e));
-        if (q == kKeepNone) e = 0.f;
-        if (v + 2 * k + i == target) e = expf(tl - lse) - 1.f;
-        x[i] = weight == 0.f ? 0.f : (lse != lse ? lse : weight * e);
-      }
-      o[k] = pack_bf16(x[0], x[1]);
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t q = k & 1 ? in[k >> 1] >> 16 : in[k >> 1] & 0xffffu;
+      // (a whole number below 2^16 as a float: in the low bits of 2^23, less that)
+      const float steps = __uint_as_float(0x4b000000u | q) - 8388608.f;
+      x[k] = weight * (q == kKeepNone ? none : ex2(fmaf(steps, -kLog2e / kKeepSteps, from[u])));
     }
-    *reinterpret_cast<uint4*>(g + v) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (weight == 0.f || v + 8 > see) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) if (weight == 0.f || v + k >= see) x[k] = 0.f;
+    }
+    if (target >= v && target < v + 8 && weight != 0.f) {
+      const float e = weight * (expf(tl - lse) - 1.f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = v + k == target ? e : x[k];
+    }
+    *reinterpret_cast<uint4*>(g + v) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
   }
 }
-__global__ void __launch_bounds__(256) k_xent_kept(CbView cb, RowArgs a, Plan pl, KeptArgs w, KeptArgs u, const float* tl, int chunks) {
+__global__ void __launch_bounds__(kKeptThreads) k_xent_kept(CbView cb, RowArgs a, Plan pl, KeptArgs w, KeptArgs u, const float* tl, int chunks, int hyper) {
   pdl_wait();
   pdl_trigger();
-  const int pos = blockIdx.x, live = pl.head[0];
-  if (pos >= pad32(live)) return;
-  const float4 r = pos < live ? pl.meta[pos] : make_float4(0.f, 0.f, __int_as_float(-1), 0.f);
-  const float t = pos < live ? tl[pos] : 0.f;
-  const int chunk = blockIdx.y, target = __float_as_int(r.z);
-  if (chunk < chunks) {
-    kept_columns(reinterpret_cast<uint16_t*>(w.g) + (size_t)pos * w.pitch, pad64(cb.V), chunk * 2048, w.part + pos, w.part_rows, w.nv, r,
-                 target < cb.V ? target : -1, t);
-    return;
+  const int live = pl.head[0];
+  const long long units = (long long)pad32(live) * (chunks + hyper);
+  for (long long i = blockIdx.x; i < units; i += gridDim.x) {
+    const int pos = (int)(i / (chunks + hyper)), chunk = (int)(i - (long long)pos * (chunks + hyper));
+    const float4 r = pos < live ? pl.meta[pos] : make_float4(0.f, 0.f, __int_as_float(-1), 0.f);
+    const float t = pos < live ? tl[pos] : 0.f;
+    const int target = __float_as_int(r.z);
+    if (chunk < chunks) {
+      kept_columns(reinterpret_cast<uint16_t*>(w.g) + (size_t)pos * w.pitch, chunk * kKeptColumns, pad64(cb.V), cb.V, w.part + pos, w.part_rows, w.nv, r,
+                   target < cb.V ? target : -1, t);
+      continue;
+    }
+    if (pos >= live) continue;
+    // hypertokens, and the zeros up to the sequence's next multiple of 32
+    const int row = pl.perm[pos], b = a.row_seq ? a.row_seq[row] : row, n = pad32(cb.n[b]), lo = (chunk - chunks) * kKeptColumns;
+    if (lo >= n) continue;
+    const int h = pl.h0[b] + pos - pl.s0[b];
+    kept_columns(reinterpret_cast<uint16_t*>(u.g) + (size_t)h * u.pitch, lo, n, __float_as_int(r.w), u.part + pos, u.part_rows, u.nv, r, target - cb.V, t);
+    if (pos + 1 == pl.s0[b + 1])
+      for (int k = h + 1; k < pl.h0[b + 1]; ++k)
+        for (int v = lo + threadIdx.x * 8; v < min(n, lo + kKeptColumns); v += kKeptThreads * 8)
+          *reinterpret_cast<uint4*>(u.g + (size_t)k * u.pitch + v) = make_uint4(0u, 0u, 0u, 0u);
   }
-  if (pos >= live) return;
-  // hypertokens, and the zeros up to the sequence's next multiple of 32
-  const int row = pl.perm[pos], b = a.row_seq ? a.row_seq[row] : row, n = pad32(cb.n[b]), lo = (chunk - chunks) * 2048;
-  if (lo >= n) return;
-  const int h = pl.h0[b] + pos - pl.s0[b];
-  kept_columns(reinterpret_cast<uint16_t*>(u.g) + (size_t)h * u.pitch, n, lo, u.part + pos, u.part_rows, u.nv, r, target - cb.V, t);
-  if (pos + 1 == pl.s0[b + 1])
-    for (int i = h + 1; i < pl.h0[b + 1]; ++i)
-      for (int v = lo + threadIdx.x * 8; v < min(n, lo + 2048); v += blockDim.x * 8) *reinterpret_cast<uint4*>(u.g + (size_t)i * u.pitch + v) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // dh of a row: its partial sums, those of the vocabulary's parts first, times the largest weight.
@@ -1101,11 +1168,14 @@ Shape shape_of(const z2z_config& c, int N, int grad_dtype, long long vc, bool ke
   s.pieces = (int)((c.V + vc - 1) / vc);
   s.vc = (int)up_to((c.V + s.pieces - 1) / s.pieces, kTile);
   s.pieces = (c.V + s.vc - 1) / s.vc;
-  // One row tile: as many vocabulary rows per tile as make its rounds of all clusters even.
+  // Vocabulary rows per tile: the number of rounds of all clusters times the rows that a CTA loads for a tile (and something).
+  // Multiples of 64, since G's tiles are stored in blocks of 64 columns.
   s.nv = kTile;
-  if (rt == 1) {
-    const int rounds = (s.vc + kClusters * kTile - 1) / (kClusters * kTile), each = (s.vc + rounds * kClusters - 1) / (rounds * kClusters);
-    s.nv = (int)up_to(each, 32);
+  const int row_tiles = (N + 2 * s.cta_rows - 1) / (2 * s.cta_rows);
+  long long best = -1;
+  for (int nv = kTile; nv >= 128; nv -= 64) {
+    const long long rounds = ((long long)row_tiles * ((s.vc + nv - 1) / nv) + kClusters - 1) / kClusters, cost = rounds * (s.cta_rows + nv / 2 + 16);
+    if (best < 0 || cost < best) { best = cost; s.nv = nv; }
   }
   return s;
 }
@@ -1199,14 +1269,16 @@ EncodeFn encode_fn() {
   return fn;
 }
 
-// Map over `planes` bf16 matrices [rows, cols], rows `pitch` elements apart; box = 64 columns x box_rows rows of one.
-bool make_map(CUtensorMap* m, const void* base, long long rows, long long cols, long long pitch, int planes, long long plane, int box_rows) {
+// Map over `planes` matrices [rows, cols] of bf16 (or fp32), rows `pitch` elements apart; box = 128 bytes x box_rows rows of one.
+bool make_map(CUtensorMap* m, const void* base, long long rows, long long cols, long long pitch, int planes, long long plane, int box_rows,
+              bool f32 = false) {
   const EncodeFn fn = encode_fn();
   if (!fn || rows < 1 || cols < 1) return false;
+  const int es_ = f32 ? 4 : 2;
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
-  const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)(planes > 1 ? plane : rows * pitch) * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, es[3] = {1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint64_t strides[2] = {(cuuint64_t)pitch * es_, (cuuint64_t)(planes > 1 ? plane : rows * pitch) * es_};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / es_), (cuuint32_t)box_rows, 1}, es[3] = {1, 1, 1};
+  return fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -1294,11 +1366,14 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
       ok = ok && make_map(&tm.u_m, U, ur, d, d, sh.parts, g.up_plane, 64) && make_map(&tm.ut_m, l.ut, sh.B * 16, d, d, sh.parts, g.ut_plane, 16) &&
            make_map(&tm.hh_m, l.hh, sh.nh, d, d, sh.parts, g.hh_plane, 64) &&
            make_map(&tm.gh_k, l.gh, sh.nh, hyper_rows(sh), hyper_rows(sh), sh.g_parts, p.gh_plane, sh.th / 2) &&
-           make_map(&tm.gh_m, l.gh, sh.nh, hyper_rows(sh), hyper_rows(sh), sh.g_parts, p.gh_plane, 64);
+           make_map(&tm.gh_m, l.gh, sh.nh, hyper_rows(sh), hyper_rows(sh), sh.g_parts, p.gh_plane, 64) &&
+           make_map(&tm.gh_s, l.gh, sh.nh, hyper_rows(sh), hyper_rows(sh), sh.g_parts, p.gh_plane, 32);
   }
   if (grad)
     ok = ok && make_map(&tm.hs_m, l.hs, sh.np, d, d, sh.parts, g.hs_plane, 64) &&
-         make_map(&tm.g_k, l.g, sh.np, sh.vc, sh.vc, sh.g_parts, p.g_plane, sh.tr / 2) && make_map(&tm.g_m, l.g, sh.np, sh.vc, sh.vc, sh.g_parts, p.g_plane, 64);
+         make_map(&tm.g_k, l.g, sh.np, sh.vc, sh.vc, sh.g_parts, p.g_plane, sh.tr / 2) && make_map(&tm.g_m, l.g, sh.np, sh.vc, sh.vc, sh.g_parts, p.g_plane, 64) &&
+         make_map(&tm.g_s, l.g, sh.np, sh.vc, sh.vc, sh.g_parts, p.g_plane, 32) &&
+         (!x.g_WU || make_map(&tm.o_w, x.g_WU, sh.V, d, d, 1, 0, 32, x.grad_dtype == Z2Z_DTYPE_FP32));
   const void* W = sh.parts > 1 ? l.wp : x.WU;
   const long long w_rows = sh.parts > 1 ? sh.vc : sh.V, w_plane = (long long)sh.vc * d;
   ok = ok && make_map(&tm.w_k, W, w_rows, d, d, sh.parts, w_plane, 128) && make_map(&tm.w_m, W, w_rows, d, d, sh.parts, w_plane, 64);
@@ -1333,8 +1408,8 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   if (!grad) return cudaSuccess;
   if (keep) {
     const KeptArgs w{l.g, p.g_pitch, l.part, p.part_rows, sh.nv}, u{l.gh, p.gh_pitch, l.part_h, p.part_rows_h, kTile};
-    const int chunks = (pad64(sh.V) + 2047) / 2048, hyper = (sh.cap + 2047) / 2048;
-    if ((e = launch_pdl(k_xent_kept, dim3(sh.np, chunks + hyper), dim3(256), 0, s, cb, a, l.pl, w, u, l.tl, chunks)) != cudaSuccess) return e;
+    const int chunks = (pad64(sh.V) + kKeptColumns - 1) / kKeptColumns, hyper = (sh.cap + kKeptColumns - 1) / kKeptColumns;
+    if ((e = launch_pdl(k_xent_kept, dim3(148 * 6), dim3(kKeptThreads), 0, s, cb, a, l.pl, w, u, l.tl, chunks, hyper)) != cudaSuccess) return e;
   }
   p.r_lo = 0; p.r_hi = x.N;
   for (int i = 0; i < sh.pieces; ++i) {
