@@ -25,7 +25,7 @@ constexpr int kClipThreads = 256;
 constexpr int kVecs = 8;                         // 16-byte vectors per thread and chunk, loaded before any is used
 constexpr int kChunkVecs = kClipThreads * kVecs;
 constexpr int kBlocksPerSm = 4;
-constexpr int kRecords = 512;                    // tensors per launch (kernel parameters)
+constexpr int kRecords = 512, kFewRecords = 64;  // tensors per launch: they are kernel parameters, which cost time to hand over
 
 struct Record {
   const char* g;
@@ -34,13 +34,15 @@ struct Record {
   int first;                                     // its first chunk
   int type;                                      // bit 0: gradient is bf16, bit 1: output is
 };
+template <int MAX>
 struct Records {
   int count, chunks;
-  Record r[kRecords];
+  Record r[MAX];
 };
 
 // The tensor that holds a chunk.
-__device__ __forceinline__ int record_of(const Records& t, int chunk) {
+template <int MAX>
+__device__ __forceinline__ int record_of(const Records<MAX>& t, int chunk) {
   int lo = 0, hi = t.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -139,7 +141,8 @@ __device__ __forceinline__ double block_sum(double x) {
   return x;
 }
 
-__global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_norm(const __grid_constant__ Records t, double* part) {
+template <int MAX>
+__global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_norm(const __grid_constant__ Records<MAX> t, double* part) {
   pdl_wait();
   pdl_trigger();
   double sum = 0.0;
@@ -203,7 +206,8 @@ __device__ __forceinline__ void chunk_scale(const Record& r, const Span& s, floa
   }
 }
 
-__global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_scale(const __grid_constant__ Records t, const double* part, int parts, float scale, float max_norm,
+template <int MAX>
+__global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_scale(const __grid_constant__ Records<MAX> t, const double* part, int parts, float scale, float max_norm,
                                                              float* norm_out) {
   __shared__ float s_factor;
   __shared__ int s_write;
@@ -259,14 +263,14 @@ int chunks_of(const z2z_grad_tensor& t) {
 size_t grad_clip_scratch_bytes(int n) { return (size_t)((n + kRecords - 1) / kRecords) * clip_blocks() * sizeof(double); }
 long long grad_clip_max_elements() { return (long long)kChunkVecs * 4 << 30; }
 
-cudaError_t launch_grad_clip(const z2z_grad_tensor* t, int n, float scale, float max_norm, float* norm, double* part, cudaStream_t s) {
+template <int MAX>
+static cudaError_t launch_clip(const z2z_grad_tensor* t, int n, float scale, float max_norm, float* norm, double* part, cudaStream_t s) {
   const int blocks = clip_blocks();
-  // (16 KB of parameters: filled where they are handed over, launch by launch)
-  Records rec;
+  Records<MAX> rec;                              // filled where it is handed over, launch by launch
   auto fill = [&](int from) {
     rec.count = rec.chunks = 0;
     bool writes = false;
-    for (int i = from; i < n && i < from + kRecords; ++i) {
+    for (int i = from; i < n && i < from + MAX; ++i) {
       if (t[i].numel == 0) continue;
       Record& r = rec.r[rec.count++];
       r.g = reinterpret_cast<const char*>(t[i].d_grad); r.out = reinterpret_cast<char*>(t[i].d_out); r.n = t[i].numel;
@@ -278,22 +282,27 @@ cudaError_t launch_grad_clip(const z2z_grad_tensor* t, int n, float scale, float
     return writes;
   };
   int parts = 0;
-  for (int from = 0; from < n; from += kRecords) {
-    fill(from);
+  bool writes = false;
+  for (int from = 0; from < n; from += MAX) {
+    writes = fill(from);
     const int g = rec.chunks < blocks ? (rec.chunks > 0 ? rec.chunks : 1) : blocks;
-    const cudaError_t e = launch_pdl(k_clip_norm, dim3(g), dim3(kClipThreads), 0, s, rec, part + parts);
+    const cudaError_t e = launch_pdl(k_clip_norm<MAX>, dim3(g), dim3(kClipThreads), 0, s, rec, part + parts);
     if (e != cudaSuccess) return e;
     parts += g;
   }
-  for (int from = 0; from < n || from == 0; from += kRecords) {
-    const bool writes = fill(from);
+  for (int from = 0; from < n || from == 0; from += MAX) {
+    if (n > MAX || n == 0) writes = fill(from);
     if (!writes && from > 0) continue;
     const int g = writes ? (rec.chunks < blocks ? rec.chunks : blocks) : 1;
     if (!writes) rec.chunks = 0;
-    const cudaError_t e = launch_pdl(k_clip_scale, dim3(g), dim3(kClipThreads), 0, s, rec, part, parts, scale, max_norm, from == 0 ? norm : nullptr);
+    const cudaError_t e = launch_pdl(k_clip_scale<MAX>, dim3(g), dim3(kClipThreads), 0, s, rec, part, parts, scale, max_norm, from == 0 ? norm : nullptr);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
+}
+
+cudaError_t launch_grad_clip(const z2z_grad_tensor* t, int n, float scale, float max_norm, float* norm, double* part, cudaStream_t s) {
+  return n <= kFewRecords ? launch_clip<kFewRecords>(t, n, scale, max_norm, norm, part, s) : launch_clip<kRecords>(t, n, scale, max_norm, norm, part, s);
 }
 
 }  // namespace z2z

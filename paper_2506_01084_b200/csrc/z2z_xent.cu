@@ -41,12 +41,12 @@ constexpr int kThreads = 128 + 32 * kEpiWarps;   // a warpgroup of producer, iss
 // Registers: 384 threads are launched with 168 each; the epilogue, which holds a tile's sums, takes what the others leave
 // (128 x 56 + 256 x 224 = 384 x 168).
 constexpr int kRegsFew = 56, kRegsEpi = 224;
-constexpr int kStages = 5;
+constexpr int kRing = 8;                         // stages at most
 constexpr int kTile = 256;                       // vocabulary rows or columns of a tile (128 per CTA)
-constexpr int kStageBytes = 32768;               // 128 x 64 of either operand
+constexpr int kRingBytes = 5 * 32768;            // a stage: 128 x 64 of either operand, or less of the hidden rows
 constexpr int kTurnBytes = 32 * 128;             // a warp's 32 rows of 128 bytes on their way to memory; two of them
 constexpr int kFrontBytes = 1024 + kEpiWarps * 2 * kTurnBytes;     // a multiple of 1024
-constexpr size_t kSmemBytes = 1024 + kFrontBytes + (size_t)kStages * kStageBytes;
+constexpr size_t kSmemBytes = 1024 + kFrontBytes + kRingBytes;
 constexpr int kHyperPad = 32;                    // a sequence's rows start at a multiple of this beside its hypertokens
 constexpr int kLossRows = 8192;                  // rows whose partial sums are held at a time
 constexpr int kMaxParts = 3;                     // bf16 parts of an fp32 value
@@ -54,7 +54,7 @@ constexpr int kMaxSplit = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Ctrl {
-  unsigned long long full[kStages], empty[kStages], acc_full[2], acc_empty[2];
+  unsigned long long full[kRing], empty[kRing], acc_full[2], acc_empty[2];
   uint32_t tmem_base;
   int abort;
 };
@@ -86,6 +86,7 @@ struct Params {
   int v0, vn;                // piece: vocabulary rows v0 .. v0 + vn
   int w_row0;                // its first row in the tensor map of W
   int cta_rows, nv;          // logits: hidden rows per CTA, vocabulary rows per tile
+  int a_bytes;               // and shared memory of a stage's hidden rows
   int tr, th;                // rows per tile of dh, and per tile of a sequence's rows
   int r_lo, r_hi;            // positions of this launch (losses: a share of the rows)
   int sb;                    // row tiles that are taken through all vocabulary tiles before the next ones
@@ -251,6 +252,7 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[kMaxParts]) {
 // A row of a matrix into bf16 (parts), zeros without one; 8 elements per thread and step.
 template <typename T>
 __device__ __forceinline__ void put_row(const T* src, __nv_bfloat16* dst, long long plane, int d, int tid, int threads) {
+#pragma unroll 4
   for (int i = tid * 8; i < d; i += threads * 8) {
     if constexpr (sizeof(T) == 2) {
       uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -386,7 +388,8 @@ struct LogitsWalk {
 // of the table's gradient meanwhile, and then all take those.
 struct GradWalk {
   const Params& p;
-  int c, C, live, RT, T, J2, J3, k3, rest, ahead, skip, phase, idx, jh3, jh2, kb, cost2, cost3;
+  int c, C, live, RT, T, J2, J3, k3, rest, ahead, skip, idx, jh3, jh2, kb, cost2, cost3;
+  int phase;                                     // 0: dh, 1: tables ahead, 2: tables, 3: hypertokens
   __device__ GradWalk(const Params& pp, int c_, int C_) : p(pp), c(c_), C(C_) {
     live = p.pl.head[0];
     RT = ceil_div(live, p.tr);
@@ -404,23 +407,22 @@ struct GradWalk {
     jh2 = p.hyper_hidden ? p.pl.head[2] : 0;
     phase = 0; idx = c;
   }
-  __device__ void table_tile(Job& j, int f) {
+  __device__ __forceinline__ void table_tile(Job& j, int f) {
     const int vt = f / p.dt, ct = f - vt * p.dt;
     j.type = kTables; j.b = -1; j.m0 = vt * kTile; j.r0 = ct * kTile;
     j.n = min(kTile, pad32(p.d - j.r0));
     j.k0 = 0; j.k16 = k3; j.tail = false; j.limit = 0; j.part = 0;
   }
-  __device__ bool next(Job& j) {
+  __device__ __forceinline__ void hidden_tile(Job& j, int f) {
+    const int part = f / T, t = f - part * T, rt = t / p.dt;
+    const int kb0 = (int)((long long)part * kb / p.split), kb1 = (int)((long long)(part + 1) * kb / p.split);
+    j.type = kHidden; j.b = -1; j.m0 = (t - rt * p.dt) * kTile;
+    j.r0 = rt * p.tr; j.limit = min(p.tr, live - j.r0); j.n = pad32(j.limit);
+    j.k0 = kb0 * 64; j.k16 = (kb1 - kb0) * 4; j.tail = false; j.part = part;
+  }
+  __device__ __forceinline__ bool next(Job& j) {
     if (phase == 0) {
-      if (idx < J2) {
-        const int part = idx / T, t = idx - part * T, rt = t / p.dt;
-        const int kb0 = (int)((long long)part * kb / p.split), kb1 = (int)((long long)(part + 1) * kb / p.split);
-        j.type = kHidden; j.b = -1; j.m0 = (t - rt * p.dt) * kTile;
-        j.r0 = rt * p.tr; j.limit = min(p.tr, live - j.r0); j.n = pad32(j.limit);
-        j.k0 = kb0 * 64; j.k16 = (kb1 - kb0) * 4; j.tail = false; j.part = part;
-        idx += C;
-        return true;
-      }
+      if (idx < J2) { hidden_tile(j, idx); idx += C; return true; }
       phase = 1; idx = c - rest;
     }
     if (phase == 1) {
@@ -633,8 +635,13 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   const int rank = (int)cluster_ctarank();       // 0: leader (issues the MMAs), 1: peer
   const int C = gridDim.x >> 1, c = blockIdx.x >> 1;
 
+  // An MMA of the logits reads 128 hidden rows from a stage's start; with fewer loaded it reads on, which only feeds rows of
+  // the result that nobody looks at.
+  const uint32_t b_off = KIND == kProducts ? 16384u : (uint32_t)p.a_bytes, stage_bytes = b_off + 16384u;
+  const int stages = min(kRing, (int)(kRingBytes / stage_bytes));
+
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&ctrl->full[s]), 1); mbar_init(smem_u32(&ctrl->empty[s]), 1); }
+    for (int s = 0; s < kRing; ++s) { mbar_init(smem_u32(&ctrl->full[s]), 1); mbar_init(smem_u32(&ctrl->empty[s]), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctrl->acc_full[b]), 1); mbar_init(smem_u32(&ctrl->acc_empty[b]), 2 * kEpiWarps); }
     ctrl->abort = 0;
     mbar_init_fence();
@@ -654,8 +661,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
     if (warp == 0 && lane == 0) {
       // ---------------- TMA producer (both CTAs): own 128 rows of A, own half of B's ----------------------
       const uint64_t pol = policy_evict_last();
-      uint32_t full_leader[kStages];
-      for (int s = 0; s < kStages; ++s) full_leader[s] = map_to_cta(smem_u32(&ctrl->full[s]), 0);
+      const uint32_t full_leader = map_to_cta(smem_u32(&ctrl->full[0]), 0);
       Walk w(p, c, C);
       Job j;
       int stage = 0; uint32_t phase = 0;
@@ -666,7 +672,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         for (int pr = 0; pr < job_products(p, j.type) && ok; ++pr) {
           for (int kb = 0; kb < blocks; ++kb) {
             if (!mbar_wait(smem_u32(&ctrl->empty[stage]), phase ^ 1u, &ctrl->abort)) { ok = false; break; }
-            const uint32_t A = stage_base + (uint32_t)stage * kStageBytes, B = A + 16384u, bar = full_leader[stage];
+            const uint32_t A = stage_base + (uint32_t)stage * stage_bytes, B = A + b_off, bar = full_leader + 8u * stage;
             auto expect = [&](uint32_t bytes) { if (rank == 0) mbar_expect_tx(smem_u32(&ctrl->full[stage]), 2u * bytes); };
             if (KIND != kProducts) {
               const bool hy = j.type == kLogitsHyper;
@@ -693,7 +699,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
               for (int i = 0; i < nb; ++i)
                 tma_load_3d_pair(B + 8192u * i, hy ? &tm.hh_m : &tm.hs_m, j.r0 + rank * half + 64 * i, h0 + kb * 64, p.b3[pr], bar, pol);
             }
-            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
           }
         }
       }
@@ -724,7 +730,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             --left;
             if (!mbar_wait_warp(smem_u32(&ctrl->full[stage]), phase, &ctrl->abort)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t A = stage_base + (uint32_t)stage * kStageBytes, B = A + 16384u;
+            const uint32_t A = stage_base + (uint32_t)stage * stage_bytes, B = A + b_off;
             const int steps = kb >= whole ? 1 : min(4, j.k16 - 4 * kb);
             if (elect_one()) {
 #pragma unroll
@@ -737,7 +743,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             }
             __syncwarp();
             acc = 1;
-            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
           }
         }
         if (!ok) break;
@@ -941,61 +947,61 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   if (warp == 2) tmem_dealloc_pair(tmem_base, 512);
 }
 
-// 32 threads per row, a warp for 32 rows each: the partial sums of its vocabulary and hypertoken tiles, its loss and lse.
+// Eight rows per block and 128 threads each: the partial sums of its vocabulary and hypertoken tiles, its loss and lse.
 // With gradients to follow (parts_of_rows > 0) lse also goes to the plan, and the copies of a hidden row without weight are
 // zeroed: they are contracted with g = 0, whatever they hold.
 __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan pl, const float2* part, int part_rows, int parts,
-                                                     const float2* part_h, int part_rows_h, const float* tl, int r_lo, int r_hi,
-                                                     GatherArgs g, int parts_of_rows) {
+                                                    const float2* part_h, int part_rows_h, const float* tl, int r_lo, int r_hi,
+                                                    GatherArgs g, int parts_of_rows) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float2 s_ms[32][33];
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, pos = r_lo + blockIdx.x * 32 + x;
-  const bool live = pos < min(pl.head[0], r_hi);
+  __shared__ float2 s_ms[8][129];
+  // neighbouring threads read neighbouring rows
+  const int x = threadIdx.x & 7, y = threadIdx.x >> 3, p0 = r_lo + blockIdx.x * 8, end = min(pl.head[0], r_hi);
   float m = -INFINITY, s = 0.f;
-  if (live) {
+  if (p0 + x < end) {
     auto all = [&](const float2* from, size_t stride, int count) {
       constexpr int kAhead = 8;
-      for (int i = y; i < count; i += 32 * kAhead) {
+      for (int i = y; i < count; i += 128 * kAhead) {
         float2 v[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) v[u] = i + 32 * u < count ? from[(size_t)(i + 32 * u) * stride] : make_float2(-INFINITY, 0.f);
+        for (int u = 0; u < kAhead; ++u) v[u] = i + 128 * u < count ? __ldcg(from + (size_t)(i + 128 * u) * stride) : make_float2(-INFINITY, 0.f);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) merge_ms(m, s, v[u].x, v[u].y);
       }
     };
-    all(part + pos - r_lo, part_rows, parts);
+    all(part + p0 + x - r_lo, part_rows, parts);
     if (cb.cap > 0) {
-      const int row = pl.perm[pos], b = a.row_seq ? a.row_seq[row] : row;
-      all(part_h + pos, part_rows_h, 2 * ceil_div(cb.n[b], kTile));
+      const int row = pl.perm[p0 + x], b = a.row_seq ? a.row_seq[row] : row;
+      all(part_h + p0 + x, part_rows_h, 2 * ceil_div(cb.n[b], kTile));
     }
   }
   s_ms[x][y] = make_float2(m, s);
   __syncthreads();
   // a warp per row from here on
-  const int p2 = r_lo + blockIdx.x * 32 + y;
-  const float2 v = s_ms[y][x];
-  m = v.x; s = v.y;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, pos = p0 + w;
+  if (w >= 8 || pos >= end) return;
+  m = s_ms[w][lane].x; s = s_ms[w][lane].y;
+  for (int i = 32; i < 128; i += 32) merge_ms(m, s, s_ms[w][lane + i].x, s_ms[w][lane + i].y);
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
     const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o);
     // (both lanes of a pair add in the same order)
-    if (x & o) { float lm = om, ls = os; merge_ms(lm, ls, m, s); m = lm; s = ls; }
+    if (lane & o) { float lm = om, ls = os; merge_ms(lm, ls, m, s); m = lm; s = ls; }
     else merge_ms(m, s, om, os);
   }
-  if (p2 >= min(pl.head[0], r_hi)) return;
-  const int row = pl.perm[p2];
-  if (x == 0) {
+  const int row = pl.perm[pos];
+  if (lane == 0) {
     const float ls = logf(s);
     a.lse_out[row] = m + ls;
-    a.loss_out[row] = ls + (m - tl[p2]);
-    if (parts_of_rows) pl.meta[p2].x = m + ls;
+    a.loss_out[row] = ls + (m - tl[pos]);
+    if (parts_of_rows) pl.meta[pos].x = m + ls;
   }
-  if (parts_of_rows && pl.meta[p2].y == 0.f) {
-    const int b = a.row_seq ? a.row_seq[row] : row, h = pl.h0[b] + p2 - pl.s0[b];
+  if (parts_of_rows && pl.meta[pos].y == 0.f) {
+    const int b = a.row_seq ? a.row_seq[row] : row, h = pl.h0[b] + pos - pl.s0[b];
     for (int i = 0; i < parts_of_rows; ++i) {
-      put_row<__nv_bfloat16>(nullptr, g.hs + (size_t)i * g.hs_plane + (size_t)p2 * g.d, 0, g.d, x, 32);
-      if (g.hh) put_row<__nv_bfloat16>(nullptr, g.hh + (size_t)i * g.hh_plane + (size_t)h * g.d, 0, g.d, x, 32);
+      put_row<__nv_bfloat16>(nullptr, g.hs + (size_t)i * g.hs_plane + (size_t)pos * g.d, 0, g.d, lane, 32);
+      if (g.hh) put_row<__nv_bfloat16>(nullptr, g.hh + (size_t)i * g.hh_plane + (size_t)h * g.d, 0, g.d, lane, 32);
     }
   }
 }
@@ -1075,31 +1081,39 @@ template <typename T>
 __global__ void __launch_bounds__(128) k_xent_hidden(CbView cb, RowArgs a, Plan pl, const float* dh, long long slot, int split, T* out, int d) {
   pdl_wait();
   pdl_trigger();
-  const int r = blockIdx.x, pos = pl.inv[r];
-  T* to = out + (size_t)r * d;
+  const int r = blockIdx.x, pos = pl.inv[r], i = (blockIdx.y * 128 + threadIdx.x) * 8;
+  if (i >= d) return;
   int slots = 0;
   if (pos >= 0) { const int b = a.row_seq ? a.row_seq[r] : r; slots = split + (cb.n[b] > 0 ? 1 : 0); }
-  const float scale = __int_as_float(pl.head[4]);
-  for (int i = threadIdx.x * 8; i < d; i += blockDim.x * 8) {
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < slots; ++k) {
-      const float* from = dh + (size_t)k * slot + (size_t)pos * d + i;
-      const float4 u = __ldcg(reinterpret_cast<const float4*>(from)), v = __ldcg(reinterpret_cast<const float4*>(from + 4));
-      s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w; s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
-    }
-    if (slots) {
+  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const float* from = dh + (size_t)(pos < 0 ? 0 : pos) * d + i;
+  constexpr int kAhead = 4;
+  for (int k0 = 0; k0 < slots; k0 += kAhead) {
+    float4 v[kAhead][2];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[k] *= scale;
+    for (int k = 0; k < kAhead; ++k) {
+      if (k0 + k >= slots) break;
+      v[k][0] = __ldcg(reinterpret_cast<const float4*>(from + (size_t)(k0 + k) * slot));
+      v[k][1] = __ldcg(reinterpret_cast<const float4*>(from + (size_t)(k0 + k) * slot + 4));
     }
-    if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<float4*>(to + i) = make_float4(s[0], s[1], s[2], s[3]);
-      *reinterpret_cast<float4*>(to + i + 4) = make_float4(s[4], s[5], s[6], s[7]);
-    } else {
-      uint32_t o[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) { const __nv_bfloat162 t = __floats2bfloat162_rn(s[2 * k], s[2 * k + 1]); o[k] = *reinterpret_cast<const uint32_t*>(&t); }
-      *reinterpret_cast<uint4*>(to + i) = make_uint4(o[0], o[1], o[2], o[3]);
+    for (int k = 0; k < kAhead; ++k) {
+      if (k0 + k >= slots) break;
+      s[0] += v[k][0].x; s[1] += v[k][0].y; s[2] += v[k][0].z; s[3] += v[k][0].w;
+      s[4] += v[k][1].x; s[5] += v[k][1].y; s[6] += v[k][1].z; s[7] += v[k][1].w;
     }
+  }
+  if (slots) {
+    const float scale = __int_as_float(pl.head[4]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[k] *= scale;
+  }
+  T* to = out + (size_t)r * d + i;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(to) = make_float4(s[0], s[1], s[2], s[3]);
+    *reinterpret_cast<float4*>(to + 4) = make_float4(s[4], s[5], s[6], s[7]);
+  } else {
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]), pack_bf16(s[4], s[5]), pack_bf16(s[6], s[7]));
   }
 }
 
@@ -1336,7 +1350,8 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   if (e != cudaSuccess) return e;
 
   Params p{};
-  p.cb = cb; p.pl = l.pl; p.d = d; p.dt = sh.dt; p.cta_rows = sh.cta_rows; p.nv = sh.nv; p.tr = sh.tr; p.th = sh.th;
+  p.cb = cb; p.pl = l.pl; p.d = d; p.dt = sh.dt; p.cta_rows = sh.cta_rows; p.nv = sh.nv; p.tr = sh.tr;
+  p.a_bytes = (int)up_to(128ll * (sh.cap > 0 && sh.th / 2 > sh.cta_rows ? sh.th / 2 : sh.cta_rows), 1024); p.th = sh.th;
   products(sh.parts, sh.parts, &p.np1, p.a1, p.b1);
   if (grad) {
     // (dh of a bf16 session takes the first of g's parts: it is stored in bf16)
@@ -1400,7 +1415,7 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
         if (e != cudaSuccess) return e;
       }
       const int parts = p.part0 + 2 * vocabulary_tiles(p.vn, sh.nv);
-      e = launch_pdl(k_xent_merge, dim3((p.r_hi - p.r_lo + 31) / 32), dim3(1024), 0, s, cb, a, l.pl, l.part, p.part_rows, parts, l.part_h, sh.np, l.tl,
+      e = launch_pdl(k_xent_merge, dim3((p.r_hi - p.r_lo + 7) / 8), dim3(1024), 0, s, cb, a, l.pl, l.part, p.part_rows, parts, l.part_h, sh.np, l.tl,
                      p.r_lo, p.r_hi, g, grad ? sh.parts : 0);
       if (e != cudaSuccess) return e;
     }
@@ -1423,8 +1438,8 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   }
   if (!x.g_hidden) return cudaSuccess;
   return sh.dtype == Z2Z_DTYPE_FP32
-             ? launch_pdl(k_xent_hidden<float>, dim3(x.N), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<float*>(x.g_hidden), d)
-             : launch_pdl(k_xent_hidden<__nv_bfloat16>, dim3(x.N), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<__nv_bfloat16*>(x.g_hidden), d);
+             ? launch_pdl(k_xent_hidden<float>, dim3(x.N, (d + 1023) / 1024), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<float*>(x.g_hidden), d)
+             : launch_pdl(k_xent_hidden<__nv_bfloat16>, dim3(x.N, (d + 1023) / 1024), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<__nv_bfloat16*>(x.g_hidden), d);
 }
 
 }  // namespace
