@@ -41,7 +41,7 @@ constexpr int kThreads = 128 + 32 * kEpiWarps;   // a warpgroup of producer, iss
 // Registers: 384 threads are launched with 168 each; the epilogue, which holds a tile's sums, takes what the others leave
 // (128 x 56 + 256 x 224 = 384 x 168).
 constexpr int kRegsFew = 56, kRegsEpi = 224;
-constexpr int kRing = 8;                         // stages at most
+constexpr int kRing = 10;                        // stages at most
 constexpr int kTile = 256;                       // vocabulary rows or columns of a tile (128 per CTA)
 constexpr int kRingBytes = 5 * 32768;            // a stage: 128 x 64 of either operand, or less of the hidden rows
 constexpr int kTurnBytes = 32 * 128;             // a warp's 32 rows of 128 bytes on their way to memory; two of them
@@ -54,7 +54,7 @@ constexpr int kMaxSplit = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Ctrl {
-  unsigned long long full[kRing], empty[kRing], acc_full[2], acc_empty[2];
+  unsigned long long full[kRing], empty[kRing], acc_full[2], acc_empty[2], done;
   uint32_t tmem_base;
   int abort;
 };
@@ -68,6 +68,7 @@ struct Plan {
   int32_t *j1, *j2, *j3;     // [B + 1] jobs of the sequences before
   int32_t *perm, *inv;       // position -> row, row -> position or -1
   float4* meta;              // per position: lse, weight / largest, target and visible hypertokens (bits)
+  float* rest;               // and what lse has lost to its rounding, where this call has it
 };
 
 struct RowArgs {
@@ -90,14 +91,14 @@ struct Params {
   int tr, th;                // rows per tile of dh, and per tile of a sequence's rows
   int r_lo, r_hi;            // positions of this launch (losses: a share of the rows)
   int sb;                    // row tiles that are taken through all vocabulary tiles before the next ones
-  int np1, np2, np3;         // products of parts
-  int8_t a1[6], b1[6], a2[6], b2[6], a3[6], b3[6];
+  int parts;                 // bf16 parts of the session's operands
+  int np2, np3;              // products of parts for dh and for the tables
   bool hyper;                // with the sequences' hypertokens
   bool hyper_hidden;         // their share of dh
   int first;                 // first piece: dh's partial sums are set, not added to
   // logits
   __nv_bfloat16 *g, *gh; long long g_plane, gh_plane; int g_pitch, gh_pitch, g_parts;
-  bool exact_exp; int exact_sums;                // bit 0: of dh, bit 1: of the tables
+  bool exact_exp;
   float2 *part, *part_h; int part_rows, part_rows_h, part0;
   float* tl;
   // gradients
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_xent_plan(CbView cb, RowArgs a
     __syncthreads();
     if (q >= 0 && rank == 0) { atomicAdd(&s_cnt[q], (int)s_warp[q * 32 + warp]); s_warp[q * 32 + warp] = 0; }
     if (r < a.N) pl.inv[r] = at;
-    if (at >= 0) { pl.perm[at] = r; pl.meta[at] = m; }
+    if (at >= 0) { pl.perm[at] = r; pl.meta[at] = m; pl.rest[at] = 0.f; }
     __syncthreads();
   }
 }
@@ -453,16 +454,20 @@ struct GradWalk {
   }
 };
 
-__device__ __forceinline__ int job_products(const Params& p, int type) {
-  return type <= kLogitsHyper ? p.np1 : (type <= kHiddenHyper ? p.np2 : p.np3);
-}
+// Without operands in several parts: times that the contracted axis is gone through, once for each part of g.
+__device__ __forceinline__ int job_turns(const Params& p, int type) { return type >= kTables ? p.g_parts : 1; }
 __device__ __forceinline__ int job_blocks(const Job& j) { return (j.k16 + 3) / 4 + (j.tail ? 1 : 0); }
 // The tensor cores' additions into an accumulator truncate: a chain of n of them is off by about n / 2 steps of 2^-24 to
-// one side (losses at d = 4096 were 3e-6 off).  Where that counts an accumulator takes kChain blocks of 64, and the epilogue
+// one side (losses at d = 4096 were 3e-6 off).  Where that counts an accumulator takes so many blocks of 64, and the epilogue
 // adds those sums in registers, rounded to nearest, while the MMAs go on in the other accumulator.
-constexpr int kChain = 16;
+constexpr int kChain = 8;
 __device__ __forceinline__ int job_chain(const Params& p, const Job& j) {
-  return j.type <= kLogitsHyper || (p.exact_sums & (j.type <= kHiddenHyper ? 1 : 2)) ? kChain : 1 << 30;
+  if (p.parts > 1) return 1;                     // (six products)
+  return j.type <= kLogitsHyper ? kChain : (j.type <= kHiddenHyper ? 1 << 30 : kChain);
+}
+constexpr unsigned long long kDrainNs = 10ull * 1000 * 1000;
+__device__ __forceinline__ bool mbar_wait_warp_limit(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long ns) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ns));
 }
 
 // MN-major operand of 64-column boxes of 64 rows with the 128-byte swizzle: the next 8 contracted rows are 1024 bytes
@@ -487,6 +492,12 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// exp with the rounding of x log2 e made good: ex2's own error (2^-22) is what is left.
+__device__ __forceinline__ float exp_exact(float x) {
+  const float y = x * kLog2e, r = fmaf(x, kLog2e, -y), e = ex2(y);
+  return y > -200.f ? fmaf(e, r * 0.69314718f, e) : e;                       // (-inf: r is no number)
 }
 
 __device__ __forceinline__ void merge_ms(float& m, float& s, float om, float os) {
@@ -622,8 +633,9 @@ __device__ __forceinline__ void store_columns(float (&v)[64], Turn& turn, const 
   }
 }
 
-// CHAINED: accumulators of kChain blocks, added in registers.
-template <int KIND, bool CHAINED, typename TO>
+// CHAINED: accumulators of some blocks, added in registers.  MULTI: operands of several parts, every part a stage of its own that
+// all its products read (a stage per product moved twice the bytes through L2, which is what bounds it then).
+template <int KIND, bool CHAINED, bool MULTI, typename TO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   using Walk = typename std::conditional<KIND == kProducts, GradWalk, LogitsWalk>::type;
@@ -638,11 +650,12 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   // An MMA of the logits reads 128 hidden rows from a stage's start; with fewer loaded it reads on, which only feeds rows of
   // the result that nobody looks at.
   const uint32_t b_off = KIND == kProducts ? 16384u : (uint32_t)p.a_bytes, stage_bytes = b_off + 16384u;
-  const int stages = min(kRing, (int)(kRingBytes / stage_bytes));
+  const int stages = MULTI ? kRingBytes / 16384 : min(kRing, (int)(kRingBytes / stage_bytes));
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kRing; ++s) { mbar_init(smem_u32(&ctrl->full[s]), 1); mbar_init(smem_u32(&ctrl->empty[s]), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctrl->acc_full[b]), 1); mbar_init(smem_u32(&ctrl->acc_empty[b]), 2 * kEpiWarps); }
+    mbar_init(smem_u32(&ctrl->done), 1);
     ctrl->abort = 0;
     mbar_init_fence();
   }
@@ -664,43 +677,78 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
       const uint32_t full_leader = map_to_cta(smem_u32(&ctrl->full[0]), 0);
       Walk w(p, c, C);
       Job j;
-      int stage = 0; uint32_t phase = 0;
+      int stage = 0, issued = 0; uint32_t phase = 0;
       bool ok = true;
+      auto begin = [&](uint32_t bytes) {         // the next stage, with so many bytes to come in each CTA
+        ok = mbar_wait(smem_u32(&ctrl->empty[stage]), phase ^ 1u, &ctrl->abort);
+        if (ok && rank == 0) mbar_expect_tx(smem_u32(&ctrl->full[stage]), 2u * bytes);
+        return ok;
+      };
+      auto end = [&]() { ++issued; if (++stage == stages) { stage = 0; phase ^= 1u; } };
+      // An operand of a job: boxes from (x, y) on, (dx, dy) further per block, with one 64 columns beside them where `two`.
+      // (All of it is set up per job: with the choices made per box the thread issued a block every 600 clocks, and the
+      // MMAs waited for it.)
+      struct Side {
+        const CUtensorMap* m;
+        int x, y, dx, dy;
+        bool two;
+        uint32_t bytes;
+      };
+      auto load = [&](const Side& o, uint32_t at, uint32_t bar, int x, int y, int part) {
+        tma_load_3d_pair(at, o.m, x, y, part, bar, pol);
+        if (KIND == kProducts && o.two) tma_load_3d_pair(at + 8192u, o.m, x + 64, y, part, bar, pol);
+      };
       while (ok && w.next(j)) {
-        const int blocks = job_blocks(j), half = j.n >> 1, whole = (j.k16 + 3) / 4;
-        const int h0 = j.b >= 0 ? p.pl.h0[j.b] : 0;
-        for (int pr = 0; pr < job_products(p, j.type) && ok; ++pr) {
-          for (int kb = 0; kb < blocks; ++kb) {
-            if (!mbar_wait(smem_u32(&ctrl->empty[stage]), phase ^ 1u, &ctrl->abort)) { ok = false; break; }
-            const uint32_t A = stage_base + (uint32_t)stage * stage_bytes, B = A + b_off, bar = full_leader + 8u * stage;
-            auto expect = [&](uint32_t bytes) { if (rank == 0) mbar_expect_tx(smem_u32(&ctrl->full[stage]), 2u * bytes); };
-            if (KIND != kProducts) {
-              const bool hy = j.type == kLogitsHyper;
-              expect(16384u + 128u * (uint32_t)(hy ? p.th >> 1 : p.cta_rows));
-              if (hy) {
-                tma_load_3d_pair(A, &tm.hh_k, kb * 64, h0 + j.m0 + rank * (p.th >> 1), p.a1[pr], bar, pol);
-                tma_load_3d_pair(B, &tm.u_k, kb * 64, j.b * p.cb.cap + j.r0 + rank * half, p.b1[pr], bar, pol);
-              } else {
-                tma_load_3d_pair(A, &tm.hs_k, kb * 64, j.m0 + rank * p.cta_rows, p.a1[pr], bar, pol);
-                tma_load_3d_pair(B, &tm.w_k, kb * 64, p.w_row0 + j.r0 + rank * half, p.b1[pr], bar, pol);
-              }
-            } else if (j.type == kHidden || j.type == kHiddenHyper) {
-              const bool hy = j.type == kHiddenHyper, last = kb >= whole;
-              expect((last ? 4096u : 16384u) + 64u * (uint32_t)(hy ? p.th : p.tr));            // (G: half a tile's rows)
-              const CUtensorMap* am = hy ? (last ? &tm.ut_m : &tm.u_m) : &tm.w_m;
-              const int ay = hy ? (last ? j.b * 16 : j.b * p.cb.cap + kb * 64) : p.w_row0 + j.k0 + kb * 64;
-              for (int i = 0; i < 2; ++i) tma_load_3d_pair(A + 8192u * i, am, j.m0 + rank * 128 + 64 * i, ay, p.a2[pr], bar, pol);
-              tma_load_3d_pair(B, hy ? &tm.gh_k : &tm.g_k, last ? j.k16 * 16 : j.k0 + kb * 64, h0 + j.r0 + rank * half, p.b2[pr], bar, pol);
-            } else {
-              const bool hy = j.type == kTablesHyper;
-              const int nb = half > 64 ? 2 : 1;
-              expect(16384u + 8192u * nb);
-              for (int i = 0; i < 2; ++i) tma_load_3d_pair(A + 8192u * i, hy ? &tm.gh_m : &tm.g_m, j.m0 + rank * 128 + 64 * i, h0 + kb * 64, p.a3[pr], bar, pol);
-              for (int i = 0; i < nb; ++i)
-                tma_load_3d_pair(B + 8192u * i, hy ? &tm.hh_m : &tm.hs_m, j.r0 + rank * half + 64 * i, h0 + kb * 64, p.b3[pr], bar, pol);
-            }
-            if (++stage == stages) { stage = 0; phase ^= 1u; }
+        const int half = j.n >> 1, whole = (j.k16 + 3) / 4;
+        const bool hy = j.b >= 0;
+        const int h0 = hy ? p.pl.h0[j.b] : 0;
+        Side A, B;
+        if (KIND != kProducts) {
+          const int rows = hy ? p.th >> 1 : p.cta_rows;
+          A = Side{hy ? &tm.hh_k : &tm.hs_k, 0, h0 + j.m0 + rank * rows, 64, 0, false, 128u * rows};
+          B = Side{hy ? &tm.u_k : &tm.w_k, 0, (hy ? j.b * p.cb.cap : p.w_row0) + j.r0 + rank * half, 64, 0, false, 16384u};
+        } else if (j.type == kHidden || j.type == kHiddenHyper) {
+          A = Side{hy ? &tm.u_m : &tm.w_m, j.m0 + rank * 128, hy ? j.b * p.cb.cap : p.w_row0 + j.k0, 0, 64, true, 16384u};
+          B = Side{hy ? &tm.gh_k : &tm.g_k, j.k0, h0 + j.r0 + rank * half, 64, 0, false, 64u * (hy ? p.th : p.tr)};
+        } else {
+          A = Side{hy ? &tm.gh_m : &tm.g_m, j.m0 + rank * 128, h0, 0, 64, true, 16384u};
+          B = Side{hy ? &tm.hh_m : &tm.hs_m, j.r0 + rank * half, h0, 0, 64, half > 64, half > 64 ? 16384u : 8192u};
+        }
+        const int turns = MULTI ? 1 : job_turns(p, j.type);
+        auto block = [&](int part, int ax, int ay, int bx, int by) {
+          if constexpr (MULTI) {
+            // (in the order in which the MMAs want them)
+            auto one = [&](const Side& o, int x, int y, int i) {
+              if (ok && begin(o.bytes)) { load(o, stage_base + (uint32_t)stage * 16384u, full_leader + 8u * stage, x, y, i); end(); }
+            };
+            one(A, ax, ay, 2); one(B, bx, by, 0); one(A, ax, ay, 0); one(B, bx, by, 2); one(A, ax, ay, 1); one(B, bx, by, 1);
+          } else if (begin(A.bytes + B.bytes)) {
+            const uint32_t at = stage_base + (uint32_t)stage * stage_bytes, bar = full_leader + 8u * stage;
+            load(A, at, bar, ax, ay, part);
+            load(B, at + b_off, bar, bx, by, 0);
+            end();
           }
+        };
+        for (int part = 0; part < turns && ok; ++part) {
+          int ax = A.x, ay = A.y, bx = B.x, by = B.y;
+          for (int kb = 0; kb < whole && ok; ++kb) {
+            block(part, ax, ay, bx, by);
+            ax += A.dx; ay += A.dy; bx += B.dx; by += B.dy;
+          }
+        }
+        if (KIND == kProducts && j.tail && ok) { // (dh alone: one turn)
+          A.m = &tm.ut_m; A.bytes = 4096u;
+          block(0, A.x, j.b * 16, j.k16 * 16, B.y);
+        }
+      }
+      // A role that gave up: copies that are under way land before the block ends (the peer's count on the leader's barriers,
+      // and it waits for the leader below).
+      if (!ok && rank == 0) {
+        int left = 0;
+        for (int i = 0; i < min(issued, stages); ++i) {
+          const int at = stage - 1 - i;
+          mbar_wait(smem_u32(&ctrl->full[at < 0 ? at + stages : at]), at < 0 ? phase ^ 1u : phase, &left, kDrainNs);
+          left = 0;
         }
       }
     } else if (warp == 1 && rank == 0) {
@@ -709,47 +757,89 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
       Job j;
       int stage = 0; uint32_t phase = 0, job_i = 0;
       bool ok = true;
+      auto arrived = [&]() {
+        ok = mbar_wait_warp(smem_u32(&ctrl->full[stage]), phase, &ctrl->abort);
+        tc_fence_after();
+        return ok;
+      };
+      auto advance = [&]() { if (++stage == stages) { stage = 0; phase ^= 1u; } };
       while (ok && w.next(j)) {
-        const int blocks = job_blocks(j), products = job_products(p, j.type), whole = (j.k16 + 3) / 4;
+        const int blocks = job_blocks(j), whole = (j.k16 + 3) / 4;
         if (blocks == 0) continue;               // (nothing to contract: the epilogue writes zeros)
         const int chain = CHAINED ? job_chain(p, j) : 1 << 30;
         int left = 0;                            // blocks until the accumulator changes
         const bool a_mn = KIND == kProducts, b_mn = j.type >= kTables;
         const uint32_t idesc = idesc_bf16_f32(kTile, j.n) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
         uint32_t acc = 0, D = 0;
-        for (int pr = 0; pr < products && ok; ++pr) {
-          for (int kb = 0; kb < blocks; ++kb) {
-            if (left == 0) {
-              if (acc) { if (elect_one()) umma_commit_pair(smem_u32(&ctrl->acc_full[job_i & 1u])); __syncwarp(); ++job_i; }
-              if (!mbar_wait_warp(smem_u32(&ctrl->acc_empty[job_i & 1u]), ((job_i >> 1) & 1u) ^ 1u, &ctrl->abort)) { ok = false; break; }
-              tc_fence_after();
-              D = tmem_base + (job_i & 1u) * kTile;
-              acc = 0;
-              left = chain;
-            }
-            --left;
-            if (!mbar_wait_warp(smem_u32(&ctrl->full[stage]), phase, &ctrl->abort)) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t A = stage_base + (uint32_t)stage * stage_bytes, B = A + b_off;
-            const int steps = kb >= whole ? 1 : min(4, j.k16 - 4 * kb);
-            if (elect_one()) {
+        // (a descriptor's address counts 16 bytes in its low bits: a step of 16 is 32 bytes on in a K-major operand, 2048 in
+        // an MN-major one)
+        const uint64_t a_kind = a_mn ? smem_desc_mn(0) : smem_desc_sw128(0), b_kind = b_mn ? smem_desc_mn(0) : smem_desc_sw128(0);
+        const uint32_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
+        auto mma = [&](uint32_t A, uint32_t B, int steps) {        // by one lane
+          const uint64_t a = a_kind + (A >> 4), b = b_kind + (B >> 4);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                if (k < steps)
-                  umma_bf16_pair(D, a_mn ? smem_desc_mn(A + k * 2048) : smem_desc_sw128(A + k * 32),
-                                 b_mn ? smem_desc_mn(B + k * 2048) : smem_desc_sw128(B + k * 32), idesc, k ? 1u : acc);
-              }
+          for (int k = 0; k < 4; ++k)
+            if (k < steps) umma_bf16_pair(D, a + k * a_step, b + k * b_step, idesc, k ? 1u : acc);
+        };
+        const int turns = MULTI ? 1 : job_turns(p, j.type);
+        for (int i = 0, kb = 0; i < blocks * turns; ++i, kb = kb + 1 == blocks ? 0 : kb + 1) {
+          if (left == 0) {
+            if (i) { if (elect_one()) umma_commit_pair(smem_u32(&ctrl->acc_full[job_i & 1u])); __syncwarp(); ++job_i; }
+            ok = mbar_wait_warp(smem_u32(&ctrl->acc_empty[job_i & 1u]), ((job_i >> 1) & 1u) ^ 1u, &ctrl->abort);
+            if (!ok) break;
+            tc_fence_after();
+            D = tmem_base + (job_i & 1u) * kTile;
+            acc = 0;
+            left = chain;
+          }
+          --left;
+          const int steps = kb >= whole ? 1 : min(4, j.k16 - 4 * kb);
+          if constexpr (MULTI) {
+            // The six products of parts that fp32 can hold, the smallest first: the accumulator has its size only for the last
+            // one, and what truncation there is counts from then on.
+            uint32_t at[6], bar[6];
+            auto take = [&](int i) {
+              at[i] = stage_base + (uint32_t)stage * 16384u;
+              bar[i] = smem_u32(&ctrl->empty[stage]);
+              if (!arrived()) return false;
+              advance();
+              return true;
+            };
+            if (!take(0) || !take(1)) break;                                 // A2, B0
+            if (elect_one()) mma(at[0], at[1], steps);
+            __syncwarp();
+            acc = 1;
+            if (!take(2) || !take(3)) break;                                 // A0, B2
+            if (elect_one()) { mma(at[2], at[3], steps); umma_commit_pair(bar[0]); umma_commit_pair(bar[3]); }
+            __syncwarp();
+            if (!take(4) || !take(5)) break;                                 // A1, B1
+            if (elect_one()) {
+              mma(at[4], at[5], steps); mma(at[4], at[1], steps); mma(at[2], at[5], steps); mma(at[2], at[1], steps);
+              umma_commit_pair(bar[1]); umma_commit_pair(bar[2]); umma_commit_pair(bar[4]); umma_commit_pair(bar[5]);
+            }
+            __syncwarp();
+          } else {
+            if (!arrived()) break;
+            const uint32_t at = stage_base + (uint32_t)stage * stage_bytes;
+            if (elect_one()) {
+              mma(at, at + b_off, steps);
               umma_commit_pair(smem_u32(&ctrl->empty[stage]));
             }
             __syncwarp();
             acc = 1;
-            if (++stage == stages) { stage = 0; phase ^= 1u; }
+            advance();
           }
         }
         if (!ok) break;
         if (elect_one()) umma_commit_pair(smem_u32(&ctrl->acc_full[job_i & 1u]));
         __syncwarp();
         ++job_i;
+      }
+      if (!ok) {                                 // MMAs under way end before their memory is given back
+        if (elect_one()) umma_commit_pair(smem_u32(&ctrl->done));
+        __syncwarp();
+        int none = 0;
+        mbar_wait_warp_limit(smem_u32(&ctrl->done), 0, &none, kDrainNs);
       }
     }
   } else {
@@ -767,7 +857,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
     uint32_t job_i = 0;
     bool ok = true;
     while (w.next(j)) {
-      const int blocks = job_blocks(j) * job_products(p, j.type), chain = CHAINED ? job_chain(p, j) : 1 << 30;
+      const int blocks = job_blocks(j) * (MULTI ? 1 : job_turns(p, j.type)), chain = CHAINED ? job_chain(p, j) : 1 << 30;
       const bool some = blocks > 0;
       // the tile's sums, after which its accumulators are free
       float acc[2][64];                          // columns 128 half + 64 u + x
@@ -829,7 +919,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         const long long pitch = 2ll * (hy ? p.gh_pitch : p.g_pitch);
         if constexpr (KIND == kGrad) {
           const long long plane = hy ? p.gh_plane : p.g_plane;
-          const float lse = r.x, weight = r.y;
+          const float lse = r.x, weight = r.y, rest = there ? p.pl.rest[pos] : 0.f;
           const int show = weight != 0.f ? see : 0;
           const bool all = __all_sync(0xffffffffu, show >= 128);
 #pragma unroll
@@ -839,7 +929,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             float (&v)[64] = acc[u];
             if (p.exact_exp) {
 #pragma unroll
-              for (int x = 0; x < 64; ++x) v[x] = weight * (expf(v[x] - lse) - (x == at - 64 * u ? 1.f : 0.f));
+              for (int x = 0; x < 64; ++x) v[x] = weight * (exp_exact((v[x] - lse) - rest) - (x == at - 64 * u ? 1.f : 0.f));
             } else {
 #pragma unroll
               for (int x = 0; x < 64; ++x) v[x] = weight * (ex2((v[x] - lse) * kLog2e) - (x == at - 64 * u ? 1.f : 0.f));
@@ -995,7 +1085,7 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
     const float ls = logf(s);
     a.lse_out[row] = m + ls;
     a.loss_out[row] = ls + (m - tl[pos]);
-    if (parts_of_rows) pl.meta[pos].x = m + ls;
+    if (parts_of_rows) { pl.meta[pos].x = m + ls; pl.rest[pos] = m == INFINITY ? 0.f : (m - (m + ls)) + ls; }
   }
   if (parts_of_rows && pl.meta[pos].y == 0.f) {
     const int b = a.row_seq ? a.row_seq[row] : row, h = pl.h0[b] + pos - pl.s0[b];
@@ -1217,7 +1307,7 @@ Layout layout_of(const Shape& s, char* base) {
   int32_t** tables[] = {&l.pl.s0, &l.pl.h0, &l.pl.j1, &l.pl.j2, &l.pl.j3};
   for (int32_t** t : tables) *t = (int32_t*)take((size_t)(s.B + 1) * 4);
   l.pl.perm = (int32_t*)take((size_t)s.np * 4); l.pl.inv = (int32_t*)take((size_t)s.np * 4);
-  l.pl.meta = (float4*)take((size_t)s.np * 16);
+  l.pl.meta = (float4*)take((size_t)s.np * 16); l.pl.rest = (float*)take((size_t)s.np * 4);
   l.hs = (__nv_bfloat16*)take(row * s.np);
   if (s.cap > 0) {
     l.hh = (__nv_bfloat16*)take(row * s.nh);
@@ -1296,27 +1386,18 @@ bool make_map(CUtensorMap* m, const void* base, long long rows, long long cols, 
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Products of parts, the smallest first.
-void products(int parts_a, int parts_b, int* n, int8_t* a, int8_t* b) {
-  *n = 0;
-  for (int sum = kMaxParts - 1; sum >= 0; --sum)
-    for (int i = 0; i < parts_a; ++i) {
-      const int k = sum - i;
-      if (k >= 0 && k < parts_b) { a[*n] = (int8_t)i; b[*n] = (int8_t)k; ++*n; }
-    }
-}
-
-template <int KIND, bool CHAINED, typename TO>
+template <int KIND, bool CHAINED, bool MULTI, typename TO>
 cudaError_t launch_main(const Params& p, const Maps& tm, int clusters, cudaStream_t s) {
-  auto kern = k_xent<KIND, CHAINED, TO>;
+  auto kern = k_xent<KIND, CHAINED, MULTI, TO>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   if (e != cudaSuccess) return e;
   return launch_pdl(kern, dim3(2 * clusters), dim3(kThreads), kSmemBytes, s, p, tm);
 }
-
-template <int KIND, typename TO>
-cudaError_t launch_main(const Params& p, const Maps& tm, int clusters, bool chained, cudaStream_t s) {
-  return chained ? launch_main<KIND, true, TO>(p, tm, clusters, s) : launch_main<KIND, false, TO>(p, tm, clusters, s);
+template <int KIND>
+cudaError_t launch_logits(const Params& p, const Maps& tm, int clusters, cudaStream_t s) {
+  if constexpr (KIND != kKeep)
+    if (p.parts > 1) return launch_main<KIND, true, true, float>(p, tm, clusters, s);
+  return p.d > 64 * kChain ? launch_main<KIND, true, false, float>(p, tm, clusters, s) : launch_main<KIND, false, false, float>(p, tm, clusters, s);
 }
 
 // Losses, gradients from lse, or both.
@@ -1352,14 +1433,10 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   Params p{};
   p.cb = cb; p.pl = l.pl; p.d = d; p.dt = sh.dt; p.cta_rows = sh.cta_rows; p.nv = sh.nv; p.tr = sh.tr;
   p.a_bytes = (int)up_to(128ll * (sh.cap > 0 && sh.th / 2 > sh.cta_rows ? sh.th / 2 : sh.cta_rows), 1024); p.th = sh.th;
-  products(sh.parts, sh.parts, &p.np1, p.a1, p.b1);
-  if (grad) {
-    // (dh of a bf16 session takes the first of g's parts: it is stored in bf16)
-    products(sh.parts, sh.parts, &p.np2, p.a2, p.b2);
-    products(sh.g_parts, sh.parts, &p.np3, p.a3, p.b3);
-  }
+  p.parts = sh.parts;
+  // (dh of a bf16 session takes the first of g's parts: it is stored in bf16)
+  p.np2 = sh.parts > 1 ? 6 : 1; p.np3 = sh.parts > 1 ? 6 : sh.g_parts;
   p.g_parts = sh.g_parts; p.exact_exp = sh.g_parts > 1;
-  p.exact_sums = (sh.parts > 1 ? 1 : 0) | (sh.g_parts > 1 ? 2 : 0);
   p.g = l.g; p.g_pitch = sh.vc; p.g_plane = (long long)sh.vc * sh.np;
   p.gh = l.gh; p.gh_pitch = hyper_rows(sh); p.gh_plane = (long long)hyper_rows(sh) * sh.nh;
   p.part = l.part; p.part_h = l.part_h; p.part_rows = loss_rows(sh); p.part_rows_h = sh.np; p.tl = l.tl;
@@ -1403,7 +1480,6 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
     if (sh.parts == 1 || (again && sh.pieces == 1)) return cudaSuccess;
     return launch_pdl(k_xent_split, dim3(p.vn < 4096 ? p.vn : 4096), dim3(128), 0, s, reinterpret_cast<const float*>(x.WU) + (size_t)p.v0 * d, l.wp, w_plane, p.vn, d);
   };
-  const bool chained = p.np1 * ((d + 63) / 64) > kChain;                     // (logits)
   if (loss) {
     const int share = loss_rows(sh) < x.N ? loss_rows(sh) : x.N;
     for (int r0 = 0; r0 < x.N; r0 += share) {
@@ -1411,7 +1487,7 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
       for (int i = 0; i < sh.pieces; ++i) {
         p.hyper = i == 0 && r0 == 0 && sh.cap > 0;
         if ((e = piece(i, r0 > 0)) != cudaSuccess) return e;
-        e = keep ? launch_main<kKeep, float>(p, tm, clusters, chained, s) : launch_main<kLoss, float>(p, tm, clusters, chained, s);
+        e = keep ? launch_logits<kKeep>(p, tm, clusters, s) : launch_logits<kLoss>(p, tm, clusters, s);
         if (e != cudaSuccess) return e;
       }
       const int parts = p.part0 + 2 * vocabulary_tiles(p.vn, sh.nv);
@@ -1431,9 +1507,11 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
     p.hyper = i == 0 && sh.cap > 0;
     p.hyper_hidden = p.hyper && p.dh;
     if ((e = piece(i, loss)) != cudaSuccess) return e;
-    if (!keep && (e = launch_main<kGrad, float>(p, tm, clusters, chained, s)) != cudaSuccess) return e;
-    e = x.grad_dtype == Z2Z_DTYPE_FP32 ? launch_main<kProducts, true, float>(p, tm, clusters, s)
-                                       : launch_main<kProducts, __nv_bfloat16>(p, tm, clusters, p.exact_sums != 0, s);
+    if (!keep && (e = launch_logits<kGrad>(p, tm, clusters, s)) != cudaSuccess) return e;
+    if (x.grad_dtype == Z2Z_DTYPE_FP32)
+      e = sh.parts > 1 ? launch_main<kProducts, true, true, float>(p, tm, clusters, s) : launch_main<kProducts, true, false, float>(p, tm, clusters, s);
+    else
+      e = sh.parts > 1 ? launch_main<kProducts, true, true, __nv_bfloat16>(p, tm, clusters, s) : launch_main<kProducts, false, false, __nv_bfloat16>(p, tm, clusters, s);
     if (e != cudaSuccess) return e;
   }
   if (!x.g_hidden) return cudaSuccess;
