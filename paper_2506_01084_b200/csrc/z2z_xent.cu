@@ -724,7 +724,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             one(A, ax, ay, 2); one(B, bx, by, 0); one(A, ax, ay, 0); one(B, bx, by, 2); one(A, ax, ay, 1); one(B, bx, by, 1);
           } else if (begin(A.bytes + B.bytes)) {
             const uint32_t at = stage_base + (uint32_t)stage * stage_bytes, bar = full_leader + 8u * stage;
-            load(A, at, bar, ax, ay, part);
+            load(A, at, bar, ax, ay, turns - 1 - part);        // (g's smallest part first)
             load(B, at + b_off, bar, bx, by, 0);
             end();
           }
@@ -929,11 +929,17 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             float (&v)[64] = acc[u];
             if (p.exact_exp) {
 #pragma unroll
-              for (int x = 0; x < 64; ++x) v[x] = weight * (exp_exact((v[x] - lse) - rest) - (x == at - 64 * u ? 1.f : 0.f));
+              for (int x = 0; x < 64; ++x) v[x] = exp_exact((v[x] - lse) - rest);
             } else {
 #pragma unroll
-              for (int x = 0; x < 64; ++x) v[x] = weight * (ex2((v[x] - lse) * kLog2e) - (x == at - 64 * u ? 1.f : 0.f));
+              for (int x = 0; x < 64; ++x) v[x] = ex2((v[x] - lse) * kLog2e);
             }
+            if (__any_sync(0xffffffffu, at >= 64 * u && at < 64 * u + 64)) {
+#pragma unroll
+              for (int x = 0; x < 64; ++x) v[x] -= x == at - 64 * u ? 1.f : 0.f;
+            }
+#pragma unroll
+            for (int x = 0; x < 64; ++x) v[x] *= weight;
             if (!all) {
 #pragma unroll
               for (int x = 0; x < 64; ++x) v[x] = x < show - 64 * u ? v[x] : 0.f;
@@ -941,10 +947,13 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             for (int part = 0; part < p.g_parts; ++part) {
               uint32_t o[32];
 #pragma unroll
-              for (int x = 0; x < 32; ++x) {
-                o[x] = pack_bf16(v[2 * x], v[2 * x + 1]);
-                v[2 * x] -= __uint_as_float(o[x] << 16);
-                v[2 * x + 1] -= __uint_as_float(o[x] & 0xffff0000u);
+              for (int x = 0; x < 32; ++x) o[x] = pack_bf16(v[2 * x], v[2 * x + 1]);
+              if (part + 1 < p.g_parts) {
+#pragma unroll
+                for (int x = 0; x < 32; ++x) {
+                  v[2 * x] -= __uint_as_float(o[x] << 16);
+                  v[2 * x + 1] -= __uint_as_float(o[x] & 0xffff0000u);
+                }
               }
               if (rows == 32) turn.tma<false>(o, hy ? &tm.gh_s : &tm.g_s, j.r0 + 128 * half + 64 * u, row0, part);
               else turn.lines<false>(o, reinterpret_cast<char*>(out + (size_t)part * plane + 64 * u), pitch, rows, 2 * cols);
