@@ -1046,7 +1046,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   if (warp == 2) tmem_dealloc_pair(tmem_base, 512);
 }
 
-// Eight rows per block and 128 threads each: the partial sums of its vocabulary and hypertoken tiles, its loss and lse.
+// Sixteen rows per block and 64 threads each: the partial sums of its vocabulary and hypertoken tiles, its loss and lse.
 // With gradients to follow (parts_of_rows > 0) lse also goes to the plan, and the copies of a hidden row without weight are
 // zeroed: they are contracted with g = 0, whatever they hold.
 __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan pl, const float2* part, int part_rows, int parts,
@@ -1054,17 +1054,18 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
                                                     GatherArgs g, int parts_of_rows) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float2 s_ms[8][129];
+  constexpr int kRows = 16, kSlices = 1024 / kRows;
+  __shared__ float2 s_ms[kRows][kSlices + 1];
   // neighbouring threads read neighbouring rows
-  const int x = threadIdx.x & 7, y = threadIdx.x >> 3, p0 = r_lo + blockIdx.x * 8, end = min(pl.head[0], r_hi);
+  const int x = threadIdx.x % kRows, y = threadIdx.x / kRows, p0 = r_lo + blockIdx.x * kRows, end = min(pl.head[0], r_hi);
   float m = -INFINITY, s = 0.f;
   if (p0 + x < end) {
     auto all = [&](const float2* from, size_t stride, int count) {
       constexpr int kAhead = 8;
-      for (int i = y; i < count; i += 128 * kAhead) {
+      for (int i = y; i < count; i += kSlices * kAhead) {
         float2 v[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) v[u] = i + 128 * u < count ? __ldcg(from + (size_t)(i + 128 * u) * stride) : make_float2(-INFINITY, 0.f);
+        for (int u = 0; u < kAhead; ++u) v[u] = i + kSlices * u < count ? __ldcg(from + (size_t)(i + kSlices * u) * stride) : make_float2(-INFINITY, 0.f);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) merge_ms(m, s, v[u].x, v[u].y);
       }
@@ -1079,9 +1080,9 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
   __syncthreads();
   // a warp per row from here on
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, pos = p0 + w;
-  if (w >= 8 || pos >= end) return;
+  if (w >= kRows || pos >= end) return;
   m = s_ms[w][lane].x; s = s_ms[w][lane].y;
-  for (int i = 32; i < 128; i += 32) merge_ms(m, s, s_ms[w][lane + i].x, s_ms[w][lane + i].y);
+  for (int i = 32; i < kSlices; i += 32) merge_ms(m, s, s_ms[w][lane + i].x, s_ms[w][lane + i].y);
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
     const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o);
@@ -1105,49 +1106,61 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
   }
 }
 
-// g from what kKeep has left, in its place: p = exp(m - steps / 2048 - lse), the target's from its own logit.  Blocks take
-// 8192 columns of a row at a time; rows up to the next multiple of 32 become zeros.
+// g from what kKeep has left, in its place: p = exp(m - steps / 2048 - lse), the target's from its own logit.  A block takes
+// 32768 columns of a row, the next vectors under way while it works on the last; rows up to the next multiple of 32 become
+// zeros.
 struct KeptArgs { __nv_bfloat16* g; int pitch; const float2* part; int part_rows, nv; };
-constexpr int kKeptThreads = 256, kKeptVecs = 4, kKeptColumns = 8 * kKeptThreads * kKeptVecs;
+constexpr int kKeptThreads = 256, kKeptVecs = 2, kKeptStep = 8 * kKeptThreads * kKeptVecs, kKeptColumns = 32768;
 // see: columns that the row sees; those behind them up to `cols` become zeros.
 __device__ __forceinline__ void kept_columns(uint16_t* g, int lo, int cols, int see, const float2* part, int part_rows, int nv, const float4& r, int target, float tl) {
   const float lse = r.x, weight = r.y, none = lse - lse;                     // (0, or NaN for a row of NaN)
+  const int hi = min(cols, lo + kKeptColumns), v0 = lo + 8 * (int)threadIdx.x;
   uint4 w[kKeptVecs];
   float from[kKeptVecs];
+  auto load = [&](int v) {
 #pragma unroll
-  for (int u = 0; u < kKeptVecs; ++u) {
-    const int v = lo + 8 * (u * kKeptThreads + (int)threadIdx.x);
-    if (v >= cols) break;
-    w[u] = *reinterpret_cast<const uint4*>(g + v);
-    const int vt = v / nv, half = (v - vt * nv) >> 7;
-    from[u] = (part[(size_t)(2 * vt + half) * part_rows].x - lse) * kLog2e;
-  }
-#pragma unroll
-  for (int u = 0; u < kKeptVecs; ++u) {
-    const int v = lo + 8 * (u * kKeptThreads + (int)threadIdx.x);
-    if (v >= cols) break;
-    const uint32_t in[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
-    float x[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const uint32_t q = k & 1 ? in[k >> 1] >> 16 : in[k >> 1] & 0xffffu;
-      // (a whole number below 2^16 as a float: in the low bits of 2^23, less that)
-      const float steps = __uint_as_float(0x4b000000u | q) - 8388608.f;
-      x[k] = weight * (q == kKeepNone ? none : ex2(fmaf(steps, -kLog2e / kKeepSteps, from[u])));
+    for (int u = 0; u < kKeptVecs; ++u, v += 8 * kKeptThreads) {
+      if (v >= hi) break;
+      w[u] = *reinterpret_cast<const uint4*>(g + v);
+      int slot = v >> 7;                         // half tiles of 128, unless a tile is shorter than 256
+      if (nv != kTile) { const int vt = v / nv; slot = 2 * vt + ((v - vt * nv) >> 7); }
+      from[u] = part[(size_t)slot * part_rows].x;
     }
-    if (weight == 0.f || v + 8 > see) {
+  };
+  load(v0);
+  for (int v = v0; v < hi; v += kKeptStep) {
+    uint4 now[kKeptVecs];
+    float top[kKeptVecs];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) if (weight == 0.f || v + k >= see) x[k] = 0.f;
-    }
-    if (target >= v && target < v + 8 && weight != 0.f) {
-      const float e = weight * (expf(tl - lse) - 1.f);
+    for (int u = 0; u < kKeptVecs; ++u) { now[u] = w[u]; top[u] = (from[u] - lse) * kLog2e; }
+    load(v + kKeptStep);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = v + k == target ? e : x[k];
+    for (int u = 0; u < kKeptVecs; ++u) {
+      const int c = v + u * 8 * kKeptThreads;
+      if (c >= hi) break;
+      const uint32_t in[4] = {now[u].x, now[u].y, now[u].z, now[u].w};
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t q = k & 1 ? in[k >> 1] >> 16 : in[k >> 1] & 0xffffu;
+        // (a whole number below 2^16 as a float: in the low bits of 2^23, less that)
+        const float steps = __uint_as_float(0x4b000000u | q) - 8388608.f;
+        x[k] = weight * (q == kKeepNone ? none : ex2(fmaf(steps, -kLog2e / kKeepSteps, top[u])));
+      }
+      if (weight == 0.f || c + 8 > see) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) if (weight == 0.f || c + k >= see) x[k] = 0.f;
+      }
+      if (target >= c && target < c + 8 && weight != 0.f) {
+        const float e = weight * (expf(tl - lse) - 1.f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = c + k == target ? e : x[k];
+      }
+      *reinterpret_cast<uint4*>(g + c) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
     }
-    *reinterpret_cast<uint4*>(g + v) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
   }
 }
-__global__ void __launch_bounds__(kKeptThreads) k_xent_kept(CbView cb, RowArgs a, Plan pl, KeptArgs w, KeptArgs u, const float* tl, int chunks, int hyper) {
+__global__ void __launch_bounds__(kKeptThreads, 5) k_xent_kept(CbView cb, RowArgs a, Plan pl, KeptArgs w, KeptArgs u, const float* tl, int chunks, int hyper) {
   pdl_wait();
   pdl_trigger();
   const int live = pl.head[0];
@@ -1500,7 +1513,7 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
         if (e != cudaSuccess) return e;
       }
       const int parts = p.part0 + 2 * vocabulary_tiles(p.vn, sh.nv);
-      e = launch_pdl(k_xent_merge, dim3((p.r_hi - p.r_lo + 7) / 8), dim3(1024), 0, s, cb, a, l.pl, l.part, p.part_rows, parts, l.part_h, sh.np, l.tl,
+      e = launch_pdl(k_xent_merge, dim3((p.r_hi - p.r_lo + 15) / 16), dim3(1024), 0, s, cb, a, l.pl, l.part, p.part_rows, parts, l.part_h, sh.np, l.tl,
                      p.r_lo, p.r_hi, g, grad ? sh.parts : 0);
       if (e != cudaSuccess) return e;
     }
@@ -1509,7 +1522,7 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   if (keep) {
     const KeptArgs w{l.g, p.g_pitch, l.part, p.part_rows, sh.nv}, u{l.gh, p.gh_pitch, l.part_h, p.part_rows_h, kTile};
     const int chunks = (pad64(sh.V) + kKeptColumns - 1) / kKeptColumns, hyper = (sh.cap + kKeptColumns - 1) / kKeptColumns;
-    if ((e = launch_pdl(k_xent_kept, dim3(148 * 6), dim3(kKeptThreads), 0, s, cb, a, l.pl, w, u, l.tl, chunks, hyper)) != cudaSuccess) return e;
+    if ((e = launch_pdl(k_xent_kept, dim3(148 * 5), dim3(kKeptThreads), 0, s, cb, a, l.pl, w, u, l.tl, chunks, hyper)) != cudaSuccess) return e;
   }
   p.r_lo = 0; p.r_hi = x.N;
   for (int i = 0; i < sh.pieces; ++i) {
