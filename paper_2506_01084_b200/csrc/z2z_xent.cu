@@ -1010,14 +1010,18 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         const int limit = j.limit - 128 * half;
         if (m < p.d && (some || set)) {
 #pragma unroll
-          for (int x0 = 0; x0 < 128; x0 += 8) {
+          for (int x0 = 0; x0 < 128; x0 += 32) {
             if (x0 >= limit) break;
-            float old[8];
+            if (!set) {
+              float old[32];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) old[x] = !set && x0 + x < limit ? out[(size_t)(x0 + x) * p.d] : 0.f;
+              for (int x = 0; x < 32; ++x) old[x] = x0 + x < limit ? __ldcg(out + (size_t)(x0 + x) * p.d) : 0.f;
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
-              if (x0 + x < limit) out[(size_t)(x0 + x) * p.d] = old[x] + acc[(x0 + x) >> 6][(x0 + x) & 63];
+              for (int x = 0; x < 32; ++x) acc[(x0 + x) >> 6][(x0 + x) & 63] += old[x];
+            }
+#pragma unroll
+            for (int x = 0; x < 32; ++x)
+              if (x0 + x < limit) out[(size_t)(x0 + x) * p.d] = acc[(x0 + x) >> 6][(x0 + x) & 63];
           }
         }
       } else if (some || !p.acc) {
