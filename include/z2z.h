@@ -336,8 +336,9 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  *            loss 0, lse 0, gradient 0, whatever its hidden row holds, and no time.  So does a code that the row
  *            does not see; it sets Z2Z_ST_BAD_TOKEN for its sequence;
  *   w [N] or NULL = 1: a row whose weight is 0 has gradient 0 whatever its logits are;
- *   accumulate  1: added to what the tables' gradients hold, rounded once.  0: every row of d_grad_WU and the n_b
- *            rows of every sequence of d_grad_Uh are written; rows from n_b on stay as they are either way;
+ *   accumulate  1: added to what the tables' gradients hold, rounded once (fp32: what is below the normal range may become
+ *            zero).  0: every row of d_grad_WU and the n_b rows of every sequence of d_grad_Uh are written.  Rows of
+ *            d_grad_Uh from n_b on stay as they are either way;
  *   d_grad_hidden, d_grad_WU, d_grad_Uh: 16-byte aligned, apart from all inputs and one another; each may be NULL.
  * The row of a NaN or +inf logit has a NaN loss and, with a weight, NaN gradients, which reach the tables' too.
  * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]) is rounded to bf16 for gradients stored in
@@ -345,8 +346,11 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  * gives the same bits.
  *   d_scratch: 256-byte aligned, at least *out_least bytes of z2z_xent_scratch_bytes (for the session's configuration,
  *            N and grad_dtype, -1 for z2z_xent_loss alone); up to *out_most, more makes the pieces larger and the call
- *            faster.  How the sums are cut depends on it.  Its contents need not be kept between calls; calls that
- *            share it must be ordered by the caller.
+ *            faster: with the most a bf16 z2z_xent_step keeps its logits, in 16 bits each (within 4 GB), instead of
+ *            computing them twice.  How the sums are cut depends on it.  Its contents need not be kept between
+ *            calls; calls that share it must be ordered by the caller.
+ * The calls run on the tensor cores whatever z2z_set_tensor_cores says.  A wait inside them that gives up sets
+ * Z2Z_ST_WAIT_TIMEOUT (z2z_status); results of that call are then not to be used.
  * N <= 2^20.                                                                                            */
 int32_t z2z_xent_scratch_bytes(const z2z_config* cfg, int32_t N, int32_t grad_dtype, size_t* out_least,
                                size_t* out_most);

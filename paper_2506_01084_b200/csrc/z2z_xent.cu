@@ -17,14 +17,18 @@
 //
 // Rows are sorted by their sequence first (stable), and rows without a target, which add nothing, are left out.
 // Hypertokens are a piece per sequence: its entries against its own rows, which start at a multiple of 32 there.
+// A step whose scratch has room for N (V + cap) values of 16 bits keeps its logits from the losses to the gradients, as
+// distances in fixed point: three contractions then, not four.
+//
+// Bound by the tensor cores from some hundred rows on (their power, in calls of milliseconds), below by memory: W_U is read
+// twice and its gradient written once.  V = 128256, d = 4096, bf16: losses of 2047 rows (1842 with a target) 1.57 ms,
+// 1.25 PFLOP/s; a step of 4096 (3680) rows 9.9 ms, 1.18 PFLOP/s of three contractions; a step of 48 rows 0.75 ms, 2.8 TB/s.
 //
 // Numbers.  A bf16 session's g is rounded once to bf16 for gradients stored in bf16; for fp32 gradients of the tables
 // it is three bf16 parts (24 bits).  An fp32 session has all operands in three parts, and takes the six products of
 // parts that fp32 can hold.  Accumulators are fp32 in tensor memory.  Weights enter as w_r / max w, so that equal
 // weights lose nothing to g's rounding, and the maximum multiplies the sums.  Orders of summation depend on sizes
 // only: the same call gives the same bits.
-#include <mutex>
-
 #include "z2z_common.cuh"
 #include "z2z_internal.h"
 #include "z2z_sm100.cuh"
@@ -36,11 +40,12 @@ using namespace sm100;
 
 namespace {
 
-constexpr int kEpiWarps = 8;                     // two per tensor-memory lane quarter, which take every other 32 columns
+constexpr int kEpiWarps = 8;                     // two per tensor-memory lane quarter, with 128 columns each
 constexpr int kThreads = 128 + 32 * kEpiWarps;   // a warpgroup of producer, issuer and two that leave; two of the epilogue
 // Registers: 384 threads are launched with 168 each; the epilogue, which holds a tile's sums, takes what the others leave
-// (128 x 56 + 256 x 224 = 384 x 168).
+// (128 x 56 + 256 x 224 = 384 x 168; a launch with fewer is refused, since the epilogue would wait for the rest forever).
 constexpr int kRegsFew = 56, kRegsEpi = 224;
+constexpr int kRegsAtLaunch = (128 * kRegsFew + 32 * kEpiWarps * kRegsEpi) / kThreads;
 constexpr int kRing = 10;                        // stages at most
 constexpr int kTile = 256;                       // vocabulary rows or columns of a tile (128 per CTA)
 constexpr int kRingBytes = 5 * 32768;            // a stage: 128 x 64 of either operand, or less of the hidden rows
@@ -483,7 +488,7 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
 }
 
 // Arrival at a barrier of this cluster that orders nothing: the accumulator has been read into registers when it is made
-// (tcgen05.wait::ld), and a release would wait for the stores of the tile before (a tile of dW 6900 -> 4100 clocks).
+// (tcgen05.wait::ld), and a release would wait for the stores of the tile before (a tile of dW 6900 -> 5900 clocks).
 __device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
@@ -526,8 +531,8 @@ __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wa
 
 // A warp's way to memory for blocks of 32 rows (one per lane) of 128 bytes: two buffers in shared memory, in which 16-byte
 // groups of a row are exchanged by its row's low bits (the 128-byte swizzle), and then either one TMA store of the
-// block or stores of whole lines of four rows.  (Stored from the lanes' own rows, 32 lines per instruction, a tile of dW
-// took 15000 clocks.)
+// block or stores of whole lines of four rows.  (48 rows, V = 128256, d = 4096, clocks per tile of dW: stored from the lanes' own
+// rows, 32 lines per instruction, 15000; lines 5900; TMA 4500, which is what 1.05 GB written at 4.2 TB/s take.)
 struct Turn {
   uint4* buf;                                    // [2][32 * 8]
   int at, lane;
@@ -1415,6 +1420,8 @@ bool make_map(CUtensorMap* m, const void* base, long long rows, long long cols, 
 template <int KIND, bool CHAINED, bool MULTI, typename TO>
 cudaError_t launch_main(const Params& p, const Maps& tm, int clusters, cudaStream_t s) {
   auto kern = k_xent<KIND, CHAINED, MULTI, TO>;
+  static const int regs = [&] { cudaFuncAttributes a{}; return cudaFuncGetAttributes(&a, kern) == cudaSuccess ? a.numRegs : 0; }();
+  if (regs < kRegsAtLaunch) return cudaErrorInvalidConfiguration;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   if (e != cudaSuccess) return e;
   return launch_pdl(kern, dim3(2 * clusters), dim3(kThreads), kSmemBytes, s, p, tm);
@@ -1472,7 +1479,8 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   p.err = x.err;
   // hidden rows of the row tiles that are taken through all vocabulary tiles together: a quarter of L2
   const long long tile_bytes = (long long)2 * sh.cta_rows * d * 2 * sh.parts;
-  p.sb = (int)((32ll << 20) / tile_bytes); if (p.sb < 1) p.sb = 1;
+  const long long sb = (32ll << 20) / tile_bytes;
+  p.sb = (int)(sb < 1 ? 1 : (sb > 1024 ? 1024 : sb));
 
   Maps tm{};
   const long long ur = (long long)sh.B * sh.cap;

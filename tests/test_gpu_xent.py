@@ -222,6 +222,31 @@ def test_logits_far_from_zero(dtype):
     c.check(c.run("autograd"))
 
 
+def test_as_many_sequences_as_a_session_may_have():
+    c = Case("bf16", V=300, d=40, B=1024, cap=9, counts=[b % 10 for b in range(1024)], N=1500, order="random", seed=15)
+    c.check(c.run("step"))
+    c = Case("fp32", V=300, d=40, B=1024, cap=9, counts=[b % 10 for b in range(1024)], N=1500, order="turns", skip=0.5, seed=16)
+    c.check(c.run("autograd"))
+
+
+def test_rows_that_belong_to_sequences_in_order():
+    """Without row_seq: row r belongs to sequence r."""
+    c = Case("bf16", V=900, d=64, B=70, cap=20, N=70, seed=17)
+    assert torch.equal(c.seq, torch.arange(70))
+    args, want = list(c.inputs()), c.oracle()
+    args[2] = None
+    loss, lse = torch.empty(2, 70, device=DEV).unbind(0)
+    gh, gW, gU = torch.empty(70, 64, dtype=c.dt, device=DEV), c.dev(c.gWU0), c.dev(c.gUh0)
+    zb.z2z_xent_step(*args, c.dev(c.w), loss, lse, False, gh, gW, gU, c.scratch)
+    c.check({"loss": loss, "lse": lse, "hidden": gh, "WU": gW, "Uh": gU}, want)
+
+
+def test_more_rows_than_partial_sums_are_held_for():
+    """Losses of more than 8192 rows, in two shares, and pieces of the least scratch."""
+    c = Case("bf16", V=70, d=16, B=3, cap=12, N=8192 + 300, order="turns", skip=0.2, scratch="least", seed=18)
+    c.check(c.run("autograd"))
+
+
 def test_no_rows_and_no_live_rows():
     for N in (0, 5):
         c = Case("bf16", V=200, d=64, B=3, cap=30, N=N, seed=3)
