@@ -48,10 +48,12 @@ constexpr int kRegsFew = 56, kRegsEpi = 224;
 constexpr int kRegsAtLaunch = (128 * kRegsFew + 32 * kEpiWarps * kRegsEpi) / kThreads;
 constexpr int kRing = 10;                        // stages at most
 constexpr int kTile = 256;                       // vocabulary rows or columns of a tile (128 per CTA)
-constexpr int kRingBytes = 5 * 32768;            // a stage: 128 x 64 of either operand, or less of the hidden rows
 constexpr int kTurnBytes = 32 * 128;             // a warp's 32 rows of 128 bytes on their way to memory; two of them
 constexpr int kFrontBytes = 1024 + kEpiWarps * 2 * kTurnBytes;     // a multiple of 1024
-constexpr size_t kSmemBytes = 1024 + kFrontBytes + kRingBytes;
+constexpr size_t kSmemBytes = 232448;            // all that a block may have: control block and turns, then the ring
+// A stage: 128 x 64 of either operand, or less of the hidden rows.  (The losses store no tiles.)
+__host__ __device__ constexpr int front_bytes(bool turns) { return turns ? kFrontBytes : 1024; }
+__host__ __device__ constexpr int ring_bytes(bool turns) { return (int)kSmemBytes - 1024 - front_bytes(turns); }
 constexpr int kHyperPad = 32;                    // a sequence's rows start at a multiple of this beside its hypertokens
 constexpr int kLossRows = 8192;                  // rows whose partial sums are held at a time
 constexpr int kMaxParts = 3;                     // bf16 parts of an fp32 value
@@ -647,7 +649,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Ctrl* ctrl = reinterpret_cast<Ctrl*>(sm);
-  const uint32_t stage_base = smem_u32(sm + kFrontBytes);
+  const uint32_t stage_base = smem_u32(sm + front_bytes(KIND != kLoss));
   const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();       // 0: leader (issues the MMAs), 1: peer
   const int C = gridDim.x >> 1, c = blockIdx.x >> 1;
@@ -655,7 +657,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   // An MMA of the logits reads 128 hidden rows from a stage's start; with fewer loaded it reads on, which only feeds rows of
   // the result that nobody looks at.
   const uint32_t b_off = KIND == kProducts ? 16384u : (uint32_t)p.a_bytes, stage_bytes = b_off + 16384u;
-  const int stages = MULTI ? kRingBytes / 16384 : min(kRing, (int)(kRingBytes / stage_bytes));
+  const int stages = min(kRing, (int)(ring_bytes(KIND != kLoss) / (MULTI ? 16384u : stage_bytes)));
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kRing; ++s) { mbar_init(smem_u32(&ctrl->full[s]), 1); mbar_init(smem_u32(&ctrl->empty[s]), 1); }
