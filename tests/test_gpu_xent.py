@@ -59,7 +59,7 @@ class Case:
         self.gWU0, self.gUh0 = ((torch.randn(*s, generator=g) * 0.01).to(self.gt) for s in ((V, d), (B, cap, d)))
         sizes = zb.z2z_xent_scratch_bytes(self.cb.cfg, N, self.gt)
         assert sizes[0] <= sizes[1]
-        size = sizes[0 if scratch == "least" else 1]
+        size = {"least": sizes[0], "between": (sizes[0] + sizes[1]) // 2, "most": sizes[1]}[scratch]
         self.scratch = torch.full((size,), 255, dtype=torch.uint8, device=DEV)         # (NaN wherever it is read as a number)
 
     def dev(self, t, dtype=None):
@@ -150,7 +150,7 @@ def test_an_fp32_session_with_bf16_gradients_of_the_tables():
     c.check(c.run())
 
 
-@pytest.mark.parametrize("scratch", ["least", "most"])
+@pytest.mark.parametrize("scratch", ["least", "between", "most"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_pieces(scratch, dtype):
     """More than one piece of the vocabulary, the last one short."""
@@ -245,6 +245,43 @@ def test_more_rows_than_partial_sums_are_held_for():
     """Losses of more than 8192 rows, in two shares, and pieces of the least scratch."""
     c = Case("bf16", V=70, d=16, B=3, cap=12, N=8192 + 300, order="turns", skip=0.2, scratch="least", seed=18)
     c.check(c.run("autograd"))
+
+
+def test_offsets_that_pass_32_bits():
+    """A table and a gradient of more than 2^31 elements: losses, and the gradients at both ends."""
+    V, d, N = 530000, 4096, 6
+    g = torch.Generator(device=DEV).manual_seed(3)
+    cb = session(V, d, 0, 1, "bf16", [0])
+    W = torch.empty(V, d, dtype=torch.bfloat16, device=DEV)
+    for i in range(0, V, 1 << 16):
+        W[i:i + (1 << 16)] = (torch.randn(min(1 << 16, V - i), d, generator=g, device=DEV) * 0.02).bfloat16()
+    hidden = torch.randn(N, d, generator=g, device=DEV).bfloat16()
+    target = torch.tensor([0, V - 1, V - 2, 1 << 19, 5, V // 2], dtype=torch.int32, device=DEV)
+    seq = torch.zeros(N, dtype=torch.int32, device=DEV)
+    l = torch.cat([hidden.double() @ W[i:i + (1 << 15)].double().T for i in range(0, V, 1 << 15)], 1)
+    lse64, at = torch.logsumexp(l, 1), target.long()
+    g64 = torch.exp(l - lse64[:, None])
+    g64[torch.arange(N), at] -= 1.0
+    loss, lse = torch.empty(2, N, device=DEV).unbind(0)
+    gh, gW = torch.empty_like(hidden), torch.full_like(W, 7.0)
+    scratch = torch.empty(zb.z2z_xent_scratch_bytes(cb.cfg, N, torch.bfloat16)[1], dtype=torch.uint8, device=DEV)
+    zb.z2z_xent_step(cb, hidden, seq, None, W, None, target, None, loss, lse, False, gh, gW, None, scratch)
+    # (bounds of Case.check: a logit's sum of magnitudes is below 130 here, d 0.02 0.8 0.8 and a few deviations)
+    e_l = ((d + 8) * 2 * U32 + 8 * U32) * 130
+    e_lse = e_l + 2 * U32 * float(lse64.abs().max()) + (64 + V / 64) * U32 + 2.0 ** -21
+    assert float((lse.double() - lse64).abs().max()) <= e_lse
+    assert float((loss.double() - (lse64 - l[torch.arange(N), at])).abs().max()) <= 2 * e_lse
+    rel = 2.0 ** -8 + e_l + e_lse + 2.0 ** -20 + 2.0 ** -12 + (N + 16) * 2 * U32
+    for rows in (slice(0, 600), slice((1 << 19) - 300, (1 << 19) + 300), slice(V - 600, V)):
+        want, mag = g64[:, rows].T @ hidden.double(), g64[:, rows].abs().T @ hidden.double().abs()
+        assert bool(((gW[rows].double() - want).abs() <= rel * mag + 1.01 * 2.0 ** -8 * (want.abs() + rel * mag) + 1e-30).all())
+    want, mag = torch.zeros(2, N, d, dtype=torch.float64, device=DEV).unbind(0)
+    for i in range(0, V, 1 << 15):
+        w = W[i:i + (1 << 15)].double()
+        want += g64[:, i:i + (1 << 15)] @ w
+        mag += g64[:, i:i + (1 << 15)].abs() @ w.abs()
+    rel += V * 2 * U32
+    assert bool(((gh.double() - want).abs() <= rel * mag + 1.01 * 2.0 ** -8 * (want.abs() + rel * mag)).all())
 
 
 def test_no_rows_and_no_live_rows():
