@@ -74,6 +74,7 @@ struct Plan {
   int32_t *s0, *h0;          // [B + 1] first position of a sequence's rows, and the one beside its hypertokens
   int32_t *j1, *j2, *j3;     // [B + 1] jobs of the sequences before
   int32_t *perm, *inv;       // position -> row, row -> position or -1
+  int2* place;               // position -> row beside the hypertokens, and zero rows behind it (the last of a sequence)
   float4* meta;              // per position: lse, weight / largest, target and visible hypertokens (bits)
   float* rest;               // and what lse has lost to its rounding, where this call has it
 };
@@ -133,49 +134,60 @@ struct PlanShared {
   int warp_sums[32];
   float wmax;
 };
-constexpr int kPlanThreads = 1024;
-__host__ __device__ constexpr size_t plan_shared_bytes(int B) { return sizeof(PlanShared) + (size_t)B * 8 + (size_t)32 * B * 2; }
+constexpr int kPlanThreads = 1024, kPlanFew = 256;                      // (few: up to 1024 rows of up to 32 sequences)
+__host__ __device__ constexpr size_t plan_shared_bytes(int B) { return sizeof(PlanShared) + (size_t)B * 16 + (size_t)32 * B * 2; }
 
-__global__ void __launch_bounds__(kPlanThreads) k_xent_plan(CbView cb, RowArgs a, Plan pl) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) k_xent_plan(CbView cb, RowArgs a, Plan pl) {
   extern __shared__ unsigned char smem[];
   PlanShared& sh = *reinterpret_cast<PlanShared*>(smem);
   int* s_cnt = reinterpret_cast<int*>(smem + sizeof(PlanShared));       // rows of a sequence, then where its next ones go
-  int* s_n = s_cnt + cb.B;
-  unsigned short* s_warp = reinterpret_cast<unsigned short*>(s_n + cb.B);      // [B][32] rows of a warp
+  int *s_n = s_cnt + cb.B, *s_off = s_n + cb.B, *s_last = s_off + cb.B;        // hypertokens; place beside them less position; last position
+  unsigned short* s_warp = reinterpret_cast<unsigned short*>(s_last + cb.B);   // [B][32] rows of a warp
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // rows of a thread whose loads are under way together; where these are all, they stay in registers
+  constexpr int kBatch = 4, kBatchRows = kBatch * THREADS;
+  int q[kBatch], tgt[kBatch], nv[kBatch];        // sequence, -1 where the row takes no part
+  float w[kBatch], lse[kBatch];
+  auto load = [&](int r0) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int r = r0 + u * THREADS + tid;
+      const bool in = r < a.N;
+      q[u] = in ? (a.row_seq ? a.row_seq[r] : r) : -1;
+      tgt[u] = in ? a.targets[r] : Z2Z_CODE_NONE;
+      nv[u] = in && a.row_nvis ? max(a.row_nvis[r], 0) : 0x7fffffff;
+      w[u] = in && a.weight ? a.weight[r] : 1.f;
+      lse[u] = in && a.lse ? a.lse[r] : 0.f;
+    }
+  };
   pdl_wait();
   pdl_trigger();
-  for (int b = tid; b < cb.B; b += kPlanThreads) { s_cnt[b] = 0; s_n[b] = cb.n[b]; }
-  for (int i = tid; i < 32 * cb.B; i += kPlanThreads) s_warp[i] = 0;
+  load(0);
+  for (int b = tid; b < cb.B; b += THREADS) { s_cnt[b] = 0; s_n[b] = cb.n[b]; }
+  for (int i = tid; i < 32 * cb.B; i += THREADS) s_warp[i] = 0;
   if (tid == 0) sh.wmax = 0.f;
   __syncthreads();
 
-  constexpr int kAhead = 4;                      // rows of a thread whose loads are under way together
+  // whose row it is, if it takes part
+  auto settle = [&](int u) {
+    const int b = q[u];
+    q[u] = -1;
+    if (b < 0 || b >= cb.B || tgt[u] == Z2Z_CODE_NONE) return;
+    nv[u] = min(nv[u], s_n[b]);
+    if (tgt[u] < 0 || tgt[u] >= cb.V + nv[u]) atomicOr(&cb.status[b], Z2Z_ST_BAD_TOKEN);
+    else if (w[u] != 0.f || a.loss_out) q[u] = b;
+  };
   int wbits = 0; bool wnan = false;
-  for (int r0 = tid; r0 < a.N; r0 += kAhead * kPlanThreads) {
-    int seq[kAhead], tgt[kAhead], nv[kAhead]; float w[kAhead];
+  for (int r0 = 0; r0 < a.N; r0 += kBatchRows) {
+    if (r0) load(r0);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int r = r0 + u * kPlanThreads;
-      const bool in = r < a.N;
-      seq[u] = in ? (a.row_seq ? a.row_seq[r] : r) : -1;
-      tgt[u] = in ? a.targets[r] : Z2Z_CODE_NONE;
-      nv[u] = in && a.row_nvis ? a.row_nvis[r] : 0x7fffffff;
-      w[u] = in && a.weight ? a.weight[r] : 1.f;
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int r = r0 + u * kPlanThreads;
-      if (r >= a.N) continue;
-      int b = -1;
-      if (seq[u] >= 0 && seq[u] < cb.B && tgt[u] != Z2Z_CODE_NONE) {
-        const int n = min(max(nv[u], 0), s_n[seq[u]]);
-        if (tgt[u] < 0 || tgt[u] >= cb.V + n) atomicOr(&cb.status[seq[u]], Z2Z_ST_BAD_TOKEN);
-        else if (w[u] != 0.f || a.loss_out) b = seq[u];
-      }
-      pl.inv[r] = b;                             // (read again below by the same thread)
-      if (b >= 0) {
-        atomicAdd(&s_cnt[b], 1);
+    for (int u = 0; u < kBatch; ++u) {
+      const int r = r0 + u * THREADS + tid;
+      if (r >= a.N) { q[u] = -1; continue; }
+      settle(u);
+      if (q[u] >= 0) {
+        atomicAdd(&s_cnt[q[u]], 1);
         const float x = fabsf(w[u]);
         if (x != x) wnan = true;
         wbits = max(wbits, __float_as_int(x));
@@ -197,47 +209,68 @@ __global__ void __launch_bounds__(kPlanThreads) k_xent_plan(CbView cb, RowArgs a
   const int rt = ceil_div(c, a.th), kt = ceil_div(n, kTile);
   const int v[5] = {c, ceil_div(c, kHyperPad) * kHyperPad, rt * kt, a.hidden && n ? rt * a.dt : 0, a.tables ? kt * a.dt : 0};
   int32_t* const out[5] = {pl.s0, pl.h0, pl.j1, pl.j2, pl.j3};
-  int first = 0;
+  int x[5] = {0, 0, 0, 0, 0}, total[5];
+  if (THREADS < 1024 || cb.B <= 32) {
+    if (warp == 0) {
 #pragma unroll
-  for (int i = 0; i < 5; ++i) {
-    int total;
-    const int x = block_scan_1024(v[i], sh.warp_sums, total);
-    if (b < cb.B) out[i][b] = x;
-    if (tid == 0) {
-      out[i][cb.B] = total;
-      if (i == 0) pl.head[0] = total;
-      if (i >= 2) pl.head[i - 1] = total;
+      for (int i = 0; i < 5; ++i) {
+        x[i] = v[i];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x[i], o); if (lane >= o) x[i] += y; }
+        total[i] = __shfl_sync(0xffffffffu, x[i], 31);
+        x[i] -= v[i];
+      }
     }
-    if (i == 0) first = x;
+  } else if constexpr (THREADS == 1024) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) x[i] = block_scan_1024(v[i], sh.warp_sums, total[i]);
+    __syncthreads();
   }
-  if (b < cb.B) { pl.cnt[b] = c; s_cnt[b] = first; }
-  if (tid == 0) pl.head[4] = __float_as_int(wmax);
+  if (b < cb.B) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) out[i][b] = x[i];
+    pl.cnt[b] = c;
+    s_cnt[b] = x[0]; s_off[b] = x[1] - x[0]; s_last[b] = x[0] + c - 1;
+  }
+  if (tid == 0) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) out[i][cb.B] = total[i];
+    pl.head[0] = total[0]; pl.head[1] = total[2]; pl.head[2] = total[3]; pl.head[3] = total[4]; pl.head[4] = __float_as_int(wmax);
+  }
   __syncthreads();
 
-  // Places, 1024 rows at a time: rows of the same sequence in a warp by votes, the warps of a sequence one after another.
-  for (int r0 = 0; r0 < a.N; r0 += kPlanThreads) {
-    const int r = r0 + tid, q = r < a.N ? pl.inv[r] : -1;
-    float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (q >= 0) {
-      int nv = s_n[q];
-      if (a.row_nvis) nv = min(max(a.row_nvis[r], 0), nv);
-      const float x = a.weight ? a.weight[r] : 1.f;
-      m = make_float4(a.lse ? a.lse[r] : 0.f, x == 0.f ? 0.f : x / wmax, __int_as_float(a.targets[r]), __int_as_float(nv));
+  // Places, a row per thread at a time: rows of the same sequence in a warp by votes, the warps of a sequence one after another.
+  for (int r0 = 0; r0 < a.N; r0 += kBatchRows) {
+    if (a.N > kBatchRows) {
+      load(r0);
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) settle(u);
     }
-    const unsigned same = __match_any_sync(0xffffffffu, q);
-    const int rank = __popc(same & ((1u << lane) - 1u));
-    if (q >= 0 && rank == 0) s_warp[q * 32 + warp] = (unsigned short)__popc(same);
-    __syncthreads();
-    int at = -1;
-    if (q >= 0) {
-      at = s_cnt[q] + rank;
-      for (int i = 0; i < warp; ++i) at += s_warp[q * 32 + i];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (r0 + u * THREADS >= a.N) break;
+      const int r = r0 + u * THREADS + tid;
+      const unsigned same = __match_any_sync(0xffffffffu, q[u]);
+      const int rank = __popc(same & ((1u << lane) - 1u));
+      if (q[u] >= 0 && rank == 0) s_warp[q[u] * 32 + warp] = (unsigned short)__popc(same);
+      __syncthreads();
+      int at = -1;
+      if (q[u] >= 0) {
+        at = s_cnt[q[u]] + rank;
+        for (int i = 0; i < warp; ++i) at += s_warp[q[u] * 32 + i];
+      }
+      __syncthreads();
+      if (q[u] >= 0 && rank == 0) { atomicAdd(&s_cnt[q[u]], (int)s_warp[q[u] * 32 + warp]); s_warp[q[u] * 32 + warp] = 0; }
+      if (r < a.N) pl.inv[r] = at;
+      if (at >= 0) {
+        const int h = at + s_off[q[u]];
+        pl.perm[at] = r;
+        pl.place[at] = make_int2(h, at == s_last[q[u]] ? -(h + 1) & (kHyperPad - 1) : 0);
+        pl.meta[at] = make_float4(lse[u], w[u] == 0.f ? 0.f : w[u] / wmax, __int_as_float(tgt[u]), __int_as_float(nv[u]));
+        pl.rest[at] = 0.f;
+      }
+      __syncthreads();
     }
-    __syncthreads();
-    if (q >= 0 && rank == 0) { atomicAdd(&s_cnt[q], (int)s_warp[q * 32 + warp]); s_warp[q * 32 + warp] = 0; }
-    if (r < a.N) pl.inv[r] = at;
-    if (at >= 0) { pl.perm[at] = r; pl.meta[at] = m; pl.rest[at] = 0.f; }
-    __syncthreads();
   }
 }
 
@@ -302,16 +335,15 @@ __global__ void __launch_bounds__(128) k_xent_gather(CbView cb, RowArgs a, Plan 
   pdl_trigger();
   const int tid = threadIdx.x, d = g.d;
   if ((int)blockIdx.x < g.positions) {
-    const int p = blockIdx.x, live = pl.head[0];
+    const int p = blockIdx.x, at = pl.perm[p], live = pl.head[0];
+    const int2 place = pl.place[p];
     if (p >= ceil_div(live, kTile) * kTile) return;
-    const int row = p < live ? pl.perm[p] : -1;
+    const int row = p < live ? at : -1;
     const T* src = row >= 0 ? reinterpret_cast<const T*>(g.hidden) + (size_t)row * d : nullptr;
     put_row(src, g.hs + (size_t)p * d, g.hs_plane, d, tid, blockDim.x);
     if (g.hh && row >= 0) {
-      const int b = a.row_seq ? a.row_seq[row] : row, h = pl.h0[b] + p - pl.s0[b];
-      put_row(src, g.hh + (size_t)h * d, g.hh_plane, d, tid, blockDim.x);
-      if (p + 1 == pl.s0[b + 1])
-        for (int i = h + 1; i < pl.h0[b + 1]; ++i) put_row<T>(nullptr, g.hh + (size_t)i * d, g.hh_plane, d, tid, blockDim.x);
+      put_row(src, g.hh + (size_t)place.x * d, g.hh_plane, d, tid, blockDim.x);
+      for (int i = 1; i <= place.y; ++i) put_row<T>(nullptr, g.hh + (size_t)(place.x + i) * d, g.hh_plane, d, tid, blockDim.x);
     }
     return;
   }
@@ -1082,10 +1114,8 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
       }
     };
     all(part + p0 + x - r_lo, part_rows, parts);
-    if (cb.cap > 0) {
-      const int row = pl.perm[p0 + x], b = a.row_seq ? a.row_seq[row] : row;
-      all(part_h + p0 + x, part_rows_h, 2 * ceil_div(cb.n[b], kTile));
-    }
+    // (tiles beyond what the row sees have nothing for it)
+    if (cb.cap > 0) all(part_h + p0 + x, part_rows_h, 2 * ceil_div(__float_as_int(pl.meta[p0 + x].w), kTile));
   }
   s_ms[x][y] = make_float2(m, s);
   __syncthreads();
@@ -1109,7 +1139,7 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
     if (parts_of_rows) { pl.meta[pos].x = m + ls; pl.rest[pos] = m == INFINITY ? 0.f : (m - (m + ls)) + ls; }
   }
   if (parts_of_rows && pl.meta[pos].y == 0.f) {
-    const int b = a.row_seq ? a.row_seq[row] : row, h = pl.h0[b] + pos - pl.s0[b];
+    const int h = pl.place[pos].x;
     for (int i = 0; i < parts_of_rows; ++i) {
       put_row<__nv_bfloat16>(nullptr, g.hs + (size_t)i * g.hs_plane + (size_t)pos * g.d, 0, g.d, lane, 32);
       if (g.hh) put_row<__nv_bfloat16>(nullptr, g.hh + (size_t)i * g.hh_plane + (size_t)h * g.d, 0, g.d, lane, 32);
@@ -1190,24 +1220,22 @@ __global__ void __launch_bounds__(kKeptThreads, 5) k_xent_kept(CbView cb, RowArg
     // hypertokens, and the zeros up to the sequence's next multiple of 32
     const int row = pl.perm[pos], b = a.row_seq ? a.row_seq[row] : row, n = pad32(cb.n[b]), lo = (chunk - chunks) * kKeptColumns;
     if (lo >= n) continue;
-    const int h = pl.h0[b] + pos - pl.s0[b];
-    kept_columns(reinterpret_cast<uint16_t*>(u.g) + (size_t)h * u.pitch, lo, n, __float_as_int(r.w), u.part + pos, u.part_rows, u.nv, r, target - cb.V, t);
-    if (pos + 1 == pl.s0[b + 1])
-      for (int k = h + 1; k < pl.h0[b + 1]; ++k)
-        for (int v = lo + threadIdx.x * 8; v < min(n, lo + kKeptColumns); v += kKeptThreads * 8)
-          *reinterpret_cast<uint4*>(u.g + (size_t)k * u.pitch + v) = make_uint4(0u, 0u, 0u, 0u);
+    const int2 place = pl.place[pos];
+    kept_columns(reinterpret_cast<uint16_t*>(u.g) + (size_t)place.x * u.pitch, lo, n, __float_as_int(r.w), u.part + pos, u.part_rows, u.nv, r, target - cb.V, t);
+    for (int k = 1; k <= place.y; ++k)
+      for (int v = lo + threadIdx.x * 8; v < min(n, lo + kKeptColumns); v += kKeptThreads * 8)
+        *reinterpret_cast<uint4*>(u.g + (size_t)(place.x + k) * u.pitch + v) = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 
 // dh of a row: its partial sums, those of the vocabulary's parts first, times the largest weight.
 template <typename T>
-__global__ void __launch_bounds__(128) k_xent_hidden(CbView cb, RowArgs a, Plan pl, const float* dh, long long slot, int split, T* out, int d) {
+__global__ void __launch_bounds__(128) k_xent_hidden(Plan pl, const float* dh, long long slot, int split, T* out, int d) {
   pdl_wait();
   pdl_trigger();
   const int r = blockIdx.x, pos = pl.inv[r], i = (blockIdx.y * 128 + threadIdx.x) * 8;
   if (i >= d) return;
-  int slots = 0;
-  if (pos >= 0) { const int b = a.row_seq ? a.row_seq[r] : r; slots = split + (cb.n[b] > 0 ? 1 : 0); }
+  const int slots = pos < 0 ? 0 : split + (__float_as_int(pl.meta[pos].w) > 0 ? 1 : 0);       // (the last: hypertokens, if it sees any)
   float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const float* from = dh + (size_t)(pos < 0 ? 0 : pos) * d + i;
   constexpr int kAhead = 4;
@@ -1340,6 +1368,7 @@ Layout layout_of(const Shape& s, char* base) {
   int32_t** tables[] = {&l.pl.s0, &l.pl.h0, &l.pl.j1, &l.pl.j2, &l.pl.j3};
   for (int32_t** t : tables) *t = (int32_t*)take((size_t)(s.B + 1) * 4);
   l.pl.perm = (int32_t*)take((size_t)s.np * 4); l.pl.inv = (int32_t*)take((size_t)s.np * 4);
+  l.pl.place = (int2*)take((size_t)s.np * 8);
   l.pl.meta = (float4*)take((size_t)s.np * 16); l.pl.rest = (float*)take((size_t)s.np * 4);
   l.hs = (__nv_bfloat16*)take(row * s.np);
   if (s.cap > 0) {
@@ -1451,9 +1480,11 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   if (grad) { a.weight = x.weight; a.hidden = x.g_hidden != nullptr; a.tables = x.g_Uh != nullptr; }
   if (loss) { a.loss_out = x.loss; a.lse_out = x.lse; }
   else a.lse = x.lse;
-  cudaError_t e = cudaFuncSetAttribute(k_xent_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan_shared_bytes(1024));
+  cudaError_t e = cudaFuncSetAttribute(k_xent_plan<kPlanThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan_shared_bytes(1024));
   if (e != cudaSuccess) return e;
-  if ((e = launch_pdl(k_xent_plan, dim3(1), dim3(kPlanThreads), plan_shared_bytes(sh.B), s, cb, a, l.pl)) != cudaSuccess) return e;
+  e = sh.N <= 4 * kPlanFew && sh.B <= 32 ? launch_pdl(k_xent_plan<kPlanFew>, dim3(1), dim3(kPlanFew), plan_shared_bytes(sh.B), s, cb, a, l.pl)
+                                         : launch_pdl(k_xent_plan<kPlanThreads>, dim3(1), dim3(kPlanThreads), plan_shared_bytes(sh.B), s, cb, a, l.pl);
+  if (e != cudaSuccess) return e;
   GatherArgs g{};
   g.hidden = x.hidden; g.Uh = x.Uh; g.d = d; g.positions = sh.np;
   g.hs = l.hs; g.hs_plane = (long long)sh.np * d;
@@ -1552,8 +1583,8 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   }
   if (!x.g_hidden) return cudaSuccess;
   return sh.dtype == Z2Z_DTYPE_FP32
-             ? launch_pdl(k_xent_hidden<float>, dim3(x.N, (d + 1023) / 1024), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<float*>(x.g_hidden), d)
-             : launch_pdl(k_xent_hidden<__nv_bfloat16>, dim3(x.N, (d + 1023) / 1024), dim3(128), 0, s, cb, a, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<__nv_bfloat16*>(x.g_hidden), d);
+             ? launch_pdl(k_xent_hidden<float>, dim3(x.N, (d + 1023) / 1024), dim3(128), 0, s, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<float*>(x.g_hidden), d)
+             : launch_pdl(k_xent_hidden<__nv_bfloat16>, dim3(x.N, (d + 1023) / 1024), dim3(128), 0, s, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<__nv_bfloat16*>(x.g_hidden), d);
 }
 
 }  // namespace
