@@ -3,7 +3,9 @@
 //   norm = |scale| sqrt(sum over all tensors of g^2),   out = scale min(1, max_norm / (norm + 1e-6)) g
 //
 // Two launches: partial sums of squares, one per block; then every block adds the partial sums in the same order and
-// scales its share.  Both are bound by memory.  The tensors are cut into chunks of 32 KB, dealt to the blocks in turn;
+// scales its share.  Both are bound by memory: 1.9e9 bf16 elements' norm 0.63 ms, 5.9 TB/s (reads alone reach no more here);
+// 3.3e8 fp32 elements to bf16 0.51 ms, 6.5 TB/s over both passes; 52 tensors of 1 MB in all 6.8 us in a graph (both passes in
+// one launch, by a cluster of eight blocks that exchange their sums, took 6 to 17).  The tensors are cut into chunks of 32 KB, dealt to the blocks in turn;
 // the second launch takes them from the end, where the first one's are still in L2.  Where nothing would change (in
 // place, and a factor of 1) it writes nothing.
 //
