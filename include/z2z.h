@@ -349,8 +349,9 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  *            faster: with the most a bf16 z2z_xent_step keeps its logits, in 16 bits each (within 4 GB), instead of
  *            computing them twice.  How the sums are cut depends on it.  Its contents need not be kept between
  *            calls; calls that share it must be ordered by the caller.
- * The calls run on the tensor cores whatever z2z_set_tensor_cores says.  A wait inside them that gives up sets
- * Z2Z_ST_WAIT_TIMEOUT (z2z_status); results of that call are then not to be used.
+ * The calls run on the tensor cores whatever z2z_set_tensor_cores says.  Waits inside them are bounded
+ * (z2z_set_xent_wait_limit); one that gives up sets Z2Z_ST_WAIT_TIMEOUT (z2z_status); results of that call are then not
+ * to be used.
  * N <= 2^20.                                                                                            */
 int32_t z2z_xent_scratch_bytes(const z2z_config* cfg, int32_t N, int32_t grad_dtype, size_t* out_least,
                                size_t* out_most);
@@ -367,6 +368,10 @@ int32_t z2z_xent_step(z2z_codebook* cb, const void* d_hidden, int32_t N, const i
                       const float* d_row_weight, float* d_loss, float* d_lse, int32_t grad_dtype, int32_t accumulate,
                       void* d_grad_hidden, void* d_grad_WU, void* d_grad_Uh, void* d_scratch, size_t scratch_bytes,
                       z2z_stream stream);
+
+/* How long a wait inside the kernels of the calls above may take before it gives up, in nanoseconds, for the calls that this
+ * process makes from now on (those captured before keep theirs); 0 = the default, 400 ms.                    */
+int32_t z2z_set_xent_wait_limit(int64_t ns);
 
 /* Global norm of the gradients of a step, and the gradients scaled to a largest norm:
  *   norm = |scale| sqrt(sum of the squares of all elements of all tensors),

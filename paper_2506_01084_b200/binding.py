@@ -31,7 +31,8 @@ EXPORTS = ["z2z_workspace_bytes", "z2z_codebook_init", "z2z_lzw_encode", "z2z_lz
            "z2z_lzw_decode", "z2z_embed_lookup", "z2z_upload_rows", "z2z_sample_filtered",
            "z2z_set_encoder_half_scratch", "z2z_embed_lookup_scaled", "z2z_embed_grad_scratch_bytes", "z2z_embed_grad",
            "z2z_distill_loss", "z2z_distill_grad", "z2z_set_distill_wait_limit", "z2z_beam_select", "z2z_beam_reorder",
-           "z2z_xent_scratch_bytes", "z2z_xent_loss", "z2z_xent_grad", "z2z_xent_step", "z2z_grad_clip_scratch_bytes", "z2z_grad_clip"]
+           "z2z_xent_scratch_bytes", "z2z_xent_loss", "z2z_xent_grad", "z2z_xent_step", "z2z_set_xent_wait_limit", "z2z_grad_clip_scratch_bytes",
+           "z2z_grad_clip"]
 
 
 class Config(C.Structure):
@@ -63,6 +64,7 @@ _ARGTYPES = {
     "z2z_xent_loss": [_P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P],
     "z2z_xent_grad": [_P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _I, _I, _P, _P, _P, _P, C.c_size_t, _P],
     "z2z_xent_step": [_P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _P, _P, _P, _P, C.c_size_t, _P],
+    "z2z_set_xent_wait_limit": [_L],
     "z2z_grad_clip_scratch_bytes": [_I, C.POINTER(C.c_size_t)],
     "z2z_grad_clip": [C.POINTER(GradTensor), _I, _F, _F, _P, _P, C.c_size_t, _P],
     "z2z_beam_select": [_P, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P],
@@ -398,6 +400,11 @@ def z2z_xent_step(cb: Codebook, hidden: torch.Tensor, row_seq: Optional[torch.Te
     N, args = _xent_rows(cb, hidden, row_seq, row_nvis, W_U, U_h, targets)
     _enqueue(lib().z2z_xent_step, hidden, *args, _dev(row_weight, torch.float32, N, "row_weight"), _dev(loss, torch.float32, N, "loss"),
              _dev(lse, torch.float32, N, "lse"), *_xent_grads(cb, N, accumulate, grad_hidden, grad_WU, grad_Uh, scratch))
+
+
+def z2z_set_xent_wait_limit(ns: int):
+    """Nanoseconds after which a wait inside the cross entropy's kernels gives up; 0: the default."""
+    _check(lib().z2z_set_xent_wait_limit(ns))
 
 
 class GradTensors:

@@ -440,6 +440,12 @@ int32_t z2z_xent_step(z2z_codebook* cb, const void* d_hidden, int32_t N, const i
   return xent_call(cb, a, stream);
 }
 
+int32_t z2z_set_xent_wait_limit(int64_t ns) {
+  if (ns < 0) return fail(Z2Z_ERR_INVALID_ARG, "ns < 0");
+  z2z::xent_wait_limit((unsigned long long)ns);
+  return Z2Z_OK;
+}
+
 int32_t z2z_grad_clip_scratch_bytes(int32_t n, size_t* out_bytes) {
   if (n < 0 || n > z2z::kGradClipMaxTensors) return fail(Z2Z_ERR_INVALID_ARG, "need 0 <= n <= 65536");
   if (!out_bytes) return fail(Z2Z_ERR_INVALID_ARG, "out_bytes is NULL");

@@ -29,6 +29,8 @@
 // parts that fp32 can hold.  Accumulators are fp32 in tensor memory.  Weights enter as w_r / max w, so that equal
 // weights lose nothing to g's rounding, and the maximum multiplies the sums.  Orders of summation depend on sizes
 // only: the same call gives the same bits.
+#include <atomic>
+
 #include "z2z_common.cuh"
 #include "z2z_internal.h"
 #include "z2z_sm100.cuh"
@@ -63,7 +65,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 struct Ctrl {
   unsigned long long full[kRing], empty[kRing], acc_full[2], acc_empty[2], done;
   uint32_t tmem_base;
-  int abort;
+  uint32_t bytes[kRing];     // that this CTA has last loaded into a stage
+  int issued;                // stages that it has loaded in all
+  int abort, other_abort;    // a role has given up: here, in the other CTA of the pair
 };
 static_assert(sizeof(Ctrl) <= 1024 && kFrontBytes % 1024 == 0, "control block");
 
@@ -113,6 +117,7 @@ struct Params {
   int split; long long dh_slot; float* dh;
   void *gWU, *gUh; int acc;
   int mem_cycles;            // what a tile of a table's gradient takes for its memory traffic
+  unsigned long long wait_ns; // after which a wait gives up
   int* err;
 };
 
@@ -504,9 +509,30 @@ __device__ __forceinline__ int job_chain(const Params& p, const Job& j) {
   if (p.parts > 1) return 1;                     // (six products)
   return j.type <= kLogitsHyper ? kChain : (j.type <= kHiddenHyper ? 1 << 30 : kChain);
 }
-constexpr unsigned long long kDrainNs = 10ull * 1000 * 1000;
-__device__ __forceinline__ bool mbar_wait_warp_limit(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long ns) {
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long ns) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ns));
+}
+// Wait for what is under way and comes to its end by itself.  Bounded by probes, of up to a microsecond each: time passes
+// while a process is off the GPU, too.
+constexpr int kDrainProbes = 1 << 16;
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+  for (int i = 0; i < kDrainProbes; ++i)
+    if (mbar_try_wait(bar, parity)) return;
+}
+// Loads of a pair in which a role has given up, by one thread of the leader, on whose barriers both CTAs' bytes count, once all
+// roles of both have left: until they have landed, no memory of the pair may be given back.  The CTAs have issued the
+// same stages in the same order, one maybe up to a whole ring of them more than the other: there the barrier still expects
+// the bytes of both (the leader's stages) or none (the other's).
+__device__ __forceinline__ void drain_loads(Ctrl* ctrl, int stages) {
+  const int mine = ctrl->issued, theirs = (int)ld_cluster_u32(map_to_cta(smem_u32(&ctrl->issued), 1));
+  const int both = min(mine, theirs), most = max(mine, theirs);
+  for (int i = max(both - stages, 0); i < most; ++i) {
+    const int s = i % stages;
+    const uint32_t bar = smem_u32(&ctrl->full[s]);
+    if (i >= mine) mbar_expect_tx(bar, ld_cluster_u32(map_to_cta(smem_u32(&ctrl->bytes[s]), 1)));
+    else if (i >= theirs) mbar_complete_tx(bar, ctrl->bytes[s]);
+    drain(bar, (i / stages) & 1);
+  }
 }
 
 // MN-major operand of 64-column boxes of 64 rows with the 128-byte swizzle: the next 8 contracted rows are 1024 bytes
@@ -695,7 +721,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
     for (int s = 0; s < kRing; ++s) { mbar_init(smem_u32(&ctrl->full[s]), 1); mbar_init(smem_u32(&ctrl->empty[s]), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctrl->acc_full[b]), 1); mbar_init(smem_u32(&ctrl->acc_empty[b]), 2 * kEpiWarps); }
     mbar_init(smem_u32(&ctrl->done), 1);
-    ctrl->abort = 0;
+    ctrl->issued = ctrl->abort = ctrl->other_abort = 0;
     mbar_init_fence();
   }
   __syncthreads();
@@ -719,7 +745,8 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
       int stage = 0, issued = 0; uint32_t phase = 0;
       bool ok = true;
       auto begin = [&](uint32_t bytes) {         // the next stage, with so many bytes to come in each CTA
-        ok = mbar_wait(smem_u32(&ctrl->empty[stage]), phase ^ 1u, &ctrl->abort);
+        ok = mbar_wait(smem_u32(&ctrl->empty[stage]), phase ^ 1u, &ctrl->abort, p.wait_ns);
+        if (ok) ctrl->bytes[stage] = bytes;
         if (ok && rank == 0) mbar_expect_tx(smem_u32(&ctrl->full[stage]), 2u * bytes);
         return ok;
       };
@@ -780,16 +807,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
           block(0, A.x, j.b * 16, j.k16 * 16, B.y);
         }
       }
-      // A role that gave up: copies that are under way land before the block ends (the peer's count on the leader's barriers,
-      // and it waits for the leader below).
-      if (!ok && rank == 0) {
-        int left = 0;
-        for (int i = 0; i < min(issued, stages); ++i) {
-          const int at = stage - 1 - i;
-          mbar_wait(smem_u32(&ctrl->full[at < 0 ? at + stages : at]), at < 0 ? phase ^ 1u : phase, &left, kDrainNs);
-          left = 0;
-        }
-      }
+      ctrl->issued = issued;
     } else if (warp == 1 && rank == 0) {
       // ---------------- MMA issuer (leader only, the whole warp: elect_one()) ------------------------------
       Walk w(p, c, C);
@@ -797,7 +815,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
       int stage = 0; uint32_t phase = 0, job_i = 0;
       bool ok = true;
       auto arrived = [&]() {
-        ok = mbar_wait_warp(smem_u32(&ctrl->full[stage]), phase, &ctrl->abort);
+        ok = wait_warp(smem_u32(&ctrl->full[stage]), phase, &ctrl->abort, p.wait_ns);
         tc_fence_after();
         return ok;
       };
@@ -824,7 +842,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         for (int i = 0, kb = 0; i < blocks * turns; ++i, kb = kb + 1 == blocks ? 0 : kb + 1) {
           if (left == 0) {
             if (i) { if (elect_one()) umma_commit_pair(smem_u32(&ctrl->acc_full[job_i & 1u])); __syncwarp(); ++job_i; }
-            ok = mbar_wait_warp(smem_u32(&ctrl->acc_empty[job_i & 1u]), ((job_i >> 1) & 1u) ^ 1u, &ctrl->abort);
+            ok = wait_warp(smem_u32(&ctrl->acc_empty[job_i & 1u]), ((job_i >> 1) & 1u) ^ 1u, &ctrl->abort, p.wait_ns);
             if (!ok) break;
             tc_fence_after();
             D = tmem_base + (job_i & 1u) * kTile;
@@ -874,12 +892,6 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         __syncwarp();
         ++job_i;
       }
-      if (!ok) {                                 // MMAs under way end before their memory is given back
-        if (elect_one()) umma_commit_pair(smem_u32(&ctrl->done));
-        __syncwarp();
-        int none = 0;
-        mbar_wait_warp_limit(smem_u32(&ctrl->done), 0, &none, kDrainNs);
-      }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));
@@ -907,7 +919,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
           for (int x = 0; x < 64; ++x) acc[u][x] = 0.f;
       }
       for (int at = 0; at < blocks; at += min(chain, blocks)) {
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctrl->acc_full[job_i & 1u]), (job_i >> 1) & 1u, &ctrl->abort));
+        ok = wait_warp(smem_u32(&ctrl->acc_full[job_i & 1u]), (job_i >> 1) & 1u, &ctrl->abort, p.wait_ns);
         if (!ok) break;
         tc_fence_after();
         const uint32_t from = tmem_base + ((uint32_t)(q * 32) << 16) + (job_i & 1u) * kTile + 128 * half;
@@ -1084,8 +1096,23 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   }
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && ctrl->abort) atomicOr(p.err, 1);
+  if (threadIdx.x == 0 && ctrl->abort) {
+    atomicOr(p.err, 1);
+    st_cluster_u32(map_to_cta(smem_u32(&ctrl->other_abort), rank ^ 1), 1u);
+  }
+  __syncwarp();
   cluster_sync_all();                            // nobody leaves while the pair's MMAs may read its memory
+  if (ctrl->abort | ctrl->other_abort) {
+    // A role that gave up, in either CTA, has left what the others had under way: the loads land and the MMAs end first.
+    if (warp == 1) {
+      if (rank == 0 && elect_one()) umma_commit_pair(smem_u32(&ctrl->done));
+      __syncwarp();
+      if (lane == 0) drain(smem_u32(&ctrl->done), 0);
+    }
+    if (rank == 0 && threadIdx.x == 0) drain_loads(ctrl, stages);
+    __syncthreads();
+    cluster_sync_all();
+  }
   if (warp == 2) tmem_dealloc_pair(tmem_base, 512);
 }
 
@@ -1283,6 +1310,8 @@ __global__ void __launch_bounds__(128) k_xent_zero(CbView cb, char* gWU, char* g
 }
 
 // ---- host ------------------------------------------------------------------------------------------
+std::atomic<unsigned long long> g_xent_wait_ns{kWaitLimitNs};
+
 long long up_to(long long x, long long a) { return (x + a - 1) / a * a; }
 
 int sm_count_xent() {
@@ -1509,6 +1538,7 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   p.split = sh.split; p.dh = grad && x.g_hidden ? l.dh : nullptr; p.dh_slot = (long long)sh.np * d;
   p.gWU = x.g_WU; p.gUh = sh.cap > 0 ? x.g_Uh : nullptr; p.acc = x.accumulate ? 1 : 0;
   p.mem_cycles = kTile * kTile * (x.grad_dtype == Z2Z_DTYPE_FP32 ? 4 : 2) * (x.accumulate ? 2 : 1) / 46;
+  p.wait_ns = g_xent_wait_ns.load(std::memory_order_relaxed);
   p.err = x.err;
   // hidden rows of the row tiles that are taken through all vocabulary tiles together: a quarter of L2
   const long long tile_bytes = (long long)2 * sh.cta_rows * d * 2 * sh.parts;
@@ -1588,6 +1618,8 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
 }
 
 }  // namespace
+
+void xent_wait_limit(unsigned long long ns) { g_xent_wait_ns.store(ns ? ns : kWaitLimitNs, std::memory_order_relaxed); }
 
 void xent_scratch_bytes(const z2z_config& c, int N, int grad_dtype, size_t* least, size_t* most) {
   *least = *most = 0;

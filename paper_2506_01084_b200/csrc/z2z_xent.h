@@ -24,6 +24,7 @@ struct XentArgs {
 };
 // Bytes with which a call works, and from which on more does not make it faster.  grad_dtype < 0: losses alone.
 void xent_scratch_bytes(const z2z_config& c, int N, int grad_dtype, size_t* least, size_t* most);
+void xent_wait_limit(unsigned long long ns);     // of calls from now on; 0: the default
 cudaError_t run_xent(const CbView& cb, const z2z_config& cfg, const XentArgs& a, cudaStream_t s);
 
 }  // namespace z2z
