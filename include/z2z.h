@@ -350,8 +350,8 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  *            computing them twice.  How the sums are cut depends on it.  Its contents need not be kept between
  *            calls; calls that share it must be ordered by the caller.
  * The calls run on the tensor cores whatever z2z_set_tensor_cores says.  Waits inside them are bounded
- * (z2z_set_xent_wait_limit); one that gives up sets Z2Z_ST_WAIT_TIMEOUT (z2z_status); results of that call are then not
- * to be used.
+ * (z2z_set_xent_wait_limit); one that gives up sets Z2Z_ST_WAIT_TIMEOUT (z2z_status) and leaves NaN in every result that
+ * lacks something: the losses of rows whose logits did not come, and the gradients that depend on them.
  * N <= 2^20.                                                                                            */
 int32_t z2z_xent_scratch_bytes(const z2z_config* cfg, int32_t N, int32_t grad_dtype, size_t* out_least,
                                size_t* out_most);

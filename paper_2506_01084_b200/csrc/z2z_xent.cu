@@ -918,7 +918,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
 #pragma unroll
           for (int x = 0; x < 64; ++x) acc[u][x] = 0.f;
       }
-      for (int at = 0; at < blocks; at += min(chain, blocks)) {
+      for (int at = ok ? 0 : blocks; at < blocks; at += min(chain, blocks)) {
         ok = wait_warp(smem_u32(&ctrl->acc_full[job_i & 1u]), (job_i >> 1) & 1u, &ctrl->abort, p.wait_ns);
         if (!ok) break;
         tc_fence_after();
@@ -952,7 +952,12 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
         if (lane == 0) mbar_arrive_relaxed(acc_empty_leader[job_i & 1u]);
         ++job_i;
       }
-      if (!ok) break;
+      if (!ok) {                                 // a wait gave up: NaN in place of this tile, and of all that follow
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int x = 0; x < 64; ++x) acc[u][x] = __int_as_float(0x7fc00000);
+      }
       if constexpr (KIND != kProducts) {
         const bool hy = j.b >= 0;
         const int cta_rows = hy ? p.th >> 1 : p.cta_rows, row = rank * cta_rows + in_cta;       // of the tile
