@@ -1267,7 +1267,8 @@ __global__ void __launch_bounds__(128) k_xent_hidden(Plan pl, const float* dh, l
   pdl_trigger();
   const int r = blockIdx.x, pos = pl.inv[r], i = (blockIdx.y * 128 + threadIdx.x) * 8;
   if (i >= d) return;
-  const int slots = pos < 0 ? 0 : split + (__float_as_int(pl.meta[pos].w) > 0 ? 1 : 0);       // (the last: hypertokens, if it sees any)
+  // (the last: hypertokens, if it sees any.  Without weight: none, since 0 times what the tables hold may be NaN)
+  const int slots = pos < 0 || pl.meta[pos].y == 0.f ? 0 : split + (__float_as_int(pl.meta[pos].w) > 0 ? 1 : 0);
   float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const float* from = dh + (size_t)(pos < 0 ? 0 : pos) * d + i;
   constexpr int kAhead = 4;
