@@ -340,7 +340,8 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  *            zero).  0: every row of d_grad_WU and the n_b rows of every sequence of d_grad_Uh are written.  Rows of
  *            d_grad_Uh from n_b on stay as they are either way;
  *   d_grad_hidden, d_grad_WU, d_grad_Uh: 16-byte aligned, apart from all inputs and one another; each may be NULL.
- * The row of a NaN or +inf logit has a NaN loss and, with a weight, NaN gradients, which reach the tables' too.
+ * The row of a NaN or +inf logit has a NaN loss and, with a weight, NaN gradients, which reach all of d_grad_WU and of its
+ * sequence's d_grad_Uh.  Entries that a row does not see do not reach its loss or gradient, whatever they hold.
  * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]) is rounded to bf16 for gradients stored in
  * bf16 and has 24 bits for fp32 gradients of the tables.  fp32 sessions: fp32's precision throughout.  The same call
  * gives the same bits.

@@ -73,7 +73,8 @@ static_assert(sizeof(Ctrl) <= 1024 && kFrontBytes % 1024 == 0, "control block");
 
 // What the plan leaves in the scratch.
 struct Plan {
-  int32_t* head;             // [0] rows that take part, [1..3] jobs of hypertokens: logits, hidden, tables; [4] largest weight
+  int32_t* head;             // [0] rows that take part, [1..3] jobs of hypertokens: logits, hidden, tables; [4] largest weight;
+                             // [5] a wait of this call has given up
   int32_t* cnt;              // [B] rows of a sequence that take part
   int32_t *s0, *h0;          // [B + 1] first position of a sequence's rows, and the one beside its hypertokens
   int32_t *j1, *j2, *j3;     // [B + 1] jobs of the sequences before
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(THREADS) k_xent_plan(CbView cb, RowArgs a, Pla
   if (tid == 0) {
 #pragma unroll
     for (int i = 0; i < 5; ++i) out[i][cb.B] = total[i];
-    pl.head[0] = total[0]; pl.head[1] = total[2]; pl.head[2] = total[3]; pl.head[3] = total[4]; pl.head[4] = __float_as_int(wmax);
+    pl.head[0] = total[0]; pl.head[1] = total[2]; pl.head[2] = total[3]; pl.head[3] = total[4]; pl.head[4] = __float_as_int(wmax); pl.head[5] = 0;
   }
   __syncthreads();
 
@@ -1103,6 +1104,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
   __syncthreads();
   if (threadIdx.x == 0 && ctrl->abort) {
     atomicOr(p.err, 1);
+    p.pl.head[5] = 1;
     st_cluster_u32(map_to_cta(smem_u32(&ctrl->other_abort), rank ^ 1), 1u);
   }
   __syncwarp();
@@ -1261,8 +1263,13 @@ __global__ void __launch_bounds__(kKeptThreads, 5) k_xent_kept(CbView cb, RowArg
 }
 
 // dh of a row: its partial sums, those of the vocabulary's parts first, times the largest weight.
+// The tiles of dh contract all entries of a sequence, with g = 0 for those that a row does not see; where these are not finite
+// (not computed yet, maybe) the row's sum over the entries that it does see is taken here, one by one.  A call without
+// such entries pays a comparison; with them 333 rows that see up to 150 entries take 43 us more (d = 1024, all of it 223), 3680 rows
+// of up to 780 1.2 ms (d = 4096; 9.1).
+struct SeenArgs { const __nv_bfloat16* gh; long long plane; int pitch, parts; const void* Uh; const int32_t* row_seq; };
 template <typename T>
-__global__ void __launch_bounds__(128) k_xent_hidden(Plan pl, const float* dh, long long slot, int split, T* out, int d) {
+__global__ void __launch_bounds__(128) k_xent_hidden(CbView cb, Plan pl, const float* dh, long long slot, int split, SeenArgs u, T* out, int d) {
   pdl_wait();
   pdl_trigger();
   const int r = blockIdx.x, pos = pl.inv[r], i = (blockIdx.y * 128 + threadIdx.x) * 8;
@@ -1285,6 +1292,38 @@ __global__ void __launch_bounds__(128) k_xent_hidden(Plan pl, const float* dh, l
       if (k0 + k >= slots) break;
       s[0] += v[k][0].x; s[1] += v[k][0].y; s[2] += v[k][0].z; s[3] += v[k][0].w;
       s[4] += v[k][1].x; s[5] += v[k][1].y; s[6] += v[k][1].z; s[7] += v[k][1].w;
+    }
+  }
+  if (slots > split) {
+    bool finite = true;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) finite &= fabsf(s[k]) < INFINITY;
+    const float4 m = pl.meta[pos];
+    if (!finite && fabsf(m.x) < INFINITY && fabsf(m.y) < INFINITY && !pl.head[5]) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[k] = 0.f;
+      for (int j = 0; j < split; ++j)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] += __ldcg(from + (size_t)j * slot + k);
+      const T* entry = reinterpret_cast<const T*>(u.Uh) + (size_t)(u.row_seq ? u.row_seq[r] : r) * cb.cap * d + i;
+      const __nv_bfloat16* g = u.gh + (size_t)pl.place[pos].x * u.pitch;
+      const int last = u.parts > 1 ? 1 : 0;      // (one part, or three)
+#pragma unroll 8
+      for (int e = 0; e < __float_as_int(m.w); ++e, entry += d) {
+        const float w = __bfloat162float(g[e]) + last * (__bfloat162float(g[last * u.plane + e]) + __bfloat162float(g[2 * last * u.plane + e]));
+        float x[8];
+        if constexpr (sizeof(T) == 4) {
+          const float4 a = *reinterpret_cast<const float4*>(entry), b = *reinterpret_cast<const float4*>(entry + 4);
+          x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        } else {
+          const uint4 a = *reinterpret_cast<const uint4*>(entry);
+          const uint32_t o[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(o[k] << 16); x[2 * k + 1] = __uint_as_float(o[k] & 0xffff0000u); }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] = fmaf(w, x[k], s[k]);
+      }
     }
   }
   if (slots) {
@@ -1618,9 +1657,11 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
     if (e != cudaSuccess) return e;
   }
   if (!x.g_hidden) return cudaSuccess;
+  const SeenArgs seen{l.gh, p.gh_plane, p.gh_pitch, p.g_parts, x.Uh, x.row_seq};
+  const dim3 grid(x.N, (d + 1023) / 1024);
   return sh.dtype == Z2Z_DTYPE_FP32
-             ? launch_pdl(k_xent_hidden<float>, dim3(x.N, (d + 1023) / 1024), dim3(128), 0, s, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<float*>(x.g_hidden), d)
-             : launch_pdl(k_xent_hidden<__nv_bfloat16>, dim3(x.N, (d + 1023) / 1024), dim3(128), 0, s, l.pl, l.dh, p.dh_slot, sh.split, reinterpret_cast<__nv_bfloat16*>(x.g_hidden), d);
+             ? launch_pdl(k_xent_hidden<float>, grid, dim3(128), 0, s, cb, l.pl, l.dh, p.dh_slot, sh.split, seen, reinterpret_cast<float*>(x.g_hidden), d)
+             : launch_pdl(k_xent_hidden<__nv_bfloat16>, grid, dim3(128), 0, s, cb, l.pl, l.dh, p.dh_slot, sh.split, seen, reinterpret_cast<__nv_bfloat16*>(x.g_hidden), d);
 }
 
 }  // namespace
