@@ -335,14 +335,15 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  *   d_targets [N]: a code the row sees.  A row with Z2Z_CODE_NONE, or of no sequence of the session, takes no part:
  *            loss 0, lse 0, gradient 0, whatever its hidden row holds, and no time.  So does a code that the row
  *            does not see; it sets Z2Z_ST_BAD_TOKEN for its sequence;
- *   w [N] or NULL = 1: a row whose weight is 0 has gradient 0 whatever its logits are;
+ *   w [N] or NULL = 1: a row whose weight is 0 has gradient 0 whatever its logits are; the gradients of a row whose weight
+ *            is not finite, and of the tables, are not either;
  *   accumulate  1: added to what the tables' gradients hold, rounded once (fp32: what is below the normal range may become
  *            zero).  0: every row of d_grad_WU and the n_b rows of every sequence of d_grad_Uh are written.  Rows of
  *            d_grad_Uh from n_b on stay as they are either way;
  *   d_grad_hidden, d_grad_WU, d_grad_Uh: 16-byte aligned, apart from all inputs and one another; each may be NULL.
  * The row of a NaN or +inf logit has a NaN loss and, with a weight, NaN gradients, which reach all of d_grad_WU and of its
  * sequence's d_grad_Uh.  Entries that a row does not see do not reach its loss or gradient, whatever they hold.
- * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]) is rounded to bf16 for gradients stored in
+ * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]), of the finite weights, is rounded to bf16 for gradients stored in
  * bf16 and has 24 bits for fp32 gradients of the tables.  fp32 sessions: fp32's precision throughout.  The same call
  * gives the same bits.
  *   d_scratch: 256-byte aligned, at least *out_least bytes of z2z_xent_scratch_bytes (for the session's configuration,

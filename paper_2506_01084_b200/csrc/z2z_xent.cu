@@ -73,7 +73,7 @@ static_assert(sizeof(Ctrl) <= 1024 && kFrontBytes % 1024 == 0, "control block");
 
 // What the plan leaves in the scratch.
 struct Plan {
-  int32_t* head;             // [0] rows that take part, [1..3] jobs of hypertokens: logits, hidden, tables; [4] largest weight;
+  int32_t* head;             // [0] rows that take part, [1..3] jobs of hypertokens: logits, hidden, tables; [4] largest finite weight, or 1;
                              // [5] a wait of this call has given up
   int32_t* cnt;              // [B] rows of a sequence that take part
   int32_t *s0, *h0;          // [B + 1] first position of a sequence's rows, and the one beside its hypertokens
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(THREADS) k_xent_plan(CbView cb, RowArgs a, Pla
     if (tgt[u] < 0 || tgt[u] >= cb.V + nv[u]) atomicOr(&cb.status[b], Z2Z_ST_BAD_TOKEN);
     else if (w[u] != 0.f || a.loss_out) q[u] = b;
   };
-  int wbits = 0; bool wnan = false;
+  int wbits = 0;
   for (int r0 = 0; r0 < a.N; r0 += kBatchRows) {
     if (r0) load(r0);
 #pragma unroll
@@ -195,20 +195,18 @@ __global__ void __launch_bounds__(THREADS) k_xent_plan(CbView cb, RowArgs a, Pla
       if (q[u] >= 0) {
         atomicAdd(&s_cnt[q[u]], 1);
         const float x = fabsf(w[u]);
-        if (x != x) wnan = true;
-        wbits = max(wbits, __float_as_int(x));
+        if (x < INFINITY) wbits = max(wbits, __float_as_int(x));
       } else {
         if (a.loss_out) a.loss_out[r] = 0.f;
         if (a.lse_out) a.lse_out[r] = 0.f;
       }
     }
   }
-  // (magnitudes compare as whole numbers)
-  if (wnan) wbits = 0x7fc00000;
+  // (magnitudes compare as whole numbers.  A weight that is not finite stays what it is in its own row)
   wbits = __reduce_max_sync(0xffffffffu, wbits);
   if (lane == 0) atomicMax(reinterpret_cast<int*>(&sh.wmax), wbits);
   __syncthreads();
-  const float wmax = sh.wmax;
+  const float wmax = sh.wmax > 0.f ? sh.wmax : 1.f;
 
   // prefix sums over the sequences (B <= 1024: one each)
   const int b = tid, c = b < cb.B ? s_cnt[b] : 0, n = b < cb.B ? s_n[b] : 0;
