@@ -343,6 +343,8 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  *   d_grad_hidden, d_grad_WU, d_grad_Uh: 16-byte aligned, apart from all inputs and one another; each may be NULL.
  * The row of a NaN or +inf logit has a NaN loss and, with a weight, NaN gradients, which reach all of d_grad_WU and of its
  * sequence's d_grad_Uh.  Entries that a row does not see do not reach its loss or gradient, whatever they hold.
+ * z2z_xent_grad knows lse to fp32's rounding alone, |lse| 2^-24, by which its p are off and which hides the gradient of a
+ * target whose loss is smaller; z2z_xent_step does not lose it.
  * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]), of the finite weights, is rounded to bf16 for gradients stored in
  * bf16 and has 24 bits for fp32 gradients of the tables.  fp32 sessions: fp32's precision throughout.  The same call
  * gives the same bits.

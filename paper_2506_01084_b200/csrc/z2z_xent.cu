@@ -982,6 +982,13 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             const int cols = min(64, j.n - 128 * half - 64 * u);
             if (cols <= 0 || rows <= 0) continue;
             float (&v)[64] = acc[u];
+            // (the target's, p - 1, from its logit: of a row that is sure of it p is 1 after rounding)
+            const bool target = __any_sync(0xffffffffu, at >= 64 * u && at < 64 * u + 64);
+            float l = 0.f;
+            if (target) {
+#pragma unroll
+              for (int x = 0; x < 64; ++x) l = x == at - 64 * u ? v[x] : l;
+            }
             if (p.exact_exp) {
 #pragma unroll
               for (int x = 0; x < 64; ++x) v[x] = exp_exact((v[x] - lse) - rest);
@@ -989,9 +996,10 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
 #pragma unroll
               for (int x = 0; x < 64; ++x) v[x] = ex2((v[x] - lse) * kLog2e);
             }
-            if (__any_sync(0xffffffffu, at >= 64 * u && at < 64 * u + 64)) {
+            if (target) {
+              l = expm1f((l - lse) - rest);
 #pragma unroll
-              for (int x = 0; x < 64; ++x) v[x] -= x == at - 64 * u ? 1.f : 0.f;
+              for (int x = 0; x < 64; ++x) v[x] = x == at - 64 * u ? l : v[x];
             }
 #pragma unroll
             for (int x = 0; x < 64; ++x) v[x] *= weight;
@@ -1184,8 +1192,9 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
 // zeros.
 struct KeptArgs { __nv_bfloat16* g; int pitch; const float2* part; int part_rows, nv; };
 constexpr int kKeptThreads = 256, kKeptVecs = 2, kKeptStep = 8 * kKeptThreads * kKeptVecs, kKeptColumns = 32768;
-// see: columns that the row sees; those behind them up to `cols` become zeros.
-__device__ __forceinline__ void kept_columns(uint16_t* g, int lo, int cols, int see, const float2* part, int part_rows, int nv, const float4& r, int target, float tl) {
+// see: columns that the row sees; those behind them up to `cols` become zeros.  less_one: p - 1 of the target.
+__device__ __forceinline__ void kept_columns(uint16_t* g, int lo, int cols, int see, const float2* part, int part_rows, int nv, const float4& r, int target,
+                                             float less_one) {
   const float lse = r.x, weight = r.y, none = lse - lse;                     // (0, or NaN for a row of NaN)
   const int hi = min(cols, lo + kKeptColumns), v0 = lo + 8 * (int)threadIdx.x;
   uint4 w[kKeptVecs];
@@ -1225,7 +1234,7 @@ __device__ __forceinline__ void kept_columns(uint16_t* g, int lo, int cols, int 
         for (int k = 0; k < 8; ++k) if (weight == 0.f || c + k >= see) x[k] = 0.f;
       }
       if (target >= c && target < c + 8 && weight != 0.f) {
-        const float e = weight * (expf(tl - lse) - 1.f);
+        const float e = weight * less_one;
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = c + k == target ? e : x[k];
       }
@@ -1241,7 +1250,7 @@ __global__ void __launch_bounds__(kKeptThreads, 5) k_xent_kept(CbView cb, RowArg
   for (long long i = blockIdx.x; i < units; i += gridDim.x) {
     const int pos = (int)(i / (chunks + hyper)), chunk = (int)(i - (long long)pos * (chunks + hyper));
     const float4 r = pos < live ? pl.meta[pos] : make_float4(0.f, 0.f, __int_as_float(-1), 0.f);
-    const float t = pos < live ? tl[pos] : 0.f;
+    const float t = pos < live ? expm1f((tl[pos] - r.x) - pl.rest[pos]) : 0.f;
     const int target = __float_as_int(r.z);
     if (chunk < chunks) {
       kept_columns(reinterpret_cast<uint16_t*>(w.g) + (size_t)pos * w.pitch, chunk * kKeptColumns, pad64(cb.V), cb.V, w.part + pos, w.part_rows, w.nv, r,
