@@ -346,8 +346,8 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  * z2z_xent_grad knows lse to fp32's rounding alone, |lse| 2^-24, by which its p are off and which hides the gradient of a
  * target whose loss is smaller; z2z_xent_step does not lose it.
  * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]), of the finite weights, is rounded to bf16 for gradients stored in
- * bf16 and has 24 bits for fp32 gradients of the tables.  fp32 sessions: fp32's precision throughout.  The same call
- * gives the same bits.
+ * bf16 and has 24 bits for fp32 gradients of the tables.  fp32 sessions: fp32's precision throughout (but for
+ * lse in z2z_xent_grad).  The same call gives the same bits.
  *   d_scratch: 256-byte aligned, at least *out_least bytes of z2z_xent_scratch_bytes (for the session's configuration,
  *            N and grad_dtype, -1 for z2z_xent_loss alone); up to *out_most, more makes the pieces larger and the call
  *            faster: with the most a bf16 z2z_xent_step keeps its logits, in 16 bits each (within 4 GB), instead of

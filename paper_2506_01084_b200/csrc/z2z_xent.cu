@@ -558,10 +558,13 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// exp with the rounding of x log2 e made good: ex2's own error (2^-22) is what is left.
-__device__ __forceinline__ float exp_exact(float x) {
-  const float y = x * kLog2e, r = fmaf(x, kLog2e, -y), e = ex2(y);
-  return y > -200.f ? fmaf(e, r * 0.69314718f, e) : e;                       // (-inf: r is no number)
+// exp(v - lse - rest) with all roundings of the exponent made good, the difference's own (half a step of 9 is 2^-21) and
+// those of log2 e among them: ex2's own error (2^-22) is what is left.
+constexpr float kLog2eRest = 1.92596299e-8f;     // log2 e less kLog2e
+__device__ __forceinline__ float exp_exact(float v, float lse, float rest) {
+  const float x = v - lse, b = x - v, lost = (v - (x - b)) - (lse + b);      // (x + lost is the difference)
+  const float y = x * kLog2e, r = fmaf(x, kLog2eRest, fmaf(x, kLog2e, -y)), e = ex2(y);
+  return y > -200.f ? fmaf(e, fmaf(r, 0.69314718f, lost - rest), e) : e;     // (-inf: lost is no number)
 }
 
 __device__ __forceinline__ void merge_ms(float& m, float& s, float om, float os) {
@@ -991,7 +994,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             }
             if (p.exact_exp) {
 #pragma unroll
-              for (int x = 0; x < 64; ++x) v[x] = exp_exact((v[x] - lse) - rest);
+              for (int x = 0; x < 64; ++x) v[x] = exp_exact(v[x], lse, rest);
             } else {
 #pragma unroll
               for (int x = 0; x < 64; ++x) v[x] = ex2((v[x] - lse) * kLog2e);
@@ -1173,10 +1176,12 @@ __global__ void __launch_bounds__(1024) k_xent_merge(CbView cb, RowArgs a, Plan 
   }
   const int row = pl.perm[pos];
   if (lane == 0) {
-    const float ls = logf(s);
-    a.lse_out[row] = m + ls;
-    a.loss_out[row] = ls + (m - tl[pos]);
-    if (parts_of_rows) { pl.meta[pos].x = m + ls; pl.rest[pos] = m == INFINITY ? 0.f : (m - (m + ls)) + ls; }
+    // (64 bits: what lse loses to its rounding is kept, and a logarithm of 8 to 16 is off by as much in 32)
+    const double ls = log((double)s), sum = (double)m + ls;
+    const float lse = (float)sum;
+    a.lse_out[row] = lse;
+    a.loss_out[row] = (float)(ls + ((double)m - (double)tl[pos]));
+    if (parts_of_rows) { pl.meta[pos].x = lse; pl.rest[pos] = fabsf(lse) < INFINITY ? (float)(sum - lse) : 0.f; }
   }
   if (parts_of_rows && pl.meta[pos].y == 0.f) {
     const int h = pl.place[pos].x;
