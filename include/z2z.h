@@ -345,8 +345,8 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  * sequence's d_grad_Uh.  Entries that a row does not see do not reach its loss or gradient, whatever they hold.
  * z2z_xent_grad knows lse to fp32's rounding alone, |lse| 2^-24, by which its p are off and which hides the gradient of a
  * target whose loss is smaller; z2z_xent_step does not lose it.
- * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]), of the finite weights, is rounded to bf16 for gradients stored in
- * bf16 and has 24 bits for fp32 gradients of the tables.  fp32 sessions: fp32's precision throughout (but for
+ * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]), of the finite weights, is rounded to bf16 where the tables'
+ * gradients are bf16; for fp32 ones it has 24 bits there, and 16 for d_grad_hidden.  fp32 sessions: fp32's precision throughout (but for
  * lse in z2z_xent_grad).  The same call gives the same bits.
  *   d_scratch: 256-byte aligned, at least *out_least bytes of z2z_xent_scratch_bytes (for the session's configuration,
  *            N and grad_dtype, -1 for z2z_xent_loss alone); up to *out_most, more makes the pieces larger and the call

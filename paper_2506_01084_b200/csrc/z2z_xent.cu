@@ -497,16 +497,19 @@ struct GradWalk {
   }
 };
 
-// Without operands in several parts: times that the contracted axis is gone through, once for each part of g.
-__device__ __forceinline__ int job_turns(const Params& p, int type) { return type >= kTables ? p.g_parts : 1; }
+// Without operands in several parts: times that the contracted axis is gone through, once for each part of g.  (Gradients in
+// bf16, the form without chains: one.)
+__device__ __forceinline__ int job_turns(const Params& p, int type) { return type >= kTables ? p.g_parts : (type >= kHidden ? p.np2 : 1); }
 __device__ __forceinline__ int job_blocks(const Job& j) { return (j.k16 + 3) / 4 + (j.tail ? 1 : 0); }
 // The tensor cores' additions into an accumulator truncate: a chain of n of them is off by about n / 2 steps of 2^-24 to
 // one side (losses at d = 4096 were 3e-6 off).  Where that counts an accumulator takes so many blocks of 64, and the epilogue
 // adds those sums in registers, rounded to nearest, while the MMAs go on in the other accumulator.
-constexpr int kChain = 8;
+// (dh of a bf16 session: every 256 additions for g in two parts; with one, whose rounding is up to 2^-9 of each term, the
+// whole axis, 8000 additions and 2^-12 at V = 128256.)
+constexpr int kChain = 8, kChainHidden = 64;
 __device__ __forceinline__ int job_chain(const Params& p, const Job& j) {
   if (p.parts > 1) return 1;                     // (six products)
-  return j.type <= kLogitsHyper ? kChain : (j.type <= kHiddenHyper ? 1 << 30 : kChain);
+  return j.type <= kLogitsHyper ? kChain : (j.type <= kHiddenHyper ? kChainHidden : kChain);
 }
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long ns) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, ns));
@@ -782,7 +785,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
           A = Side{hy ? &tm.gh_m : &tm.g_m, j.m0 + rank * 128, h0, 0, 64, true, 16384u};
           B = Side{hy ? &tm.hh_m : &tm.hs_m, j.r0 + rank * half, h0, 0, 64, half > 64, half > 64 ? 16384u : 8192u};
         }
-        const int turns = MULTI ? 1 : job_turns(p, j.type);
+        const int turns = MULTI || !CHAINED ? 1 : job_turns(p, j.type);
         auto block = [&](int part, int ax, int ay, int bx, int by) {
           if constexpr (MULTI) {
             // (in the order in which the MMAs want them)
@@ -792,8 +795,9 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             one(A, ax, ay, 2); one(B, bx, by, 0); one(A, ax, ay, 0); one(B, bx, by, 2); one(A, ax, ay, 1); one(B, bx, by, 1);
           } else if (begin(A.bytes + B.bytes)) {
             const uint32_t at = stage_base + (uint32_t)stage * stage_bytes, bar = full_leader + 8u * stage;
-            load(A, at, bar, ax, ay, turns - 1 - part);        // (g's smallest part first)
-            load(B, at + b_off, bar, bx, by, 0);
+            // (g, the tables' A and dh's B, with its smallest part first)
+            load(A, at, bar, ax, ay, j.type >= kTables ? turns - 1 - part : 0);
+            load(B, at + b_off, bar, bx, by, j.type >= kTables ? 0 : turns - 1 - part);
             end();
           }
         };
@@ -803,10 +807,12 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
             block(part, ax, ay, bx, by);
             ax += A.dx; ay += A.dy; bx += B.dx; by += B.dy;
           }
-        }
-        if (KIND == kProducts && j.tail && ok) { // (dh alone: one turn)
-          A.m = &tm.ut_m; A.bytes = 4096u;
-          block(0, A.x, j.b * 16, j.k16 * 16, B.y);
+          if (KIND == kProducts && j.tail && ok) {
+            const Side entries = A;
+            A.m = &tm.ut_m; A.bytes = 4096u;
+            block(part, A.x, j.b * 16, j.k16 * 16, B.y);
+            A = entries;
+          }
         }
       }
       ctrl->issued = issued;
@@ -840,7 +846,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
           for (int k = 0; k < 4; ++k)
             if (k < steps) umma_bf16_pair(D, a + k * a_step, b + k * b_step, idesc, k ? 1u : acc);
         };
-        const int turns = MULTI ? 1 : job_turns(p, j.type);
+        const int turns = MULTI || !CHAINED ? 1 : job_turns(p, j.type);
         for (int i = 0, kb = 0; i < blocks * turns; ++i, kb = kb + 1 == blocks ? 0 : kb + 1) {
           if (left == 0) {
             if (i) { if (elect_one()) umma_commit_pair(smem_u32(&ctrl->acc_full[job_i & 1u])); __syncwarp(); ++job_i; }
@@ -910,7 +916,7 @@ k_xent(const __grid_constant__ Params p, const __grid_constant__ Maps tm) {
     uint32_t job_i = 0;
     bool ok = true;
     while (w.next(j)) {
-      const int blocks = job_blocks(j) * (MULTI ? 1 : job_turns(p, j.type)), chain = CHAINED ? job_chain(p, j) : 1 << 30;
+      const int blocks = job_blocks(j) * (MULTI || !CHAINED ? 1 : job_turns(p, j.type)), chain = CHAINED ? job_chain(p, j) : 1 << 30;
       const bool some = blocks > 0;
       // the tile's sums, after which its accumulators are free
       float acc[2][64];                          // columns 128 half + 64 u + x
@@ -1586,8 +1592,8 @@ cudaError_t run_passes(const CbView& cb, const z2z_config& cfg, const XentArgs& 
   p.cb = cb; p.pl = l.pl; p.d = d; p.dt = sh.dt; p.cta_rows = sh.cta_rows; p.nv = sh.nv; p.tr = sh.tr;
   p.a_bytes = (int)up_to(128ll * (sh.cap > 0 && sh.th / 2 > sh.cta_rows ? sh.th / 2 : sh.cta_rows), 1024); p.th = sh.th;
   p.parts = sh.parts;
-  // (dh of a bf16 session takes the first of g's parts: it is stored in bf16)
-  p.np2 = sh.parts > 1 ? 6 : 1; p.np3 = sh.parts > 1 ? 6 : sh.g_parts;
+  // (dh of a bf16 session is stored in bf16: of g's three parts for fp32 gradients it takes two, 16 bits)
+  p.np2 = sh.parts > 1 ? 6 : (sh.g_parts > 1 ? 2 : 1); p.np3 = sh.parts > 1 ? 6 : sh.g_parts;
   p.g_parts = sh.g_parts; p.exact_exp = sh.g_parts > 1;
   p.g = l.g; p.g_pitch = sh.vc; p.g_plane = (long long)sh.vc * sh.np;
   p.gh = l.gh; p.gh_pitch = hyper_rows(sh); p.gh_plane = (long long)hyper_rows(sh) * sh.nh;
