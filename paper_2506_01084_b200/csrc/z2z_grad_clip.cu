@@ -164,8 +164,15 @@ __global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_norm(const 
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
+// What a gradient is multiplied by: `factor`, after `pre` (1, or a power of two where the product of both is below the
+// normal range, so that it keeps its bits).
+struct Scale {
+  float pre, factor;
+  __device__ __forceinline__ float operator()(float x) const { return x * pre * factor; }
+};
+
 template <bool FROM, bool TO>
-__device__ __forceinline__ void chunk_scale(const Record& r, const Span& s, float factor) {
+__device__ __forceinline__ void chunk_scale(const Record& r, const Span& s, const Scale& by) {
   constexpr int kPer = FROM ? 8 : 4, kOut = kPer * (TO ? 2 : 4), kAlign = kOut < 16 ? kOut : 16;
   constexpr int kBatch = 4;                      // vectors loaded before any is used
   const int head = abs(s.head);
@@ -185,7 +192,7 @@ __device__ __forceinline__ void chunk_scale(const Record& r, const Span& s, floa
       float x[kPer];
       unpack<FROM>(v[u], x);
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) x[k] *= factor;
+      for (int k = 0; k < kPer; ++k) x[k] = by(x[k]);
       char* at = to + (size_t)i * kOut;
       if (!whole) {
 #pragma unroll
@@ -215,7 +222,7 @@ __device__ __forceinline__ void chunk_scale(const Record& r, const Span& s, floa
 template <int MAX>
 __global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_scale(const __grid_constant__ Records<MAX> t, const double* part, int parts, float scale, float max_norm,
                                                              float* norm_out) {
-  __shared__ float s_factor;
+  __shared__ Scale s_by;
   __shared__ int s_write;
   pdl_wait();
   pdl_trigger();
@@ -225,24 +232,33 @@ __global__ void __launch_bounds__(kClipThreads, kBlocksPerSm) k_clip_scale(const
   if (threadIdx.x == 0) {
     const float norm = (float)(fabs((double)scale) * sqrt(sum));
     if (norm_out && blockIdx.x == 0) *norm_out = norm;
-    s_factor = scale * fminf(1.f, max_norm / (norm + 1e-6f));
+    const float less = fminf(1.f, max_norm / (norm + 1e-6f));
+    Scale by{1.f, scale * less};
+    constexpr float kNormal = 0x1p-126f;
+    if (less < kNormal || fabsf(by.factor) < kNormal) {
+      // (gradients of 1e38, which a normal factor would not bring below the largest norm; 2^-100: whatever then leaves the
+      // range below would be zero after the other factor, too)
+      const double q = (double)scale * fmin(1.0, (double)max_norm / ((double)norm + 1e-6));
+      by = fabs(q) < kNormal ? Scale{0x1p-100f, (float)(q * 0x1p100)} : Scale{1.f, (float)q};
+    }
+    s_by = by;
     s_write = norm < INFINITY;                   // (nor a NaN)
   }
   __syncthreads();
   if (!s_write) return;
-  const float factor = s_factor;
+  const Scale by = s_by;
   for (int c = t.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
     const Record& r = t.r[record_of(t, c)];
-    if (!r.out || (r.out == r.g && factor == 1.f)) continue;
+    if (!r.out || (r.out == r.g && by.factor == 1.f)) continue;
     const Span s = span_of(r, c);
     switch (r.type) {
-      case 0: chunk_scale<false, false>(r, s, factor); break;
-      case 1: chunk_scale<true, false>(r, s, factor); break;
-      case 2: chunk_scale<false, true>(r, s, factor); break;
-      default: chunk_scale<true, true>(r, s, factor); break;
+      case 0: chunk_scale<false, false>(r, s, by); break;
+      case 1: chunk_scale<true, false>(r, s, by); break;
+      case 2: chunk_scale<false, true>(r, s, by); break;
+      default: chunk_scale<true, true>(r, s, by); break;
     }
-    if (s.head > (int)threadIdx.x) store_one(r, threadIdx.x, load_one(r, threadIdx.x) * factor);
-    if (s.tail0 + threadIdx.x < r.n) store_one(r, s.tail0 + threadIdx.x, load_one(r, s.tail0 + threadIdx.x) * factor);
+    if (s.head > (int)threadIdx.x) store_one(r, threadIdx.x, by(load_one(r, threadIdx.x)));
+    if (s.tail0 + threadIdx.x < r.n) store_one(r, s.tail0 + threadIdx.x, by(load_one(r, s.tail0 + threadIdx.x)));
   }
 }
 
