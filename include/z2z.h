@@ -322,8 +322,8 @@ int32_t z2z_distill_grad(const void* d_logits, int32_t dtype, int32_t N, int32_t
  * makes from now on; 0 = the default, 400 ms.  A process that shares its GPU with others in turn may have to wait longer.  */
 int32_t z2z_set_distill_wait_limit(int64_t ns);
 
-/* Cross entropy over the joint vocabulary, from hidden rows and without stored logits: with the columns of row r
- * (W_U, then the first n_vis rows of its sequence's U_h) as for z2z_dynamic_logits and l its logits,
+/* Cross entropy over the joint vocabulary, from hidden rows and without a matrix of logits (but see d_scratch): with the
+ * columns of row r (W_U, then the first n_vis rows of its sequence's U_h) as for z2z_dynamic_logits and l its logits,
  *   loss_r = lse_r - l_{t_r},  lse_r = log sum_c exp(l_c),      d loss_r / d l_c = exp(l_c - lse_r) - [c = t_r].
  * z2z_xent_loss gives the losses.  z2z_xent_grad is the backward pass on its own: d_grad_loss [N] = w is the
  * derivative for d_loss, d_lse what z2z_xent_loss left there for the same arguments; it computes the logits again,
@@ -345,13 +345,14 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  * sequence's d_grad_Uh.  Entries that a row does not see do not reach its loss or gradient, whatever they hold.
  * z2z_xent_grad knows lse to fp32's rounding alone, |lse| 2^-24, by which its p are off and which hides the gradient of a
  * target whose loss is smaller; z2z_xent_step does not lose it.
- * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]), of the finite weights, is rounded to bf16 where the tables'
- * gradients are bf16; for fp32 ones it has 24 bits there, and 16 for d_grad_hidden.  fp32 sessions: fp32's precision throughout (but for
- * lse in z2z_xent_grad).  The same call gives the same bits.
+ * bf16 sessions: products of bf16 with fp32 sums; w_r / max |w| (p - [c = t]), the maximum over finite weights, is rounded
+ * to bf16 where the tables' gradients are bf16; for fp32 ones it has 24 bits there, and 16 for d_grad_hidden.  fp32
+ * sessions: fp32's precision throughout (but for lse in z2z_xent_grad).  The same call gives the same bits.
  *   d_scratch: 256-byte aligned, at least *out_least bytes of z2z_xent_scratch_bytes (for the session's configuration,
  *            N and grad_dtype, -1 for z2z_xent_loss alone); up to *out_most, more makes the pieces larger and the call
- *            faster: with the most a bf16 z2z_xent_step keeps its logits, in 16 bits each (within 4 GB), instead of
- *            computing them twice.  How the sums are cut depends on it.  Its contents need not be kept between
+ *            faster: with the most a z2z_xent_step of a bf16 session with bf16 gradients keeps its logits, in 16 bits
+ *            each (within 4 GB), instead of computing them twice; its p are then off by up to 2^-12 of themselves, and 0
+ *            below e^-32 of the largest among 128 columns.  With less it keeps none.  How the sums are cut depends on it.  Its contents need not be kept between
  *            calls; calls that share it must be ordered by the caller.
  * The calls run on the tensor cores whatever z2z_set_tensor_cores says.  Waits inside them are bounded
  * (z2z_set_xent_wait_limit); one that gives up sets Z2Z_ST_WAIT_TIMEOUT (z2z_status) and leaves NaN in every result that

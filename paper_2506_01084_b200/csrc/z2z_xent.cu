@@ -1,5 +1,5 @@
 // Cross entropy of hidden rows over the joint vocabulary (what the model is trained on: paper Section 2.4 with the
-// distribution of Section 2.3 steps 7-9), without stored logits, and its gradients.
+// distribution of Section 2.3 steps 7-9), without a matrix of fp32 logits, and its gradients.
 //
 //   l_rv   = h_r . W_v            v over the rows of W_U and the visible rows of U_h of the row's sequence
 //   loss_r = log sum_v exp l_rv - l_rt
@@ -18,17 +18,20 @@
 // Rows are sorted by their sequence first (stable), and rows without a target, which add nothing, are left out.
 // Hypertokens are a piece per sequence: its entries against its own rows, which start at a multiple of 32 there.
 // A step whose scratch has room for N (V + cap) values of 16 bits keeps its logits from the losses to the gradients, as
-// distances in fixed point: three contractions then, not four.
+// distances in fixed point: three contractions then, not four (4096 rows, V = 128256, d = 4096: 9.4 ms, 11.9 without; 48 rows
+// 0.70 and 0.96).
 //
 // Bound by the tensor cores from some hundred rows on (their power, in calls of milliseconds), below by memory: W_U is read
 // twice and its gradient written once.  V = 128256, d = 4096, bf16: losses of 2047 rows (1842 with a target) 1.57 ms,
-// 1.25 PFLOP/s; a step of 4096 (3680) rows 9.9 ms, 1.18 PFLOP/s of three contractions; a step of 48 rows 0.75 ms, 2.8 TB/s.
+// 1.25 PFLOP/s (1.34 on a cool board); a step of 4096 (3680) rows 9.1 to 9.8 ms, 1.2 PFLOP/s of three contractions; a step of 48
+// rows 0.70 to 0.75 ms, 4.2 to 4.5 TB/s of W_U twice and its gradient.
 //
 // Numbers.  A bf16 session's g is rounded once to bf16 for gradients stored in bf16; for fp32 gradients of the tables
-// it is three bf16 parts (24 bits).  An fp32 session has all operands in three parts, and takes the six products of
-// parts that fp32 can hold.  Accumulators are fp32 in tensor memory.  Weights enter as w_r / max w, so that equal
-// weights lose nothing to g's rounding, and the maximum multiplies the sums.  Orders of summation depend on sizes
-// only: the same call gives the same bits.
+// it is three bf16 parts (24 bits), of which dh takes two.  An fp32 session has all operands in three parts, and takes
+// the six products of parts that fp32 can hold.  Accumulators are fp32 in tensor memory.  Weights enter as w_r / max w, so
+// that equal weights lose nothing to g's rounding, and the maximum (of the finite weights) multiplies the sums.  lse
+// carries what its rounding loses, and the target's p - 1 is an expm1: a row that is sure of its target keeps its gradient.
+// Orders of summation depend on sizes only: the same call gives the same bits.
 #include <atomic>
 
 #include "z2z_common.cuh"
@@ -46,6 +49,8 @@ constexpr int kEpiWarps = 8;                     // two per tensor-memory lane q
 constexpr int kThreads = 128 + 32 * kEpiWarps;   // a warpgroup of producer, issuer and two that leave; two of the epilogue
 // Registers: 384 threads are launched with 168 each; the epilogue, which holds a tile's sums, takes what the others leave
 // (128 x 56 + 256 x 224 = 384 x 168; a launch with fewer is refused, since the epilogue would wait for the rest forever).
+// The forms of the products spill 76 to 174 bytes a thread, those of the logits none, or 20 to 48 without chains; 190 bytes
+// instead of 174 took the same time.
 constexpr int kRegsFew = 56, kRegsEpi = 224;
 constexpr int kRegsAtLaunch = (128 * kRegsFew + 32 * kEpiWarps * kRegsEpi) / kThreads;
 constexpr int kRing = 10;                        // stages at most
@@ -1283,8 +1288,8 @@ __global__ void __launch_bounds__(kKeptThreads, 5) k_xent_kept(CbView cb, RowArg
 // dh of a row: its partial sums, those of the vocabulary's parts first, times the largest weight.
 // The tiles of dh contract all entries of a sequence, with g = 0 for those that a row does not see; where these are not finite
 // (not computed yet, maybe) the row's sum over the entries that it does see is taken here, one by one.  A call without
-// such entries pays a comparison; with them 333 rows that see up to 150 entries take 43 us more (d = 1024, all of it 223), 3680 rows
-// of up to 780 1.2 ms (d = 4096; 9.1).
+// such entries pays a comparison; with them 333 rows that see up to 160 entries take 43 us more (d = 1024; the step 248), 3680 rows
+// of up to 760 1.2 ms (d = 4096; the step 9.1 ms).
 struct SeenArgs { const __nv_bfloat16* gh; long long plane; int pitch, parts; const void* Uh; const int32_t* row_seq; };
 template <typename T>
 __global__ void __launch_bounds__(128) k_xent_hidden(CbView cb, Plan pl, const float* dh, long long slot, int split, SeenArgs u, T* out, int d) {
