@@ -352,7 +352,8 @@ int32_t z2z_set_distill_wait_limit(int64_t ns);
  *            N and grad_dtype, -1 for z2z_xent_loss alone); up to *out_most, more makes the pieces larger and the call
  *            faster: with the most a z2z_xent_step of a bf16 session with bf16 gradients keeps its logits, in 16 bits
  *            each (within 4 GB), instead of computing them twice; its p are then off by up to 2^-12 of themselves, and 0
- *            below e^-32 of the largest among 128 columns.  With less it keeps none.  How the sums are cut depends on it.  Its contents need not be kept between
+ *            below e^-32 of the largest among 128 columns.  With less (of a large vocabulary), with fp32 gradients and in
+ *            z2z_xent_grad none are kept.  How the sums are cut depends on the scratch.  Its contents need not be kept between
  *            calls; calls that share it must be ordered by the caller.
  * The calls run on the tensor cores whatever z2z_set_tensor_cores says.  Waits inside them are bounded
  * (z2z_set_xent_wait_limit); one that gives up sets Z2Z_ST_WAIT_TIMEOUT (z2z_status) and leaves NaN in every result that
